@@ -238,10 +238,12 @@ class _Handles:
         held = _filled(d)
         self.set(d, np.zeros_like(held))
         if held.sum():
-            B.cs_plan_set(self.plan, np.arange(case["B"]), held)
+            some = np.flatnonzero(held)
+            B.cs_plan_set(self.plan, some, held[some])
             B.cs_kv_append(self.plan, 0, d["cached_k"], d["cached_v"], rotate=False)
         self.set(d, d["ctx"])
-        B.cs_plan_set(self.plan, np.arange(case["B"]), d["new"], given=case.get("new") == "given")
+        if d["new"].sum():
+            B.cs_plan_set(self.plan, np.arange(case["B"]), d["new"], given=case.get("new") == "given")
         torch.cuda.synchronize()
 
     def set(self, d, ctx):
