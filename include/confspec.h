@@ -136,13 +136,28 @@ int cs_kv_alloc(const cs_model* model, int num_pages, int page_size, int max_seq
  * It serves the decode-shaped use of the pass, where reading the cache bounds the time: cs_verify_steps accepts it
  * when every step has at most 32 query rows per kv head (step_lens[i] * n_q_heads / n_kv_heads <= 32; CS_EINVAL
  * otherwise), widens the codes to fp16 on the fly (exact) and computes as with the 16-bit cache. The format is
- * read-only for the pass: contexts come from cs_kv_fill (host arrays of uint8 codes instead of bf16 patterns);
- * cs_prefill and cs_append_accepted return CS_EINVAL on such a cache.
+ * read-only for the pass: contexts come from cs_kv_fill (host arrays of uint8 codes instead of bf16 patterns) or from
+ * cs_kv_append; cs_prefill and cs_append_accepted return CS_EINVAL on such a cache.
  */
 #define CS_KV_E4M3 1
 #define CS_KV_E5M2 2
 int cs_kv_alloc_8bit(const cs_model* model, int num_pages, int page_size, int max_seqs, int max_pages_per_seq,
                      int format, cs_kv** out);
+/*
+ * cs_kv_alloc_4bit - the same cache in 4 bits a value (no counterpart in the paper). The channels of a K or V row of one
+ * (token, kv head) are cut into groups of 64; a group x keeps an fp16 offset o = min x, an fp16 scale
+ * s = min((max x - min x) / 15, 1023.5) and a code c = rint((x - o) / s) in 0 .. 15 per channel (0 where s = 0), which stands
+ * for s c + o: off by at most s / 2 and the roundings of s and o, where the range of a group stays below 15352 (beyond it
+ * values saturate). A row takes head_dim / 2 + 4 head_dim / 64 bytes, 0.28 of a 16-bit row:
+ *   pool bytes = n_layers * num_pages * n_kv_heads * 18 * head_dim, library-owned.
+ * Every call takes it: cs_verify_steps, cs_verify_cascade, cs_prefill and cs_append_accepted (steps of any length), cs_kv_fill
+ * (bf16 rows, quantised on the way in), and the calls on a plan below. Within a pass the new tokens see one another's keys and
+ * values as computed (fp16); what is appended is quantised. Steps of more than 32 query rows per kv head (tokens x heads in the
+ * group) have their contexts expanded to fp16 layer by layer, into a scratch pool that the cache allocates at the first such
+ * step and keeps: 4 * num_pages * n_kv_heads * 16 * head_dim bytes.
+ */
+int cs_kv_alloc_4bit(const cs_model* model, int num_pages, int page_size, int max_seqs, int max_pages_per_seq,
+                     cs_kv** out);
 int cs_kv_free(cs_kv* kv);
 /* Bytes of pool that cs_kv_alloc needs for this geometry (0 on bad arguments). */
 uint64_t cs_kv_pool_bytes(const cs_model* model, int num_pages, int page_size);
@@ -160,10 +175,85 @@ int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int 
  * cs_kv_fill — write given K/V into the pages of sequence `seq` for one layer (synthetic contexts in
  * tests and benchmarks).
  *   host_k, host_v     host bf16 [ctx_len, n_kv_heads, head_dim] (uint8 codes of the same shape for a cache from
- *                      cs_kv_alloc_8bit); K already rotated.
+ *                      cs_kv_alloc_8bit; bf16 for one from cs_kv_alloc_4bit, quantised here); K already rotated.
  * Synchronous on `stream`.
  */
 int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint16_t* host_v, void* stream);
+
+/*
+ * Cache rows and attention outside the pass: for a program that runs its own layers (cs_gemm_f16, cs_rmsnorm and its own
+ * kernels) over the library's caches, one decode step or one chunk of a prompt at a time.
+ *
+ * A plan is a batch of steps over one cache, staged on the device once and used for every layer: the new tokens' places, their
+ * rotary table (cos and sin of pos * theta^(-2j/head_dim), computed in 64 bits), and the attention's work items.
+ *   cs_plan_create     max_tokens sizes the rotary table ahead (0: grown on demand); max_steps is a hint. A plan belongs to
+ *                      the cache and to the device that is current now; free it before the cache.
+ *   cs_plan_set        lens[i] >= 1 new tokens of sequence seq_ids[i], at positions ctx_len .. ctx_len + lens[i] - 1 (host
+ *                      arrays, read before the call returns). B = 0 is an empty plan. given = 0: the keys of the new tokens
+ *                      are in the cache when attention runs (cs_kv_append comes first), so every sequence needs pages for
+ *                      them (CS_EINVAL otherwise); given = 1: they are handed to cs_attention_4bit as rows, and the cache is
+ *                      read up to ctx_len only (the same sequence may then appear several times, as in cs_verify_steps).
+ *                      Uploads on `stream`; growing a buffer synchronises the device. Not inside a stream capture (CS_ESTATE).
+ *   cs_kv_commit       host only: the plan's tokens become context (ctx_len += lens[i]), once per cs_plan_set and after the
+ *                      last layer's append has been issued. CS_ESTATE if the plan is not set or already committed, or if a
+ *                      sequence's ctx_len has changed since.
+ * Calls on a plan read its device buffers: issue them on the stream of its cs_plan_set, or order the streams yourself, and one
+ * at a time (cs_attention_4bit keeps partial results in the plan). They may be captured into a CUDA graph once the page table
+ * is on the device (cs_plan_set uploads it; CS_ESTATE if cs_kv_set_seq came after it): a replay does the plan's work as it
+ * stood at the capture, so set the plan anew only to capture anew. Two graphs that may run at the same time need two plans.
+ *
+ * Types (dtype): CS_F16 or CS_BF16, of every row argument of the call. Rows hold [heads, head_dim] contiguously; strides count
+ * elements between rows, are multiples of 8 and at least a row's length; pointers are 16-byte aligned.
+ * Errors: CS_EINVAL for arguments, before any launch; CS_ESTATE; CS_ECUDA.
+ */
+#define CS_F16 0
+#define CS_BF16 1
+typedef struct cs_plan cs_plan;
+int cs_plan_create(cs_kv* kv, int max_steps, int max_tokens, cs_plan** out);
+int cs_plan_set(cs_plan* plan, const int32_t* seq_ids, const int32_t* lens, int B, int given, void* stream);
+int cs_plan_free(cs_plan* plan);
+int cs_kv_commit(cs_plan* plan);
+/*
+ * cs_kv_append - write the plan's tokens into one layer of the cache, any format, turning keys (and queries) on the way.
+ *   k, v               device rows [T, n_kv_heads, head_dim] of the plan's tokens in step order.
+ *   rotate != 0        pairs (j, j + head_dim/2) of every K head turn by the token's position, in fp32; the result is stored
+ *                      without an intermediate rounding. rotate == 0: K is stored as it is (already rotated).
+ *   q, q_out           device rows [T, n_q_heads, head_dim] or both NULL: the queries, turned and rounded to `dtype`. Only with
+ *                      rotate != 0. q_out may be q itself.
+ * Stored: 16-bit: the nearest bf16 value in the fp16 encoding; 8-bit: the nearest value of the format, ties to even; 4-bit: as at
+ * cs_kv_alloc_4bit. NaN is stored as 0 and magnitudes saturate at the format's largest (65504, 448, 57344), so that no row can
+ * spoil another sequence that meets it behind its own end. Slots of other tokens keep their bytes.
+ * CS_EINVAL where the plan's sequences lack pages for the tokens, or where two steps would write one page (a sequence listed
+ * twice, or sequences that share the page).
+ */
+int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                 const uint16_t* q, int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int rotate, int dtype,
+                 void* stream);
+/*
+ * cs_attention_4bit - attention of the plan's tokens over one layer of a 4-bit cache (CS_EINVAL for another format):
+ *     out[t, h] = sum_j softmax_j(scale * q[t, h] . k_j) v_j,   kv head h / (n_q_heads / n_kv_heads),
+ * over the ctx_len cached keys of the token's sequence and the step's own keys up to the token itself.
+ *   q                  device rows [T, n_q_heads, head_dim], already turned.
+ *   k_new, v_new       device rows [T, n_kv_heads, head_dim] of the new tokens (keys turned), for a plan with given = 1; NULL
+ *                      for given = 0, where they are read from the cache.
+ *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
+ *   scale              0: 1 / sqrt(head_dim); else > 0 and finite.
+ * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; queries up to 2047 in magnitude),
+ * sums and the softmax are fp32, probabilities and dequantised values are rounded to fp16 once. Any number of new tokens; it is
+ * made for up to 32 query rows per kv head (longer steps read the cache once per 32 rows). Deterministic.
+ */
+int cs_attention_4bit(cs_plan* plan, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new,
+                      const uint16_t* v_new, int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype, float scale,
+                      void* stream);
+/*
+ * cs_kv_read - rows of one layer of a cache, any format, as the values that they stand for.
+ *   tok_seq, tok_pos   DEVICE int32[T]: sequence and position of each row. A place outside the page table gives a row of
+ *                      zeros, and the next cs_last_status of the model returns CS_ERANGE. Positions that were never written
+ *                      hold zeros or what the page's last user left.
+ *   out_k, out_v       device [T, n_kv_heads, head_dim] in `dtype`, contiguous (rounded once from fp32).
+ */
+int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_pos, int T, uint16_t* out_k,
+               uint16_t* out_v, int dtype, void* stream);
 
 /*
  * cs_prefill — run tokens through the model and APPEND their K/V to the sequences' pages

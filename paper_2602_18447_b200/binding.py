@@ -16,7 +16,8 @@ CS_OK, CS_EINVAL, CS_ENOMEM, CS_ECUDA, CS_ETIMEOUT, CS_ESTATE, CS_ELIMIT, CS_ERA
 EXPORTED = [
     "cs_version", "cs_strerror", "cs_last_cuda_error", "cs_model_load", "cs_model_free", "cs_model_set_lm_head_rows",
     "cs_reserve",
-    "cs_kv_alloc", "cs_kv_alloc_8bit", "cs_kv_free", "cs_kv_pool_bytes", "cs_kv_set_seq", "cs_kv_fill", "cs_prefill",
+    "cs_kv_alloc", "cs_kv_alloc_8bit", "cs_kv_alloc_4bit", "cs_plan_create", "cs_plan_set", "cs_plan_free", "cs_kv_commit",
+    "cs_kv_append", "cs_attention_4bit", "cs_kv_read", "cs_kv_free", "cs_kv_pool_bytes", "cs_kv_set_seq", "cs_kv_fill", "cs_prefill",
     "cs_verify_steps", "cs_verify_cascade", "cs_append_accepted", "cs_escalate_mask", "cs_cascade_select", "cs_set_keep_logits", "cs_set_deterministic", "cs_get_last_logits", "cs_get_last_lse",
     "cs_last_status", "cs_selftest_wait_timeout", "cs_debug_build", "cs_selftest_range_check", "cs_check_workspace", "cs_gemm_f16", "cs_rmsnorm", "cs_lm_head_gate", "cs_lm_head_gate_static", "cs_take_launch_count", "cs_last_h2d_bytes", "cs_profile", "cs_profile_read",
 ]
@@ -59,7 +60,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         raise FileNotFoundError(
             f"{path} not found: build it with `python -m paper_2602_18447_b200.build` (there is no CPU fallback)")
     lib = C.CDLL(path)
-    vp, i32, f32 = C.c_void_p, C.c_int, C.c_float
+    vp, i32, i64, f32 = C.c_void_p, C.c_int, C.c_int64, C.c_float
     sig = {
         "cs_version": (C.c_int, []),
         "cs_strerror": (C.c_char_p, [i32]),
@@ -70,6 +71,14 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "cs_reserve": (C.c_int, [vp, i32, i32]),
         "cs_kv_alloc": (C.c_int, [vp, i32, i32, i32, i32, vp, C.POINTER(vp)]),
         "cs_kv_alloc_8bit": (C.c_int, [vp, i32, i32, i32, i32, i32, C.POINTER(vp)]),
+        "cs_kv_alloc_4bit": (C.c_int, [vp, i32, i32, i32, i32, C.POINTER(vp)]),
+        "cs_plan_create": (C.c_int, [vp, i32, i32, C.POINTER(vp)]),
+        "cs_plan_set": (C.c_int, [vp, vp, vp, i32, i32, vp]),
+        "cs_plan_free": (C.c_int, [vp]),
+        "cs_kv_commit": (C.c_int, [vp]),
+        "cs_kv_append": (C.c_int, [vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, i32, i32, vp]),
+        "cs_attention_4bit": (C.c_int, [vp, i32, vp, i64, vp, vp, i64, vp, i64, i32, f32, vp]),
+        "cs_kv_read": (C.c_int, [vp, i32, vp, vp, i32, vp, vp, i32, vp]),
         "cs_kv_free": (C.c_int, [vp]),
         "cs_kv_pool_bytes": (C.c_uint64, [vp, i32, i32]),
         "cs_kv_set_seq": (C.c_int, [vp, i32, vp, i32, i32]),
@@ -225,6 +234,93 @@ def cs_kv_alloc_8bit(model: int, num_pages: int, page_size: int, max_seqs: int, 
     _check(load_library().cs_kv_alloc_8bit(model, num_pages, page_size, max_seqs, max_pages_per_seq, code,
                                            C.byref(out)), "cs_kv_alloc_8bit")
     return out.value
+
+
+def cs_kv_alloc_4bit(model: int, num_pages: int, page_size: int, max_seqs: int, max_pages_per_seq: int) -> int:
+    out = C.c_void_p()
+    _check(load_library().cs_kv_alloc_4bit(model, num_pages, page_size, max_seqs, max_pages_per_seq, C.byref(out)),
+           "cs_kv_alloc_4bit")
+    return out.value
+
+
+CS_F16, CS_BF16 = 0, 1
+
+
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError(f"expected float16 or bfloat16 rows, got {t.dtype}")
+    return CS_F16 if t.dtype == torch.float16 else CS_BF16
+
+
+def _rows(t, like=None):
+    """(device address, elements between rows) of a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim] whose rows are
+    contiguous; the rows themselves may lie apart (a slice of a fused projection). `like`: a tensor whose type and row count
+    it has to have."""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or t.dim() not in (2, 3):
+        raise ValueError("expected a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim]")
+    row = t.shape[1] * (t.shape[2] if t.dim() == 3 else 1)
+    inner = t.shape[0] == 0 or (t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2]))
+    if not inner:
+        raise ValueError("the heads of a row have to be contiguous")
+    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.device != like.device):
+        raise ValueError("the rows of one call have one type, one device and one count")
+    return t.data_ptr(), max(row, t.stride(0)) if t.shape[0] <= 1 else t.stride(0)
+
+
+def cs_plan_create(kv: int, max_steps: int = 0, max_tokens: int = 0) -> int:
+    out = C.c_void_p()
+    _check(load_library().cs_plan_create(kv, max_steps, max_tokens, C.byref(out)), "cs_plan_create")
+    return out.value
+
+
+def cs_plan_set(plan: int, seq_ids, lens, given: bool = False, stream=None) -> None:
+    s, l = _i32(seq_ids), _i32(lens)
+    if s.shape != l.shape:
+        raise ValueError("seq_ids and lens have one entry per step")
+    _check(load_library().cs_plan_set(plan, _np_ptr(s), _np_ptr(l), int(s.shape[0]), 1 if given else 0, _stream_ptr(stream)),
+           "cs_plan_set")
+
+
+def cs_plan_free(plan: int) -> None:
+    _check(load_library().cs_plan_free(plan), "cs_plan_free")
+
+
+def cs_kv_commit(plan: int) -> None:
+    _check(load_library().cs_kv_commit(plan), "cs_kv_commit")
+
+
+def cs_kv_append(plan: int, layer: int, k, v, q=None, q_out=None, rotate: bool = True, stream=None) -> None:
+    """k, v: CUDA rows [T, n_kv_heads, head_dim] (float16 or bfloat16); q, q_out: [T, n_q_heads, head_dim] or None, of the
+    same type. T, the heads and head_dim are those of the plan and its cache."""
+    (kp, ks), (vp, vs) = _rows(k), _rows(v, k)
+    (qp, qs), (op, os_) = _rows(q, k), _rows(q_out, k)
+    _check(load_library().cs_kv_append(plan, layer, kp, ks, vp, vs, qp, qs, op, os_, 1 if rotate else 0, _dtype_code(k),
+                                       _stream_ptr(stream)), "cs_kv_append")
+
+
+def cs_attention_4bit(plan: int, layer: int, q, out, k_new=None, v_new=None, scale: float = 0.0, stream=None) -> None:
+    """q, out: CUDA rows [T, n_q_heads, head_dim]; k_new, v_new: [T, n_kv_heads, head_dim] of a plan with given=True, with one
+    row stride; all of one type (float16 or bfloat16)."""
+    (qp, qs), (op, os_) = _rows(q), _rows(out, q)
+    (kp, ks), (vp, vs) = _rows(k_new, q), _rows(v_new, q)
+    if ks != vs:
+        raise ValueError("k_new and v_new have one row stride")
+    _check(load_library().cs_attention_4bit(plan, layer, qp, qs, kp, vp, ks, op, os_, _dtype_code(q), float(scale),
+                                            _stream_ptr(stream)), "cs_attention_4bit")
+
+
+def cs_kv_read(kv: int, layer: int, tok_seq, tok_pos, out_k, out_v, stream=None) -> None:
+    """tok_seq, tok_pos: CUDA int32 tensors [T]; out_k, out_v: contiguous CUDA tensors [T, n_kv_heads, head_dim] of one type."""
+    import torch
+    if tok_seq.dtype != torch.int32 or tok_pos.dtype != torch.int32 or tok_seq.shape != tok_pos.shape:
+        raise ValueError("tok_seq and tok_pos are int32 tensors of one length")
+    if out_k.dtype != out_v.dtype or out_k.shape != out_v.shape or out_k.shape[0] != tok_seq.shape[0]:
+        raise ValueError("out_k and out_v have one type, one shape and a row per place")
+    _check(load_library().cs_kv_read(kv, layer, _dev_ptr(tok_seq), _dev_ptr(tok_pos), int(tok_seq.shape[0]), _dev_ptr(out_k),
+                                     _dev_ptr(out_v), _dtype_code(out_k), _stream_ptr(stream)), "cs_kv_read")
 
 
 def cs_kv_free(kv: int) -> None:

@@ -9,8 +9,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_PATH = os.path.join(_HERE, "libconfspec.so")
 DEBUG_LIB_PATH = os.path.join(_HERE, "libconfspec_debug.so")      # the same sources with -DCS_DEBUG (device-side range checks)
-SOURCES = ["api.cu", "gemm_tcgen05.cu", "attention.cu", "attention_short.cu", "lmhead.cu", "elementwise.cu"]
-HEADERS = ["common.cuh", "gemm.h", "kernels.h", os.path.join("..", "..", "include", "confspec.h")]
+SOURCES = ["api.cu", "gemm_tcgen05.cu", "attention.cu", "attention_short.cu", "attention_4bit.cu", "kv_rows.cu", "lmhead.cu", "elementwise.cu"]
+HEADERS = ["common.cuh", "gemm.h", "kernels.h", "kv4.cuh", os.path.join("..", "..", "include", "confspec.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared"]
 

@@ -11,6 +11,7 @@
 
 #include "gemm.h"
 #include "kernels.h"
+#include "kv4.cuh"
 
 using namespace cs;
 
@@ -136,7 +137,9 @@ struct cs_kv {
   int num_pages, page_size, max_seqs, max_pages_per_seq;
   uint16_t* pool = nullptr;   // 16-bit cells (bf16 values in the fp16 encoding), or 8-bit codes when format == 1
   bool own_pool = false;
-  int format = 0;             // 0: 16-bit cells; CS_KV_E4M3 / CS_KV_E5M2: 8-bit codes (read-only for the pass)
+  // CS_KV_FMT_*: 16-bit cells, 8-bit codes (CS_KV_E4M3 / CS_KV_E5M2; read-only for the pass), or 4-bit blocks (kv4.cuh:
+  // [layer][page][kv head], K and V together)
+  int format = 0;
   size_t plane_elems;  // elements of one (layer, K or V) plane
   CUtensorMap tm_pool;
   int32_t* table_host = nullptr;  // pinned [max_seqs, max_pages_per_seq]
@@ -146,6 +149,24 @@ struct cs_kv {
   cudaEvent_t upload_ev = nullptr;
   bool upload_pending = false;
   DevBuf fill_tmp;
+  DevBuf expanded;            // 4-bit cache: one layer's pages in the 16-bit layout, for steps of many tokens
+  CUtensorMap tm_expanded;
+  void* tm_expanded_of = nullptr;
+  size_t layer4_bytes() const {
+    return static_cast<size_t>(num_pages) * model->d.n_kv_heads * kv4_block_bytes(model->d.head_dim);
+  }
+};
+
+// A batch of steps over one cache, staged on the device once for all layers.
+struct cs_plan {
+  cs_kv* kv;
+  int device = 0;
+  bool set = false, given = false, appendable = false, committed = false, any_split = false;
+  int B = 0, T = 0, n_blocks = 0, n_items = 0, row_tile = 8;
+  size_t off_pos = 0, off_blocks = 0, off_items = 0;      // int32 offsets into the staged block
+  std::vector<int32_t> seqs, lens, ctx;
+  Staging stg;
+  DevBuf rope, part_o, part_ml;
 };
 
 namespace {
@@ -196,7 +217,12 @@ int ensure_readback(cs_model* m, size_t ints) {
 struct BatchLayout {
   int B = 0, T = 0;
   size_t off_cu, off_pos, off_tseq, off_tok, off_items, total;
+  size_t off_blocks = 0, off_pages = 0;
   int n_items = 0, n_slots = 0;
+  int n_blocks = 0;        // 4-bit cache: page-wise blocks of the new tokens (appending passes)
+  int n_pages = 0;         // 4-bit cache, expand: pages to expand
+  bool expand = false;     // 4-bit cache: the tensor-core attention runs over expanded pages (else the 4-bit kernel)
+  int row_tile = 8;        // 4-bit cache: query rows per work item of the 4-bit kernel
   int max_rows = 0;        // 8-bit cache: the largest number of query rows (new tokens x heads per kv head) of a step
   bool any_split = false;  // 8-bit cache: some context is cut into pieces
 };
@@ -211,6 +237,15 @@ constexpr double kAttnItemFixed = 3.5;
 constexpr double kAttnPieceExtra = 2.0;
 constexpr double kAttnMergeFixed = 1.0;
 constexpr double kAttnMergePerSplit = 0.5;
+
+// 4-bit attention: pieces of a context hold at least this many pages, there are about this many of them per SM, and a
+// step's range is cut into at most this many.
+constexpr long kAttn4MinPages = 16;
+constexpr long kAttn4PiecesPerSm = 6;
+constexpr long kAttn4MaxPieces = 64;
+// Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves; longer
+// ones have them expanded to fp16 for the tensor-core kernel.
+constexpr int kAttn4MaxRows = 32;
 
 // Time at which the last SM finishes when the items, sorted by decreasing cost, are handed to whichever of
 // `machines` SMs is free first (what the hardware does with one CTA per SM and the grid in that order).
@@ -336,6 +371,58 @@ void build_short_work(const cs_model* m, int B, const int32_t* lens, const int32
   *n_slots = slots;
 }
 
+// Work items of the 4-bit attention: one per (step, kv head, tile of `row_tile` query rows, piece of the pages). Pages are
+// the cached ones and, when the new tokens' keys are given as rows (`given`), the pages of 16 of those behind them.
+void build_4bit_work(const cs_model* m, int B, const int32_t* lens, const int32_t* ctx, bool given, int row_tile,
+                     std::vector<AttnItem>& items, int* n_slots, bool* any_split) {
+  const int heads = m->d.n_kv_heads, G = m->d.n_q_heads / heads;
+  struct Unit { int step, row0, cached, pages; };
+  std::vector<Unit> units;
+  long total = 0;
+  for (int i = 0; i < B; ++i)
+    for (int r = 0; r < lens[i] * G; r += row_tile) {
+      const int t_last = std::min(lens[i] - 1, (r + row_tile - 1) / G);
+      const int cached = given ? (ctx[i] + kPageSize - 1) / kPageSize : (ctx[i] + t_last) / kPageSize + 1;
+      const int pages = cached + (given ? t_last / kPageSize + 1 : 0);
+      units.push_back(Unit{i, r, cached, pages});
+      total += static_cast<long>(pages) * heads;
+    }
+  const long chunk = std::max<long>(kAttn4MinPages, total / (kNumSMs * kAttn4PiecesPerSm) + 1);
+  items.clear();
+  int slots = 0;
+  *any_split = false;
+  for (const Unit& u : units) {
+    const int n = static_cast<int>(std::min<long>(kAttn4MaxPieces, std::max<long>(1, (u.pages + chunk - 1) / chunk)));
+    for (int h = 0; h < heads; ++h) {
+      for (int s = 0; s < n; ++s) {
+        const int b = static_cast<int>(static_cast<long>(u.pages) * s / n);
+        const int e = static_cast<int>(static_cast<long>(u.pages) * (s + 1) / n);
+        items.push_back(AttnItem{u.step, h, u.row0, b, e, n > 1 ? slots + s : 0, n > 1 ? slots : 0, n, 0, lens[u.step],
+                                 ctx[u.step], 0, {0, u.cached, 0, 0}});
+      }
+      if (n > 1) { slots += n; *any_split = true; }
+    }
+  }
+  std::stable_sort(items.begin(), items.end(), [](const AttnItem& a, const AttnItem& b) {
+    return (a.tile_end - a.tile_begin) > (b.tile_end - b.tile_begin);
+  });
+  *n_slots = slots;
+}
+
+// The new tokens of every step, cut at page borders.
+void build_append_blocks(int B, const int32_t* seqs, const int32_t* lens, const int32_t* ctx, std::vector<KvBlock>& blocks) {
+  blocks.clear();
+  int tok = 0;
+  for (int i = 0; i < B; ++i)
+    for (int p = 0; p < lens[i];) {
+      const int pos = ctx[i] + p;
+      const int n = std::min(lens[i] - p, kPageSize - pos % kPageSize);
+      blocks.push_back(KvBlock{tok, n, seqs[i], pos});
+      tok += n;
+      p += n;
+    }
+}
+
 int check_model_desc(const cs_model_desc* d) {
   if (!d) return CS_EINVAL;
   if (d->n_layers < 1 || d->d_model < 8 || d->n_q_heads < 1 || d->n_kv_heads < 1 || d->d_ffn < 8 || d->vocab < 1)
@@ -450,16 +537,69 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
     CS_STEP(kProfQkv, gemm_f16_rope(tm_a, lw.tm_wqkv, qkv, T, m->n_qkv, d.d_model, rope_epi, m->status, s));
     ap.k_group_base = (2 * l) * plane_groups;
     ap.v_group_base = (2 * l + 1) * plane_groups;
+    const auto append = [&]() -> cudaError_t {
+      if (append_kv->format == CS_KV_FMT_INT4) {
+        KvAppendParams q4 = {};
+        q4.k = qkv + m->q_dim;
+        q4.v = qkv + m->q_dim + m->kv_dim;
+        q4.k_stride = q4.v_stride = m->n_qkv;
+        q4.blocks = reinterpret_cast<const KvBlock*>(dev_meta + L.off_blocks);
+        q4.table = append_kv->table_dev;
+        q4.pool_k = reinterpret_cast<uint8_t*>(append_kv->pool) + static_cast<size_t>(l) * append_kv->layer4_bytes();
+        q4.max_pages_per_seq = append_kv->max_pages_per_seq;
+        q4.num_pages = append_kv->num_pages;
+        q4.n_q_heads = d.n_q_heads;
+        q4.n_kv_heads = d.n_kv_heads;
+        q4.status = m->status;
+        return launch_kv_append(q4, CS_KV_FMT_INT4, d.head_dim, L.n_blocks, s);
+      }
+      return launch_kv_scatter(qkv + m->q_dim, qkv + m->q_dim + m->kv_dim, m->n_qkv, d_tseq, d_pos, 0, 0,
+                               append_kv->table_dev, append_kv->max_pages_per_seq,
+                               append_kv->pool + static_cast<size_t>(2 * l) * append_kv->plane_elems,
+                               append_kv->pool + static_cast<size_t>(2 * l + 1) * append_kv->plane_elems,
+                               d.n_kv_heads, d.head_dim, kPageSize, T, 1, append_kv->num_pages, m->status, s);
+    };
     if (l == d.n_layers - 1 && append_kv) {
       // A pass that only appends to the cache has no use for what follows the last layer's K/V projection.
-      CS_STEP(kProfOther, launch_kv_scatter(qkv + m->q_dim, qkv + m->q_dim + m->kv_dim, m->n_qkv, d_tseq, d_pos, 0, 0,
-                                append_kv->table_dev, append_kv->max_pages_per_seq,
-                                append_kv->pool + static_cast<size_t>(2 * l) * append_kv->plane_elems,
-                                append_kv->pool + static_cast<size_t>(2 * l + 1) * append_kv->plane_elems,
-                                d.n_kv_heads, d.head_dim, kPageSize, T, 1, append_kv->num_pages, m->status, s));
+      CS_STEP(kProfOther, append());
       break;
     }
-    if (kv->format != 0) {
+    if (kv->format == CS_KV_FMT_INT4) {
+      const uint8_t* layer4 = reinterpret_cast<const uint8_t*>(kv->pool) + static_cast<size_t>(l) * kv->layer4_bytes();
+      if (L.expand) {
+        // many query rows: the pages once more as fp16, and the tensor-core kernel over those
+        uint16_t* kx = static_cast<uint16_t*>(kv->expanded.p);
+        uint16_t* vx = kx + kv->plane_elems;
+        CS_STEP(kProfOther, launch_kv_expand(layer4, dev_meta + L.off_pages, L.n_pages, kx, vx, d.n_kv_heads, d.head_dim,
+                                             kv->num_pages, m->status, s));
+        ap.k_group_base = 0;
+        ap.v_group_base = plane_groups;
+        ap.pages_just_written = 1;
+        CS_STEP(kProfAttn, launch_attention(ap, kv->tm_expanded, tm_qkv_attn, tm_q3d, d_items, L.n_items, s));
+      } else {
+        Attn4Params a4 = {};
+        a4.q = qkv;
+        a4.k_new = qkv + m->q_dim;
+        a4.v_new = qkv + m->q_dim + m->kv_dim;
+        a4.out = attn_o;
+        a4.q_stride = a4.kv_stride = m->n_qkv;
+        a4.out_stride = m->q_dim;
+        a4.page_table = kv->table_dev;
+        a4.pool = layer4;
+        a4.max_pages_per_seq = kv->max_pages_per_seq;
+        a4.num_pages = kv->num_pages;
+        a4.n_q_heads = d.n_q_heads;
+        a4.n_kv_heads = d.n_kv_heads;
+        a4.head_dim = d.head_dim;
+        a4.given = 1;
+        a4.cache_is_settled = 1;      // this layer's pages were written by an earlier call, and an upload stands in between
+        a4.scale_log2e = ap.scale_log2e;
+        a4.part_o = ap.part_o;
+        a4.part_ml = ap.part_ml;
+        a4.status = m->status;
+        CS_STEP(kProfAttn, launch_attention_4bit(a4, d_items, L.n_items, L.row_tile, L.any_split, s));
+      }
+    } else if (kv->format != 0) {
       const uint8_t* pool8 = reinterpret_cast<const uint8_t*>(kv->pool);
       CS_STEP(kProfAttn, launch_attention_short(ap, pool8 + static_cast<size_t>(2 * l) * kv->plane_elems,
                                                 pool8 + static_cast<size_t>(2 * l + 1) * kv->plane_elems, d_items,
@@ -467,13 +607,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
     } else {
       CS_STEP(kProfAttn, launch_attention(ap, kv->tm_pool, tm_qkv_attn, tm_q3d, d_items, L.n_items, s));
     }
-    if (append_kv) {
-      CS_STEP(kProfOther, launch_kv_scatter(qkv + m->q_dim, qkv + m->q_dim + m->kv_dim, m->n_qkv, d_tseq, d_pos, 0, 0,
-                                append_kv->table_dev, append_kv->max_pages_per_seq,
-                                append_kv->pool + static_cast<size_t>(2 * l) * append_kv->plane_elems,
-                                append_kv->pool + static_cast<size_t>(2 * l + 1) * append_kv->plane_elems,
-                                d.n_kv_heads, d.head_dim, kPageSize, T, 1, append_kv->num_pages, m->status, s));
-    }
+    if (append_kv) CS_STEP(kProfOther, append());
     CS_STEP(kProfO, gemm_f16(tm_o, lw.tm_wo, nullptr, x, T, d.d_model, m->q_dim, kEpiResidAdd, m->status, s, turn));
     if (l == d.n_layers - 1 && !append_kv) {
       // Only each step's last position feeds the LM head, and after the last attention no row depends on another:
@@ -522,9 +656,25 @@ int ensure_workspace(cs_model* m, int B, int T) {
   return CS_OK;
 }
 
+// Scratch pages of the 4-bit cache for the tensor-core attention: one layer's pool in the 16-bit layout (zero where nothing
+// has been expanded yet: slots behind a context are multiplied by zero probabilities) and its tensor map.
+int ensure_expanded(cs_kv* kv) {
+  int rc;
+  if ((rc = kv->expanded.ensure(2 * kv->plane_elems * 2, true))) return rc;
+  if (kv->tm_expanded_of != kv->expanded.p) {
+    const uint64_t rows = 2ull * kv->num_pages * kv->model->d.n_kv_heads * kPageSize;
+    if (!make_kv_group_map(&kv->tm_expanded, kv->expanded.p, rows, kv->model->d.head_dim, kPageSize / 8)) {
+      g_cuda_error = "cuTensorMapEncodeTiled failed for the expanded kv pages";
+      return CS_ECUDA;
+    }
+    kv->tm_expanded_of = kv->expanded.p;
+  }
+  return CS_OK;
+}
+
 // Checks a batch, writes its metadata into a staging slot and enqueues the upload.
-int stage_batch(cs_model* m, const cs_kv* kv, const int32_t* seq_ids, int B, const int32_t* tokens,
-                int tokens_on_device, const int32_t* lens, BatchLayout* out, const int32_t** dev_meta,
+int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int32_t* tokens,
+                int tokens_on_device, const int32_t* lens, bool appends, BatchLayout* out, const int32_t** dev_meta,
                 const int32_t** dev_tokens, cudaStream_t s) {
   long T = 0;
   for (int i = 0; i < B; ++i) {
@@ -543,7 +693,27 @@ int stage_batch(cs_model* m, const cs_kv* kv, const int32_t* seq_ids, int B, con
   std::vector<AttnItem> items;
   int n_slots = 0, max_rows = 0;
   bool any_split = false;
-  if (kv->format != 0) {
+  std::vector<KvBlock> blocks;
+  std::vector<int32_t> pages;
+  int row_tile = 8;
+  if (kv->format == CS_KV_FMT_INT4) {
+    const int G = m->d.n_q_heads / m->d.n_kv_heads;
+    for (int i = 0; i < B; ++i) max_rows = std::max(max_rows, lens[i] * G);
+    if (appends) build_append_blocks(B, seq_ids, lens, ctx.data(), blocks);
+    if (max_rows > kAttn4MaxRows) {
+      build_attention_work(m, B, lens, ctx.data(), items, &n_slots);
+      std::vector<char> seen(kv->max_seqs, 0);        // candidates that share a sequence share its pages
+      for (int i = 0; i < B; ++i) {
+        if (seen[seq_ids[i]]) continue;
+        seen[seq_ids[i]] = 1;
+        const int32_t* row = kv->table_host + static_cast<size_t>(seq_ids[i]) * kv->max_pages_per_seq;
+        pages.insert(pages.end(), row, row + (ctx[i] + kPageSize - 1) / kPageSize);
+      }
+    } else {
+      row_tile = attention_4bit_row_tile(max_rows);
+      build_4bit_work(m, B, lens, ctx.data(), true, row_tile, items, &n_slots, &any_split);
+    }
+  } else if (kv->format != 0) {
     const int G = m->d.n_q_heads / m->d.n_kv_heads;
     for (int i = 0; i < B; ++i) max_rows = std::max(max_rows, lens[i] * G);
     if (max_rows > 32) return CS_EINVAL;     // the 8-bit cache serves short steps only
@@ -562,8 +732,14 @@ int stage_batch(cs_model* m, const cs_kv* kv, const int32_t* seq_ids, int B, con
   L.off_tseq = take(T);
   L.off_tok = take(tokens_on_device ? 0 : T);
   L.off_items = take(items.size() * (sizeof(AttnItem) / 4));
+  L.off_blocks = take(blocks.size() * (sizeof(KvBlock) / 4));
+  L.off_pages = take(pages.size());
   L.total = o;
   L.n_items = static_cast<int>(items.size());
+  L.n_blocks = static_cast<int>(blocks.size());
+  L.n_pages = static_cast<int>(pages.size());
+  L.row_tile = row_tile;
+  L.expand = kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows;
   L.n_slots = n_slots;
   L.max_rows = max_rows;
   L.any_split = any_split;
@@ -575,6 +751,7 @@ int stage_batch(cs_model* m, const cs_kv* kv, const int32_t* seq_ids, int B, con
   if ((rc = m->attn_part_ml.ensure(static_cast<size_t>(std::max(1, n_slots)) * 128 * 2 * 4))) return rc;
   // One counter per split query tile; every launch leaves them at zero again.
   if ((rc = m->attn_counters.ensure(static_cast<size_t>(std::max(1, n_slots)) * 4, true))) return rc;
+  if (kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows && (rc = ensure_expanded(kv))) return rc;
   if ((rc = m->stg.dev.ensure(L.total * 4))) return rc;
   int slot;
   if ((rc = staging_slot(m->stg, L.total, &slot))) return rc;
@@ -594,6 +771,8 @@ int stage_batch(cs_model* m, const cs_kv* kv, const int32_t* seq_ids, int B, con
     it.seq = seq_ids[it.step];
   }
   if (!items.empty()) std::memcpy(h + L.off_items, items.data(), items.size() * sizeof(AttnItem));
+  if (!blocks.empty()) std::memcpy(h + L.off_blocks, blocks.data(), blocks.size() * sizeof(KvBlock));
+  if (!pages.empty()) std::memcpy(h + L.off_pages, pages.data(), pages.size() * sizeof(int32_t));
   CS_CUDA(cudaMemcpyAsync(m->stg.dev.p, h, L.total * 4, cudaMemcpyHostToDevice, s));
   m->last_h2d_bytes = static_cast<int64_t>(L.total) * 4;
   CS_CUDA(cudaEventRecord(m->stg.ev[slot], s));
@@ -820,6 +999,10 @@ int cs_kv_alloc_8bit(const cs_model* m, int num_pages, int page_size, int max_se
   return kv_alloc_impl(m, num_pages, page_size, max_seqs, max_pages_per_seq, nullptr, format, out);
 }
 
+int cs_kv_alloc_4bit(const cs_model* m, int num_pages, int page_size, int max_seqs, int max_pages_per_seq, cs_kv** out) {
+  return kv_alloc_impl(m, num_pages, page_size, max_seqs, max_pages_per_seq, nullptr, CS_KV_FMT_INT4, out);
+}
+
 static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int max_seqs, int max_pages_per_seq,
                          void* dev_pool, int format, cs_kv** out) {
   if (!out) return CS_EINVAL;
@@ -839,7 +1022,8 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
   kv->plane_elems = static_cast<size_t>(num_pages) * m->d.n_kv_heads * page_size * m->d.head_dim;
   kv->ctx_len.assign(max_seqs, -1);
   kv->n_pages.assign(max_seqs, 0);
-  const uint64_t bytes = cs_kv_pool_bytes(m, num_pages, page_size) / (format != 0 ? 2 : 1);
+  const uint64_t bytes = format == CS_KV_FMT_INT4 ? kv->layer4_bytes() * m->d.n_layers
+                                                  : cs_kv_pool_bytes(m, num_pages, page_size) / (format != 0 ? 2 : 1);
   int rc = CS_OK;
   cudaError_t e;
   if (dev_pool) {
@@ -877,8 +1061,27 @@ int cs_kv_free(cs_kv* kv) {
   if (kv->table_dev) cudaFree(kv->table_dev);
   if (kv->upload_ev) cudaEventDestroy(kv->upload_ev);
   kv->fill_tmp.release();
+  kv->expanded.release();
   delete kv;
   return CS_OK;
+}
+
+// Fills in the cache's side of an append and launches it.
+static cudaError_t launch_rows_append(cs_kv* kv, int layer, KvAppendParams p, const KvBlock* dev_blocks, int n_blocks,
+                                      cudaStream_t s) {
+  const cs_model_desc& d = kv->model->d;
+  uint8_t* pool = reinterpret_cast<uint8_t*>(kv->pool);
+  const size_t plane = kv->plane_elems * (kv->format == CS_KV_FMT_16BIT ? 2 : 1);
+  p.blocks = dev_blocks;
+  p.table = kv->table_dev;
+  p.pool_k = kv->format == CS_KV_FMT_INT4 ? pool + layer * kv->layer4_bytes() : pool + 2 * layer * plane;
+  p.pool_v = kv->format == CS_KV_FMT_INT4 ? nullptr : pool + (2 * layer + 1) * plane;
+  p.max_pages_per_seq = kv->max_pages_per_seq;
+  p.num_pages = kv->num_pages;
+  p.n_q_heads = d.n_q_heads;
+  p.n_kv_heads = d.n_kv_heads;
+  p.status = kv->model->status;
+  return launch_kv_append(p, kv->format, d.head_dim, n_blocks, s);
 }
 
 int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int ctx_len) {
@@ -910,8 +1113,26 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
   const size_t row = static_cast<size_t>(d.n_kv_heads) * d.head_dim;
   const size_t elems = static_cast<size_t>(c) * row;
   int rc;
-  if ((rc = kv->fill_tmp.ensure(2 * elems * 2))) return rc;
+  if ((rc = kv->fill_tmp.ensure(2 * elems * 2 + (c + 2 * kPageSize) / kPageSize * sizeof(KvBlock)))) return rc;
   if ((rc = upload_table(kv, s))) return rc;
+  if (kv->format == CS_KV_FMT_INT4) {   // bf16 rows, quantised on the way in
+    std::vector<KvBlock> blocks;
+    const int32_t zero = 0;
+    build_append_blocks(1, &seq, &c, &zero, blocks);
+    uint16_t* rows = static_cast<uint16_t*>(kv->fill_tmp.p);
+    KvBlock* dev_blocks = reinterpret_cast<KvBlock*>(rows + 2 * elems);
+    CS_CUDA(cudaMemcpyAsync(rows, host_k, elems * 2, cudaMemcpyHostToDevice, s));
+    CS_CUDA(cudaMemcpyAsync(rows + elems, host_v, elems * 2, cudaMemcpyHostToDevice, s));
+    CS_CUDA(cudaMemcpyAsync(dev_blocks, blocks.data(), blocks.size() * sizeof(KvBlock), cudaMemcpyHostToDevice, s));
+    KvAppendParams p = {};
+    p.k = rows;
+    p.v = rows + elems;
+    p.k_stride = p.v_stride = static_cast<int64_t>(row);
+    p.src_bf16 = 1;
+    CS_CUDA(launch_rows_append(kv, layer, p, dev_blocks, static_cast<int>(blocks.size()), s));
+    CS_CUDA(cudaStreamSynchronize(s));
+    return CS_OK;
+  }
   if (kv->format != 0) {   // 8-bit cache: host_k / host_v hold one code per element
     uint8_t* tk8 = static_cast<uint8_t*>(kv->fill_tmp.p);
     uint8_t* tv8 = tk8 + elems;
@@ -937,10 +1158,284 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
   return CS_OK;
 }
 
+// Nothing may be uploaded from inside a stream capture: the page table has to be on the device already.
+static int table_ready(cs_kv* kv, cudaStream_t s) {
+  if (!kv->dirty) return CS_OK;
+  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+  CS_CUDA(cudaStreamIsCapturing(s, &st));
+  if (st != cudaStreamCaptureStatusNone) return CS_ESTATE;
+  return upload_table(kv, s);
+}
+
+static bool rows_ok(const void* p, int64_t stride, int64_t row) {
+  return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride >= row && stride % 8 == 0;
+}
+
+int cs_plan_create(cs_kv* kv, int max_steps, int max_tokens, cs_plan** out) {
+  if (!out) return CS_EINVAL;
+  *out = nullptr;
+  if (!kv || max_steps < 0 || max_tokens < 0 || max_tokens > (1 << 24)) return CS_EINVAL;
+  int dev = 0;
+  CS_CUDA(cudaGetDevice(&dev));
+  cs_plan* p = new (std::nothrow) cs_plan();
+  if (!p) return CS_ENOMEM;
+  p->kv = kv;
+  p->device = dev;
+  const int rc = p->rope.ensure(static_cast<size_t>(std::max(1, max_tokens)) * (kv->model->d.head_dim / 2) * sizeof(float2));
+  if (rc) { cs_plan_free(p); return rc; }
+  *out = p;
+  return CS_OK;
+}
+
+int cs_plan_free(cs_plan* p) {
+  if (!p) return CS_OK;
+  cudaDeviceSynchronize();
+  DevBuf* bufs[] = {&p->stg.dev, &p->rope, &p->part_o, &p->part_ml};
+  for (DevBuf* b : bufs) b->release();
+  for (int i = 0; i < kStagingRing; ++i) {
+    if (p->stg.host[i]) cudaFreeHost(p->stg.host[i]);
+    if (p->stg.ev[i]) cudaEventDestroy(p->stg.ev[i]);
+  }
+  delete p;
+  return CS_OK;
+}
+
+static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int B, int given, void* stream) {
+  if (!p || B < 0 || (B > 0 && (!seq_ids || !lens))) return CS_EINVAL;
+  cs_kv* kv = p->kv;
+  const cs_model* m = kv->model;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int dev = 0;
+  CS_CUDA(cudaGetDevice(&dev));
+  if (dev != p->device) return CS_EINVAL;
+  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+  CS_CUDA(cudaStreamIsCapturing(s, &st));
+  if (st != cudaStreamCaptureStatusNone) return CS_ESTATE;
+  long T = 0;
+  bool room = true;
+  for (int i = 0; i < B; ++i) {
+    if (lens[i] < 1 || seq_ids[i] < 0 || seq_ids[i] >= kv->max_seqs) return CS_EINVAL;
+    if (kv->ctx_len[seq_ids[i]] < 0) return CS_ESTATE;
+    room = room && static_cast<long>(kv->ctx_len[seq_ids[i]]) + lens[i] <= static_cast<long>(kv->n_pages[seq_ids[i]]) * kPageSize;
+    T += lens[i];
+    if (T * (m->d.n_q_heads / m->d.n_kv_heads) > (1 << 24)) return CS_EINVAL;
+  }
+  if (!given && !room) return CS_EINVAL;      // the new tokens' keys are to be in the cache: it needs pages for them
+  const int G = m->d.n_q_heads / m->d.n_kv_heads;
+  std::vector<int32_t> ctx(B);
+  int max_rows = 0;
+  for (int i = 0; i < B; ++i) {
+    ctx[i] = kv->ctx_len[seq_ids[i]];
+    max_rows = std::max(max_rows, lens[i] * G);
+  }
+  // appending writes every page's slots once: no two steps on one sequence, or on sequences that share a page they write
+  bool distinct = true;
+  std::vector<KvBlock> blocks;
+  if (room) {
+    build_append_blocks(B, seq_ids, lens, ctx.data(), blocks);
+    std::vector<int32_t> written;
+    written.reserve(blocks.size());
+    for (const KvBlock& b : blocks)
+      written.push_back(kv->table_host[static_cast<size_t>(b.seq) * kv->max_pages_per_seq + b.pos0 / kPageSize]);
+    std::sort(written.begin(), written.end());
+    distinct = std::adjacent_find(written.begin(), written.end()) == written.end();
+  }
+  std::vector<AttnItem> items;
+  int n_slots = 0;
+  bool any_split = false;
+  const int row_tile = attention_4bit_row_tile(max_rows);
+  if (kv->format == CS_KV_FMT_INT4 && B > 0)
+    build_4bit_work(m, B, lens, ctx.data(), given != 0, row_tile, items, &n_slots, &any_split);
+  size_t o = 0;
+  auto take = [&o](size_t n) { size_t r = o; o += (n + 3) & ~size_t(3); return r; };
+  const size_t off_pos = take(T);
+  const size_t off_blocks = take(blocks.size() * (sizeof(KvBlock) / 4));
+  const size_t off_items = take(items.size() * (sizeof(AttnItem) / 4));
+  int rc;
+  p->set = false;
+  const int hd = m->d.head_dim;
+  if ((rc = p->rope.ensure(static_cast<size_t>(std::max(1L, T)) * (hd / 2) * sizeof(float2)))) return rc;
+  if ((rc = p->part_o.ensure(static_cast<size_t>(n_slots) * 32 * hd * 4))) return rc;
+  if ((rc = p->part_ml.ensure(static_cast<size_t>(n_slots) * 32 * 2 * 4))) return rc;
+  if ((rc = p->stg.dev.ensure(o * 4))) return rc;
+  if (o > 0) {
+    int slot;
+    if ((rc = staging_slot(p->stg, o, &slot))) return rc;
+    int32_t* h = p->stg.host[slot];
+    std::vector<int32_t> first(B);
+    for (int i = 0, t = 0; i < B; ++i) {
+      first[i] = t;
+      for (int j = 0; j < lens[i]; ++j) h[off_pos + t + j] = ctx[i] + j;
+      t += lens[i];
+    }
+    for (AttnItem& it : items) {
+      it.tok0 = first[it.step];
+      it.seq = seq_ids[it.step];
+    }
+    if (!blocks.empty()) std::memcpy(h + off_blocks, blocks.data(), blocks.size() * sizeof(KvBlock));
+    if (!items.empty()) std::memcpy(h + off_items, items.data(), items.size() * sizeof(AttnItem));
+    CS_CUDA(cudaMemcpyAsync(p->stg.dev.p, h, o * 4, cudaMemcpyHostToDevice, s));
+    CS_CUDA(cudaEventRecord(p->stg.ev[slot], s));
+    p->stg.pending[slot] = true;
+    CS_CUDA(launch_rope_table(static_cast<const int32_t*>(p->stg.dev.p) + off_pos, m->inv_freq,
+                              static_cast<float2*>(p->rope.p), static_cast<int>(T), hd / 2, s));
+  }
+  if ((rc = upload_table(kv, s))) return rc;
+  p->B = B;
+  p->T = static_cast<int>(T);
+  p->given = given != 0;
+  p->appendable = room && distinct;
+  p->committed = false;
+  p->any_split = any_split;
+  p->row_tile = row_tile;
+  p->n_blocks = static_cast<int>(blocks.size());
+  p->n_items = static_cast<int>(items.size());
+  p->off_pos = off_pos;
+  p->off_blocks = off_blocks;
+  p->off_items = off_items;
+  p->seqs.assign(seq_ids, seq_ids + B);
+  p->lens.assign(lens, lens + B);
+  p->ctx = ctx;
+  p->set = true;
+  return CS_OK;
+}
+
+int cs_plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int B, int given, void* stream) {
+  try {
+    return plan_set(p, seq_ids, lens, B, given, stream);
+  } catch (const std::bad_alloc&) {      // host memory for the work lists
+    return CS_ENOMEM;
+  }
+}
+
+// What every call on a plan checks: set, the right device, a layer of the model, a known type.
+static int plan_ready(const cs_plan* p, int layer, int dtype) {
+  if (!p || layer < 0 || layer >= p->kv->model->d.n_layers || (dtype != CS_F16 && dtype != CS_BF16)) return CS_EINVAL;
+  int dev = 0;
+  CS_CUDA(cudaGetDevice(&dev));
+  if (dev != p->device) return CS_EINVAL;
+  return p->set ? CS_OK : CS_ESTATE;
+}
+
+int cs_kv_append(cs_plan* p, int layer, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
+                 const uint16_t* q, int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int rotate, int dtype,
+                 void* stream) {
+  int rc;
+  if ((rc = plan_ready(p, layer, dtype))) return rc;
+  const cs_model_desc& d = p->kv->model->d;
+  if (!p->appendable || (q == nullptr) != (q_out == nullptr) || (q && !rotate)) return CS_EINVAL;
+  if (p->T == 0) return CS_OK;
+  const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
+  if (!rows_ok(k, k_stride, kv_row) || !rows_ok(v, v_stride, kv_row)) return CS_EINVAL;
+  if (q && (!rows_ok(q, q_stride, q_row) || !rows_ok(q_out, q_out_stride, q_row))) return CS_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((rc = table_ready(p->kv, s))) return rc;
+  KvAppendParams a = {};
+  a.k = k;
+  a.v = v;
+  a.q = q;
+  a.q_out = q_out;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.rope = rotate ? static_cast<const float2*>(p->rope.p) : nullptr;
+  a.src_bf16 = dtype == CS_BF16;
+  const KvBlock* blocks = reinterpret_cast<const KvBlock*>(static_cast<const int32_t*>(p->stg.dev.p) + p->off_blocks);
+  CS_CUDA(launch_rows_append(p->kv, layer, a, blocks, p->n_blocks, s));
+  return CS_OK;
+}
+
+int cs_kv_commit(cs_plan* p) {
+  if (!p) return CS_EINVAL;
+  if (!p->set || p->committed) return CS_ESTATE;
+  if (!p->appendable) return CS_EINVAL;
+  cs_kv* kv = p->kv;
+  for (int i = 0; i < p->B; ++i)               // a sequence that was set anew since
+    if (kv->ctx_len[p->seqs[i]] != p->ctx[i] ||
+        static_cast<long>(p->ctx[i]) + p->lens[i] > static_cast<long>(kv->n_pages[p->seqs[i]]) * kPageSize)
+      return CS_ESTATE;
+  for (int i = 0; i < p->B; ++i) kv->ctx_len[p->seqs[i]] += p->lens[i];
+  p->committed = true;
+  return CS_OK;
+}
+
+int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new, const uint16_t* v_new,
+                      int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype, float scale, void* stream) {
+  int rc;
+  if ((rc = plan_ready(p, layer, dtype))) return rc;
+  cs_kv* kv = p->kv;
+  const cs_model_desc& d = kv->model->d;
+  if (kv->format != CS_KV_FMT_INT4 || !(scale >= 0.f) || scale > 3.0e38f) return CS_EINVAL;
+  if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;
+  if (p->T == 0) return CS_OK;
+  const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
+  if (!rows_ok(q, q_stride, q_row) || !rows_ok(out, out_stride, q_row)) return CS_EINVAL;
+  if (p->given && (!rows_ok(k_new, kv_stride, kv_row) || !rows_ok(v_new, kv_stride, kv_row))) return CS_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((rc = table_ready(kv, s))) return rc;
+  Attn4Params a = {};
+  a.q = q;
+  a.k_new = k_new;
+  a.v_new = v_new;
+  a.out = out;
+  a.q_stride = q_stride;
+  a.kv_stride = kv_stride;
+  a.out_stride = out_stride;
+  a.page_table = kv->table_dev;
+  a.pool = reinterpret_cast<const uint8_t*>(kv->pool) + layer * kv->layer4_bytes();
+  a.max_pages_per_seq = kv->max_pages_per_seq;
+  a.num_pages = kv->num_pages;
+  a.n_q_heads = d.n_q_heads;
+  a.n_kv_heads = d.n_kv_heads;
+  a.head_dim = d.head_dim;
+  a.given = p->given;
+  a.in_bf16 = a.out_bf16 = dtype == CS_BF16;
+  const double sc = scale > 0.f ? static_cast<double>(scale) : 1.0 / std::sqrt(static_cast<double>(d.head_dim));
+  a.scale_log2e = static_cast<float>(1.4426950408889634 * sc);
+  a.part_o = static_cast<float*>(p->part_o.p);
+  a.part_ml = static_cast<float*>(p->part_ml.p);
+  a.status = kv->model->status;
+  const AttnItem* items = reinterpret_cast<const AttnItem*>(static_cast<const int32_t*>(p->stg.dev.p) + p->off_items);
+  CS_CUDA(launch_attention_4bit(a, items, p->n_items, p->row_tile, p->any_split, s));
+  return CS_OK;
+}
+
+int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_pos, int T, uint16_t* out_k, uint16_t* out_v,
+               int dtype, void* stream) {
+  if (!kv || layer < 0 || layer >= kv->model->d.n_layers || T < 0 || T > (1 << 24) || (dtype != CS_F16 && dtype != CS_BF16))
+    return CS_EINVAL;
+  if (T == 0) return CS_OK;
+  if (!tok_seq || !tok_pos || !rows_ok(out_k, 8, 8) || !rows_ok(out_v, 8, 8)) return CS_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int rc;
+  if ((rc = table_ready(kv, s))) return rc;
+  const cs_model_desc& d = kv->model->d;
+  const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv->pool);
+  const size_t plane = kv->plane_elems * (kv->format == CS_KV_FMT_16BIT ? 2 : 1);
+  KvReadParams r = {};
+  r.pool_k = kv->format == CS_KV_FMT_INT4 ? pool + layer * kv->layer4_bytes() : pool + 2 * layer * plane;
+  r.pool_v = kv->format == CS_KV_FMT_INT4 ? nullptr : pool + (2 * layer + 1) * plane;
+  r.table = kv->table_dev;
+  r.tok_seq = tok_seq;
+  r.tok_pos = tok_pos;
+  r.out_k = out_k;
+  r.out_v = out_v;
+  r.T = T;
+  r.max_seqs = kv->max_seqs;
+  r.max_pages_per_seq = kv->max_pages_per_seq;
+  r.num_pages = kv->num_pages;
+  r.n_kv_heads = d.n_kv_heads;
+  r.dst_bf16 = dtype == CS_BF16;
+  r.status = kv->model->status;
+  CS_CUDA(launch_kv_read(r, kv->format, d.head_dim, s));
+  return CS_OK;
+}
+
 int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* tokens, const int32_t* lens, int B,
                void* stream) {
   if (!m || !kv || kv->model != m || B < 0) return CS_EINVAL;
-  if (kv->format != 0) return CS_EINVAL;   // the 8-bit cache is filled with given codes, not appended to
+  if (kv->format != CS_KV_FMT_16BIT && kv->format != CS_KV_FMT_INT4) return CS_EINVAL;   // the pass does not append to the 8-bit cache
   if (B == 0) return CS_OK;
   if (!seq_ids || !tokens || !lens) return CS_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -954,7 +1449,7 @@ int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* to
   int rc;
   BatchLayout L;
   const int32_t *dev_meta, *dev_tok;
-  if ((rc = stage_batch(m, kv, seq_ids, B, tokens, 0, lens, &L, &dev_meta, &dev_tok, s))) return rc;
+  if ((rc = stage_batch(m, kv, seq_ids, B, tokens, 0, lens, true, &L, &dev_meta, &dev_tok, s))) return rc;
   if ((rc = upload_table(kv, s))) return rc;
   if ((rc = run_layers(m, kv, kv, L, dev_meta, dev_tok, s))) return rc;
   for (int i = 0; i < B; ++i) kv->ctx_len[seq_ids[i]] += lens[i];
@@ -964,7 +1459,7 @@ int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* to
 int cs_append_accepted(cs_model* m, cs_kv* kv, int R, const int32_t* req_seq_ids, const int32_t* req_offsets,
                        const int32_t* dev_prefix_len, const int32_t* step_tokens, const int32_t* step_lens,
                        const int32_t* draft_lens, int32_t* host_prefix_len, void* stream) {
-  if (!m || !kv || kv->model != m || R < 0 || kv->format != 0) return CS_EINVAL;
+  if (!m || !kv || kv->model != m || R < 0 || (kv->format != CS_KV_FMT_16BIT && kv->format != CS_KV_FMT_INT4)) return CS_EINVAL;
   if (R == 0) return CS_OK;
   if (!req_seq_ids || !req_offsets || !dev_prefix_len || !step_tokens || !step_lens || !draft_lens) return CS_EINVAL;
   if (req_offsets[0] != 0) return CS_EINVAL;
@@ -1021,7 +1516,7 @@ int cs_verify_steps(cs_model* m, const cs_kv* ckv, const int32_t* seq_ids, int B
   int rc;
   BatchLayout L;
   const int32_t *dev_meta, *dev_tok;
-  if ((rc = stage_batch(m, kv, seq_ids, B, step_tokens, tokens_on_device, step_lens, &L, &dev_meta, &dev_tok, s)))
+  if ((rc = stage_batch(m, kv, seq_ids, B, step_tokens, tokens_on_device, step_lens, false, &L, &dev_meta, &dev_tok, s)))
     return rc;
   if ((rc = upload_table(kv, s))) return rc;
   if ((rc = run_layers(m, kv, nullptr, L, dev_meta, dev_tok, s))) return rc;

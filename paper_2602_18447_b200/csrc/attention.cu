@@ -686,8 +686,11 @@ cudaError_t launch_hd(const AttnParams& p, const CUtensorMap& tm_pool, const CUt
   using L = AttnSmem<HD>;
   static std::atomic<uint64_t> smem_opted{0};
   if (cudaError_t e = opt_in_dynamic_smem(attention_kernel<HD>, L::kTotal, smem_opted); e != cudaSuccess) return e;
-  cudaError_t le = launch_pdl(attention_kernel<HD>, dim3(n_items), dim3(kAttnThreads), L::kTotal, s, p, tm_pool, tm_kv_new, tm_q3d,
-                              items);
+  cudaError_t le = cudaSuccess;
+  if (p.pages_just_written)
+    attention_kernel<HD><<<n_items, kAttnThreads, L::kTotal, s>>>(p, tm_pool, tm_kv_new, tm_q3d, items);
+  else
+    le = launch_pdl(attention_kernel<HD>, dim3(n_items), dim3(kAttnThreads), L::kTotal, s, p, tm_pool, tm_kv_new, tm_q3d, items);
   count_launch();
   return le != cudaSuccess ? le : cudaGetLastError();
 }

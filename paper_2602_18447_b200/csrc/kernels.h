@@ -61,6 +61,9 @@ struct AttnParams {
   uint32_t* status;
   int32_t num_pages;        // pages of the pool and rows of the qkv workspace in use: range checks of debug builds
   int32_t n_rows;
+  // The kernel in front of this one writes the pages that this one reads (an expanded 4-bit cache): the launch is an ordinary
+  // one then, because the kernel requests its first cached pages before it waits for its predecessor.
+  int32_t pages_just_written = 0;
 };
 
 cudaError_t launch_embed(const int32_t* tokens, const uint16_t* embed, float* x, int T, int d, int vocab,
@@ -100,6 +103,62 @@ cudaError_t launch_attention_short(const AttnParams& p, const uint8_t* pool_k, c
 cudaError_t launch_kv_scatter_u8(const uint8_t* src_k, const uint8_t* src_v, int seq, const int32_t* page_table,
                                  int max_pages_per_seq, uint8_t* pool_k_plane, uint8_t* pool_v_plane, int n_kv_heads,
                                  int hd, int page_size, int T, cudaStream_t s);
+
+// ---- cache rows in every format (kv_rows.cu), and attention over the 4-bit one (attention_4bit.cu; layout: kv4.cuh)
+constexpr int CS_KV_FMT_16BIT = 0, CS_KV_FMT_E4M3 = 1, CS_KV_FMT_E5M2 = 2, CS_KV_FMT_INT4 = 3;
+
+// Up to 16 new tokens whose positions pos0 .. pos0 + n - 1 lie in one page: rows tok0 .. of the batch's token order.
+struct KvBlock {
+  int32_t tok0, n, seq, pos0;
+};
+struct KvAppendParams {
+  const uint16_t *k, *v, *q;       // rows of fp16 (or bf16: src_bf16), strides in elements; q may be null
+  uint16_t* q_out;
+  int64_t k_stride, v_stride, q_stride, q_out_stride;
+  const float2* rope;              // [T, head_dim / 2] cosine and sine of each token's position; null: no turn
+  const KvBlock* blocks;
+  const int32_t* table;            // page table [max_seqs, max_pages_per_seq]
+  uint8_t *pool_k, *pool_v;        // the layer's planes; 4-bit: pool_k = the layer's blocks, pool_v unused
+  int32_t max_pages_per_seq, num_pages, n_q_heads, n_kv_heads, src_bf16;
+  int32_t kv_parts, kv_heads_per_part, q_heads_per_part;     // set by the launcher
+  uint32_t* status;
+};
+cudaError_t launch_kv_append(KvAppendParams p, int format, int hd, int n_blocks, cudaStream_t s);
+struct KvReadParams {
+  const uint8_t *pool_k, *pool_v;
+  const int32_t *table, *tok_seq, *tok_pos;
+  uint16_t *out_k, *out_v;         // [T, n_kv_heads, head_dim], fp16 or bf16 (dst_bf16)
+  int32_t T, max_seqs, max_pages_per_seq, num_pages, n_kv_heads, dst_bf16;
+  int32_t heads_per_part;          // set by the launcher
+  uint32_t* status;
+};
+cudaError_t launch_kv_read(KvReadParams p, int format, int hd, cudaStream_t s);
+// The listed pages of a layer of the 4-bit cache as fp16 pages [num_pages][kv heads][16][head_dim] of a scratch pool.
+cudaError_t launch_kv_expand(const uint8_t* pool, const int32_t* pages, int n_pages, uint16_t* out_k, uint16_t* out_v,
+                             int n_kv_heads, int hd, int num_pages, uint32_t* status, cudaStream_t s);
+
+struct Attn4Params {
+  const uint16_t* q;               // [T, >= n_q_heads * head_dim], rotated; fp16 or bf16 (in_bf16); strides in elements
+  const uint16_t *k_new, *v_new;   // given: the new tokens' own rows (k rotated), not in the cache; same type as q
+  void* out;                       // [T, n_q_heads * head_dim] fp16 or bf16 (out_bf16)
+  int64_t q_stride, kv_stride, out_stride;
+  const int32_t* page_table;
+  const uint8_t* pool;             // the layer's blocks [num_pages][kv heads]
+  int32_t max_pages_per_seq, num_pages, n_q_heads, n_kv_heads, head_dim;
+  int32_t given;                   // 0: the new tokens' keys are in the cache; 1: in k_new, v_new
+  int32_t in_bf16, out_bf16;
+  int32_t cache_is_settled;        // nothing that may still run before this kernel writes the cache
+  float scale_log2e;
+  float* part_o;                   // [slots][32][head_dim]
+  float* part_ml;                  // [slots][32][2]
+  uint32_t* status;
+};
+// Items reuse AttnItem: q_tok0 = first query ROW (token * G + head in group) of the item's row tile; [tile_begin, tile_end)
+// counts pages, the cached ones first (pad[1] of them), then pages of 16 own keys (given only); ctx = cached keys in front
+// of the step's first token.
+int attention_4bit_row_tile(int max_rows);
+cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int row_tile, bool any_split,
+                                  cudaStream_t s);
 
 // x_last[b] = x[cu_new[b + 1] - 1], fp32 [B, d].
 cudaError_t launch_gather_last_rows(const float* x, const int32_t* cu_new, float* x_last, int B, int d, cudaStream_t s);

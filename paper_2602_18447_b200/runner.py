@@ -42,6 +42,8 @@ class VerifySession:
         fmt = getattr(self.cfg, "kv_format", "bf16")
         if fmt in ("e4m3", "e5m2"):
             self.kv = B.cs_kv_alloc_8bit(self.model, total_pages, ps, self.n_steps, max_pp, fmt)
+        elif fmt == "int4":
+            self.kv = B.cs_kv_alloc_4bit(self.model, total_pages, ps, self.n_steps, max_pp)
         else:
             self.kv = B.cs_kv_alloc(self.model, total_pages, ps, self.n_steps, max_pp)
         for i, pages in enumerate(pages_per_step):
