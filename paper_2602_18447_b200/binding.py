@@ -246,11 +246,17 @@ def cs_kv_alloc_4bit(model: int, num_pages: int, page_size: int, max_seqs: int, 
 CS_F16, CS_BF16 = 0, 1
 
 
+_dtype_codes: dict = {}
+
+
 def _dtype_code(t) -> int:
-    import torch
-    if t.dtype not in (torch.float16, torch.bfloat16):
+    if not _dtype_codes:
+        import torch
+        _dtype_codes.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16})
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
         raise ValueError(f"expected float16 or bfloat16 rows, got {t.dtype}")
-    return CS_F16 if t.dtype == torch.float16 else CS_BF16
+    return code
 
 
 def _rows(t, like=None):
@@ -259,15 +265,18 @@ def _rows(t, like=None):
     it has to have."""
     if t is None:
         return None, 0
-    if not t.is_cuda or t.dim() not in (2, 3):
+    shape, stride = t.shape, t.stride()
+    nd = len(shape)
+    if not t.is_cuda or nd not in (2, 3):
         raise ValueError("expected a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim]")
-    row = t.shape[1] * (t.shape[2] if t.dim() == 3 else 1)
-    inner = t.shape[0] == 0 or (t.stride(-1) == 1 and (t.dim() == 2 or t.shape[1] == 1 or t.stride(1) == t.shape[2]))
-    if not inner:
+    n = shape[0]
+    if n and (stride[-1] != 1 or (nd == 3 and stride[1] != shape[2] and shape[1] != 1)):
         raise ValueError("the heads of a row have to be contiguous")
-    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.device != like.device):
+    if like is not None and (t.dtype != like.dtype or n != like.shape[0] or t.get_device() != like.get_device()):
         raise ValueError("the rows of one call have one type, one device and one count")
-    return t.data_ptr(), max(row, t.stride(0)) if t.shape[0] <= 1 else t.stride(0)
+    if n > 1:
+        return t.data_ptr(), stride[0]
+    return t.data_ptr(), max(shape[1] * (shape[2] if nd == 3 else 1), stride[0])      # the stride of one row says nothing
 
 
 def cs_plan_create(kv: int, max_steps: int = 0, max_tokens: int = 0) -> int:

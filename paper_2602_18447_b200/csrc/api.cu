@@ -161,8 +161,8 @@ struct cs_kv {
 struct cs_plan {
   cs_kv* kv;
   int device = 0;
-  bool set = false, given = false, appendable = false, committed = false, any_split = false;
-  int B = 0, T = 0, n_blocks = 0, n_items = 0, row_tile = 8;
+  bool set = false, given = false, appendable = false, committed = false;
+  int B = 0, T = 0, n_blocks = 0, n_items = 0, n_merge = 0, row_tile = 8;
   size_t off_pos = 0, off_blocks = 0, off_items = 0;      // int32 offsets into the staged block
   std::vector<int32_t> seqs, lens, ctx;
   Staging stg;
@@ -223,6 +223,7 @@ struct BatchLayout {
   int n_pages = 0;         // 4-bit cache, expand: pages to expand
   bool expand = false;     // 4-bit cache: the tensor-core attention runs over expanded pages (else the 4-bit kernel)
   int row_tile = 8;        // 4-bit cache: query rows per work item of the 4-bit kernel
+  int n_merge = 0;         // 4-bit kernel: ranges cut into pieces (listed behind the n_items items)
   int max_rows = 0;        // 8-bit cache: the largest number of query rows (new tokens x heads per kv head) of a step
   bool any_split = false;  // 8-bit cache: some context is cut into pieces
 };
@@ -238,11 +239,13 @@ constexpr double kAttnPieceExtra = 2.0;
 constexpr double kAttnMergeFixed = 1.0;
 constexpr double kAttnMergePerSplit = 0.5;
 
-// 4-bit attention: pieces of a context hold at least this many pages, there are about this many of them per SM, and a
-// step's range is cut into at most this many.
-constexpr long kAttn4MinPages = 16;
-constexpr long kAttn4PiecesPerSm = 6;
-constexpr long kAttn4MaxPieces = 64;
+// 4-bit attention, in pages of one CTA among as many as fit on its SM (0.28 us at 8 query rows): the smallest piece worth an item
+// of its own; what an item costs besides its pages (alone 3.2 us from launch to end, most of it latencies in a row; counted higher
+// because long pieces proved faster wherever there is more than one wave: 64 contexts of 2 K to 8 K keys 66.9 us with 28, 69.4 with
+// 12); what joining pieces adds to a launch.
+constexpr int kAttn4MinPages = 8;
+constexpr double kAttn4Fixed = 28;
+constexpr double kAttn4Join = 8;
 // Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves; longer
 // ones have them expanded to fp16 for the tensor-core kernel.
 constexpr int kAttn4MaxRows = 32;
@@ -371,42 +374,98 @@ void build_short_work(const cs_model* m, int B, const int32_t* lens, const int32
   *n_slots = slots;
 }
 
-// Work items of the 4-bit attention: one per (step, kv head, tile of `row_tile` query rows, piece of the pages). Pages are
-// the cached ones and, when the new tokens' keys are given as rows (`given`), the pages of 16 of those behind them.
-void build_4bit_work(const cs_model* m, int B, const int32_t* lens, const int32_t* ctx, bool given, int row_tile,
-                     std::vector<AttnItem>& items, int* n_slots, bool* any_split) {
+// Work list of the 4-bit attention.
+struct Attn4Work {
+  std::vector<AttnItem> items;   // the work, and behind it one item (the last piece) of each of the n_merge ranges that were cut
+  int n_items = 0, n_merge = 0, n_slots = 0, row_tile = 8;
+};
+
+// One item per (step, kv head, tile of query rows, piece of the pages). Pages are the cached ones and, when the new tokens' keys
+// are given as rows (`given`), the pages of 16 of those behind them.
+//
+// The pieces' size is the candidate with the smallest estimated finish time of the launch on the SMs' slots (CTAs that fit at
+// once), handed out longest first: an item costs its pages and a fixed part (kAttn4Fixed pages: work list, page ids and first
+// pages one after the other, then the warps' results), and cutting at all costs a joining step. Small batches so end up with one
+// wave of short pieces, large ones with few long pieces.
+Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const int32_t* ctx, bool given) {
+  Attn4Work w;
   const int heads = m->d.n_kv_heads, G = m->d.n_q_heads / heads;
+  int max_rows = 0;
+  for (int i = 0; i < B; ++i) max_rows = std::max(max_rows, lens[i] * G);
+  w.row_tile = attention_4bit_row_tile(max_rows);
   struct Unit { int step, row0, cached, pages; };
   std::vector<Unit> units;
   long total = 0;
+  int longest = 1;
   for (int i = 0; i < B; ++i)
-    for (int r = 0; r < lens[i] * G; r += row_tile) {
-      const int t_last = std::min(lens[i] - 1, (r + row_tile - 1) / G);
+    for (int r = 0; r < lens[i] * G; r += w.row_tile) {
+      const int t_last = std::min(lens[i] - 1, (r + w.row_tile - 1) / G);
       const int cached = given ? (ctx[i] + kPageSize - 1) / kPageSize : (ctx[i] + t_last) / kPageSize + 1;
       const int pages = cached + (given ? t_last / kPageSize + 1 : 0);
       units.push_back(Unit{i, r, cached, pages});
-      total += static_cast<long>(pages) * heads;
+      total += pages;
+      longest = std::max(longest, pages);
     }
-  const long chunk = std::max<long>(kAttn4MinPages, total / (kNumSMs * kAttn4PiecesPerSm) + 1);
-  items.clear();
-  int slots = 0;
-  *any_split = false;
+  const int fit = attention_4bit_ctas_per_sm(w.row_tile), slots = kNumSMs * fit;
+  auto pieces = [](int pages, int cap) { return std::min<int>(cs::kAttn4MaxPieces, (pages + cap - 1) / cap); };
+  // the heads of a unit cost the same: one head's items on the slots' share
+  const double machines = std::max(1.0, static_cast<double>(slots) / heads);
+  std::vector<double> cost;
+  auto estimate = [&](int cap, double to_beat) {
+    cost.clear();
+    double longest_item = 0.0, sum = 0.0;
+    bool cut = false;
+    for (const Unit& u : units) {
+      const int n = pieces(u.pages, cap);
+      cut = cut || n > 1;
+      const double c = kAttn4Fixed + static_cast<double>(u.pages) / n;
+      for (int s = 0; s < n; ++s) cost.push_back(c);
+      longest_item = std::max(longest_item, c);
+      sum += n * c;
+    }
+    const double join = cut ? kAttn4Join : 0.0;
+    if (cost.size() <= machines) {
+      // fewer items than slots: an SM with fewer of them runs each one faster (one alone takes 0.35 of its time among `fit`)
+      const double k = std::ceil(static_cast<double>(cost.size()) * heads / kNumSMs);
+      const double pace = fit > 1 ? 0.35 + 0.65 * (std::min<double>(k, fit) - 1) / (fit - 1) : 1.0;
+      return kAttn4Fixed + (longest_item - kAttn4Fixed) * pace + join;
+    }
+    if (std::max(longest_item, sum / machines) + join >= to_beat) return to_beat;
+    return list_schedule_makespan(cost, static_cast<int>(machines)) + join;
+  };
+  int best_cap = longest;
+  double best = estimate(longest, 1e300);
+  int last_cap = longest;
+  auto consider = [&](int cap) {
+    cap = std::max(cap, kAttn4MinPages);
+    if (cap >= last_cap) return;
+    last_cap = cap;
+    const double e = estimate(cap, best);
+    if (e < best) { best = e; best_cap = cap; }
+  };
+  const double share = total / machines;           // pages per slot
+  for (double f : {4.0, 2.0, 1.5, 1.33, 1.2, 1.12, 1.06, 1.0, 0.8, 0.65, 0.55, 0.5, 0.4, 0.33, 0.25, 0.2})
+    consider(static_cast<int>(std::ceil(share * f)));
+  std::vector<AttnItem> merge;
   for (const Unit& u : units) {
-    const int n = static_cast<int>(std::min<long>(kAttn4MaxPieces, std::max<long>(1, (u.pages + chunk - 1) / chunk)));
+    const int n = pieces(u.pages, best_cap);
     for (int h = 0; h < heads; ++h) {
       for (int s = 0; s < n; ++s) {
         const int b = static_cast<int>(static_cast<long>(u.pages) * s / n);
         const int e = static_cast<int>(static_cast<long>(u.pages) * (s + 1) / n);
-        items.push_back(AttnItem{u.step, h, u.row0, b, e, n > 1 ? slots + s : 0, n > 1 ? slots : 0, n, 0, lens[u.step],
-                                 ctx[u.step], 0, {0, u.cached, 0, 0}});
+        w.items.push_back(AttnItem{u.step, h, u.row0, b, e, n > 1 ? w.n_slots + s : 0, n > 1 ? w.n_slots : 0, n, 0, lens[u.step],
+                                   ctx[u.step], 0, {0, u.cached, 0, 0}});
       }
-      if (n > 1) { slots += n; *any_split = true; }
+      if (n > 1) { w.n_slots += n; merge.push_back(w.items.back()); }
     }
   }
-  std::stable_sort(items.begin(), items.end(), [](const AttnItem& a, const AttnItem& b) {
+  std::stable_sort(w.items.begin(), w.items.end(), [](const AttnItem& a, const AttnItem& b) {
     return (a.tile_end - a.tile_begin) > (b.tile_end - b.tile_begin);
   });
-  *n_slots = slots;
+  w.n_items = static_cast<int>(w.items.size());
+  w.n_merge = static_cast<int>(merge.size());
+  w.items.insert(w.items.end(), merge.begin(), merge.end());
+  return w;
 }
 
 // The new tokens of every step, cut at page borders.
@@ -597,7 +656,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
         a4.part_o = ap.part_o;
         a4.part_ml = ap.part_ml;
         a4.status = m->status;
-        CS_STEP(kProfAttn, launch_attention_4bit(a4, d_items, L.n_items, L.row_tile, L.any_split, s));
+        CS_STEP(kProfAttn, launch_attention_4bit(a4, d_items, L.n_items, L.n_merge, L.row_tile, s));
       }
     } else if (kv->format != 0) {
       const uint8_t* pool8 = reinterpret_cast<const uint8_t*>(kv->pool);
@@ -695,7 +754,7 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   bool any_split = false;
   std::vector<KvBlock> blocks;
   std::vector<int32_t> pages;
-  int row_tile = 8;
+  Attn4Work work4;
   if (kv->format == CS_KV_FMT_INT4) {
     const int G = m->d.n_q_heads / m->d.n_kv_heads;
     for (int i = 0; i < B; ++i) max_rows = std::max(max_rows, lens[i] * G);
@@ -710,8 +769,9 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
         pages.insert(pages.end(), row, row + (ctx[i] + kPageSize - 1) / kPageSize);
       }
     } else {
-      row_tile = attention_4bit_row_tile(max_rows);
-      build_4bit_work(m, B, lens, ctx.data(), true, row_tile, items, &n_slots, &any_split);
+      work4 = build_4bit_work(m, B, lens, ctx.data(), true);
+      n_slots = work4.n_slots;
+      items.swap(work4.items);
     }
   } else if (kv->format != 0) {
     const int G = m->d.n_q_heads / m->d.n_kv_heads;
@@ -735,10 +795,11 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   L.off_blocks = take(blocks.size() * (sizeof(KvBlock) / 4));
   L.off_pages = take(pages.size());
   L.total = o;
-  L.n_items = static_cast<int>(items.size());
+  L.n_items = static_cast<int>(items.size()) - work4.n_merge;
+  L.n_merge = work4.n_merge;
   L.n_blocks = static_cast<int>(blocks.size());
   L.n_pages = static_cast<int>(pages.size());
-  L.row_tile = row_tile;
+  L.row_tile = work4.row_tile;
   L.expand = kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows;
   L.n_slots = n_slots;
   L.max_rows = max_rows;
@@ -1221,13 +1282,8 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
     if (T * (m->d.n_q_heads / m->d.n_kv_heads) > (1 << 24)) return CS_EINVAL;
   }
   if (!given && !room) return CS_EINVAL;      // the new tokens' keys are to be in the cache: it needs pages for them
-  const int G = m->d.n_q_heads / m->d.n_kv_heads;
   std::vector<int32_t> ctx(B);
-  int max_rows = 0;
-  for (int i = 0; i < B; ++i) {
-    ctx[i] = kv->ctx_len[seq_ids[i]];
-    max_rows = std::max(max_rows, lens[i] * G);
-  }
+  for (int i = 0; i < B; ++i) ctx[i] = kv->ctx_len[seq_ids[i]];
   // appending writes every page's slots once: no two steps on one sequence, or on sequences that share a page they write
   bool distinct = true;
   std::vector<KvBlock> blocks;
@@ -1240,12 +1296,10 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
     std::sort(written.begin(), written.end());
     distinct = std::adjacent_find(written.begin(), written.end()) == written.end();
   }
-  std::vector<AttnItem> items;
-  int n_slots = 0;
-  bool any_split = false;
-  const int row_tile = attention_4bit_row_tile(max_rows);
-  if (kv->format == CS_KV_FMT_INT4 && B > 0)
-    build_4bit_work(m, B, lens, ctx.data(), given != 0, row_tile, items, &n_slots, &any_split);
+  Attn4Work work;
+  if (kv->format == CS_KV_FMT_INT4 && B > 0) work = build_4bit_work(m, B, lens, ctx.data(), given != 0);
+  std::vector<AttnItem>& items = work.items;
+  const int n_slots = work.n_slots;
   size_t o = 0;
   auto take = [&o](size_t n) { size_t r = o; o += (n + 3) & ~size_t(3); return r; };
   const size_t off_pos = take(T);
@@ -1255,8 +1309,8 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
   p->set = false;
   const int hd = m->d.head_dim;
   if ((rc = p->rope.ensure(static_cast<size_t>(std::max(1L, T)) * (hd / 2) * sizeof(float2)))) return rc;
-  if ((rc = p->part_o.ensure(static_cast<size_t>(n_slots) * 32 * hd * 4))) return rc;
-  if ((rc = p->part_ml.ensure(static_cast<size_t>(n_slots) * 32 * 2 * 4))) return rc;
+  if ((rc = p->part_o.ensure(static_cast<size_t>(n_slots) * kAttn4Rows * hd * 4))) return rc;
+  if ((rc = p->part_ml.ensure(static_cast<size_t>(n_slots) * kAttn4Rows * 2 * 4))) return rc;
   if ((rc = p->stg.dev.ensure(o * 4))) return rc;
   if (o > 0) {
     int slot;
@@ -1286,10 +1340,10 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
   p->given = given != 0;
   p->appendable = room && distinct;
   p->committed = false;
-  p->any_split = any_split;
-  p->row_tile = row_tile;
+  p->n_merge = work.n_merge;
+  p->row_tile = work.row_tile;
   p->n_blocks = static_cast<int>(blocks.size());
-  p->n_items = static_cast<int>(items.size());
+  p->n_items = work.n_items;
   p->off_pos = off_pos;
   p->off_blocks = off_blocks;
   p->off_items = off_items;
@@ -1397,7 +1451,7 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   a.part_ml = static_cast<float*>(p->part_ml.p);
   a.status = kv->model->status;
   const AttnItem* items = reinterpret_cast<const AttnItem*>(static_cast<const int32_t*>(p->stg.dev.p) + p->off_items);
-  CS_CUDA(launch_attention_4bit(a, items, p->n_items, p->row_tile, p->any_split, s));
+  CS_CUDA(launch_attention_4bit(a, items, p->n_items, p->n_merge, p->row_tile, s));
   return CS_OK;
 }
 

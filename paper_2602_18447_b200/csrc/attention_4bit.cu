@@ -4,7 +4,8 @@
 // Mathematics. A cached key is k_d = s c_d + o with one (s, o) per 64-channel group, so
 //     q . k = sum_groups s (sum_d q_d c_d) + o (sum_d q_d),         out_d = sum_j p_j (s_j c_jd + o_j)
 // and the products run over the integer codes, which are exact in fp16: scales multiply the fp32 sums of a group (keys) or
-// the codes in registers (values), offsets go through one small product each.
+// the probabilities (values), offsets go through one small product each. Value codes are centred, c - 8, which halves the
+// rounding of p s: it then weighs a value's distance from the middle of its group's range, not from its end.
 //
 // Shape. The keys are the rows of the products and the query rows (token, head of the group) their columns: 16 keys x 8
 // query rows x 16 channels per instruction, so that a decode step's few query rows (one token, up to 8 heads per kv head)
@@ -12,12 +13,17 @@
 // lane pair of columns; P^T turns into the operand of O^T = V^T P^T by two 8 x 8 register transposes.
 //
 // Bound. Reading the cache: HD / 2 + 4 HD / 64 bytes per row of K or V. Every warp streams whole (page, kv head) blocks with
-// asynchronous copies, two in flight; nothing waits on another CTA. At the copy bandwidth an SM has ~100 cycles per block,
+// asynchronous copies, two pages at a time and two such rounds ahead; nothing waits on another CTA. At the copy bandwidth an SM has ~100 cycles per block,
 // some 400 issue slots over its four schedulers, against ~260 instructions per block (8 query rows, HD = 128): what follows
-// counts instructions. Codes become fp16 operands with one mask and one shift per pair (no conversion instruction): a
-// nibble in the mantissa of a power of two, 64 + c, whose 64 is taken back by the accumulator's start value (keys), or
-// 64 + c / 16 and 4 + c / 16, which one fused multiply-add turns into s c / 16 exactly before rounding (values).
-// A piece of a long context leaves (max, sum, O) in fp32 and a second kernel joins the pieces in a fixed order.
+// counts instructions. Codes become fp16 operands without a conversion instruction: a nibble in the mantissa of a power of
+// two, 64 + c or 1024 + c. The 64 of half of a key's channels is taken back by the product that adds the offsets,
+//     q . k = sum_groups s (sum_d q_d h_d) + o (sum_d q_d) - 64 s (sum over those channels of q_d),
+// whose operands are the offsets and scales as they are stored; one packed addition makes c (keys) or c - 8 (values) of the
+// others. The product that sums the values' offsets has rows of ones besides, which sum the probabilities.
+// A piece of a long context leaves (max, sum, O) in fp32 and a second kernel, one CTA per query row, joins the pieces in their
+// order. (Joining by the last piece to finish saves that launch but takes longer, even for few pieces: the fence, the counter
+// and the reads follow one another at the end of the chain, while the second kernel's start overlaps this one. One token on 512
+// keys 7.9 us against 6.0, 16 sequences of up to 2048 10.7 against 9.2.)
 #include <type_traits>
 
 #include "common.cuh"
@@ -31,11 +37,13 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kWarps = 4;
 constexpr int kPage = 16;
-constexpr int kStages = 3;
+constexpr int kStages = 3;              // of two pages each, per warp
 constexpr float kNoMax = -1.0e30f;
-// The running maximum is raised only when a score passes it by this much (powers of two): probabilities reach 2^8, which
-// fp16 and the fp32 sums hold with their full relative precision, and most pages leave the accumulators alone.
-constexpr float kMaxSlack = 8.f;
+constexpr uint32_t kOnes = 0x3C003C00u;      // two fp16 ones
+// Probabilities are taken against a reference below the running maximum, so that the largest is 2^kHeadroom when the reference
+// is set and up to 2^kRaise before it is raised: most pages leave the accumulators alone, small probabilities keep fp16's
+// relative precision down to 2^-16 of the largest, and p s stays in fp16's range for every scale (kKv4MaxScale).
+constexpr float kHeadroom = 2.f, kRaise = 6.f;
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -45,27 +53,24 @@ template <int N>
 __device__ __forceinline__ void cp_async_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
-// D (16 x 8, fp32) = A (16 x 16, fp16, row) * B (16 x 8, fp16, col) + C
-__device__ __forceinline__ void mma_k16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, float c0, float c1,
-                                        float c2, float c3) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %11, %12, %13};"
-      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(c0), "f"(c1), "f"(c2), "f"(c3));
-}
+// D (16 x 8, fp32) += A (16 x 16, fp16, row) * B (16 x 8, fp16, col)
 __device__ __forceinline__ void mma_k16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  mma_k16(d, a, b0, b1, d[0], d[1], d[2], d[3]);
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// D (16 x 8, fp32) = A (16 x 8, fp16, row) * B (8 x 8, fp16, col)
-__device__ __forceinline__ void mma_k8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5}, {%6}, {%7, %7, %7, %7};"
-               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-               : "r"(a0), "r"(a1), "r"(b0), "f"(0.f));
+// the same without an addend
+__device__ __forceinline__ void mma_k16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 // 8 x 8 matrix of 16-bit elements spread over the warp, transposed
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
   uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
   return d;
 }
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
@@ -78,14 +83,23 @@ __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
   __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t hfma2_u(uint32_t a, uint32_t b, uint32_t c) {
-  __half2 r = __hfma2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b), *reinterpret_cast<__half2*>(&c));
+__device__ __forceinline__ uint32_t hadd2_u(uint32_t a, uint32_t b) {
+  __half2 r = __hadd2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<uint32_t*>(&r);
 }
-// nibbles 0 and 4 of w: 64 + c / 16;  nibbles 1 and 5: 4 + c / 16, or 64 + c when placed under the exponent of 64
-__device__ __forceinline__ uint32_t low_codes(uint32_t w) { return (w & 0x000F000Fu) | 0x54005400u; }
-__device__ __forceinline__ uint32_t high_codes(uint32_t w) { return (w & 0x00F000F0u) | 0x44004400u; }
-__device__ __forceinline__ uint32_t whole_codes(uint32_t w) { return (w & 0x00F000F0u) | 0x54005400u; }
+// (w & mask) | bits as one instruction (the compiler makes two of the expression)
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t mask, uint32_t bits) {
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(w), "r"(mask), "r"(bits));
+  return r;
+}
+// nibbles 1 and 5 of w as 64 + c
+__device__ __forceinline__ uint32_t codes64(uint32_t w) { return and_or(w, 0x00F000F0u, 0x54005400u); }
+// c of nibbles 0 and 4 (1024 + c - 1024), exact
+__device__ __forceinline__ uint32_t codes_low(uint32_t w) { return hadd2_u(and_or(w, 0x000F000Fu, 0x64006400u), 0xE400E400u); }
+// c - 8 of nibbles 0 and 4 (1024 + c - 1032) and of nibbles 1 and 5 (64 + c - 72), exact
+__device__ __forceinline__ uint32_t centred_low(uint32_t w) { return hadd2_u(and_or(w, 0x000F000Fu, 0x64006400u), 0xE408E408u); }
+__device__ __forceinline__ uint32_t centred_high(uint32_t w) { return hadd2_u(codes64(w), 0xD480D480u); }
 
 // Eight 16-bit values as fp16: bf16 sources are re-encoded (exact for magnitudes in [2^-14, 65504]).
 __device__ __forceinline__ uint4 as_f16(uint4 v, bool bf16) {
@@ -98,29 +112,57 @@ __device__ __forceinline__ void store_out(const Attn4Params& p, size_t at, float
   else reinterpret_cast<__half*>(p.out)[at] = __float2half_rn(v);
 }
 
+// CTAs that an SM holds at once (128 and 168 registers a thread).
+__host__ __device__ constexpr int ctas_per_sm(int nt) { return nt == 1 ? 4 : 3; }
+
 template <int HD, int NT>
 struct Smem4 {
-  static constexpr int kWarp = kStages * Kv4<HD>::kBlock;
+  static constexpr int kWarp = kStages * 2 * Kv4<HD>::kBlock;
   static constexpr int kStagesBytes = kWarps * kWarp;
   static constexpr int kPad = HD + 4;                                  // row stride of the partial results, in floats
   static constexpr int kPartBytes = kWarps * 8 * NT * kPad * 4;
   static constexpr int kStatBytes = kWarps * 8 * NT * 2 * 4;
   static constexpr int kUnion = kStagesBytes > kPartBytes + kStatBytes ? kStagesBytes : kPartBytes + kStatBytes;
-  // 32 query rows: the query operands do not fit the registers beside the accumulators
-  static constexpr int kQBytes = NT > 2 ? 8 * NT * HD * 2 : 0;
+  // from 16 query rows on, the query operands do not fit the registers beside the accumulators
+  static constexpr int kQBytes = NT > 1 ? 8 * NT * HD * 2 : 0;
   static constexpr int kTotal = kUnion + kQBytes;
   static_assert(kWarp >= kPage * HD * 2, "a page of own values must fit in one warp's stages");
 };
 
-// NT = number of 8-row tiles of query rows (1, 2 or 4).
+// What each piece of a cut range weighs in the output of query row r: 2^(its reference - the largest) / the whole sum. One warp,
+// two pieces a lane.
+__device__ __forceinline__ void piece_weights(const Attn4Params& p, const AttnItem& it, int r, int lane, float* weight) {
+  const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + static_cast<size_t>(it.slot0) * kAttn4Rows + r;
+  float2 x[2];
+  float M = kNoMax, sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int s = lane + 32 * j;
+    x[j] = s < it.n_splits ? __ldcg(ml + s * kAttn4Rows) : make_float2(kNoMax, 0.f);
+    M = fmaxf(M, x[j].x);
+  }
+  M = warp_max(M);
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    x[j].x = fast_exp2(x[j].x - M);
+    sum += x[j].x * x[j].y;
+  }
+  sum = warp_sum(sum);
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+    if (lane + 32 * j < it.n_splits) weight[lane + 32 * j] = x[j].x * inv;
+}
+
+// NT = number of 8-row tiles of query rows (1 or 2).
 template <int HD, int NT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 4 : NT == 2 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, ctas_per_sm(NT))
 attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   using L = Kv4<HD>;
   using S = Smem4<HD, NT>;
   constexpr int NG = L::kGroups;            // channel groups
   constexpr int MT = HD / 16;               // 16-channel tiles of the output
-  constexpr bool kQInRegs = NT <= 2;
+  constexpr bool kQInRegs = S::kQBytes == 0;
   extern __shared__ __align__(128) uint8_t smem[];
   pdl_launch_dependents();
   const AttnItem it = items[blockIdx.x];
@@ -134,27 +176,35 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   const int32_t* table = p.page_table + static_cast<size_t>(it.seq) * p.max_pages_per_seq;
   const int cached_pages = it.pad[1];
   const size_t page_stride = static_cast<size_t>(p.n_kv_heads) * L::kBlock;
-  const uint8_t* pool_h = p.pool + static_cast<size_t>(it.kv_head) * L::kBlock;
   const int end_cached = min(it.tile_end, cached_pages);
 
-  auto fetch = [&](int32_t id, int stage) {
+  // A round is two pages: half a warp copies each.
+  const int half = lane >> 4, sub = (lane & 15) * 16;
+  const uint8_t* src0 = p.pool + static_cast<size_t>(it.kv_head) * L::kBlock + sub;
+  const uint32_t dst0 = my_u + half * L::kBlock + sub;
+  auto fetch = [&](int pg, int32_t id, int stage_off) {
+    if (pg + half >= end_cached) return;
     if (!debug_in_range(id >= 0 && id < p.num_pages, p.status)) id = 0;
-    const uint8_t* src = pool_h + static_cast<size_t>(id) * page_stride + lane * 16;
-    const uint32_t dst = my_u + stage * L::kBlock + lane * 16;
+    const uint8_t* src = src0 + static_cast<size_t>(id) * page_stride;
+    const uint32_t dst = dst0 + stage_off;
 #pragma unroll
-    for (int c = 0; c < L::kBlock / 512; ++c) cp_async_16(dst + c * 512, src + c * 512);
-    if (lane < (L::kBlock % 512) / 16) cp_async_16(dst + L::kBlock / 512 * 512, src + L::kBlock / 512 * 512);
+    for (int c = 0; c < L::kBlock / 256; ++c) cp_async_16(dst + c * 256, src + c * 256);
+    if (L::kBlock % 256 && sub < L::kBlock % 256) cp_async_16(dst + L::kBlock / 256 * 256, src + L::kBlock / 256 * 256);
   };
-  const int pg0 = it.tile_begin + warp;
-  // Where nothing that precedes this kernel on the stream writes the cache (the verification pass), the first pages are
-  // requested before the wait; a caller who has just appended waits first.
-  if (!p.cache_is_settled) pdl_wait();
+  constexpr int kStep = 2 * kWarps;            // pages between a warp's rounds
+  constexpr int kStageBytes = 2 * L::kBlock;
+  const int pg0 = it.tile_begin + 2 * warp;
+  auto page_id = [&](int pg) -> int32_t { return pg + half < end_cached ? __ldg(table + pg + half) : 0; };
+  // No kernel writes the page table or the work list: they are read ahead of the wait. Where nothing that precedes this kernel on
+  // the stream writes the cache either (the verification pass), the first pages are requested before it too; a caller who has just
+  // appended waits first.
   int32_t ids[kStages];
 #pragma unroll
-  for (int st = 0; st < kStages; ++st) ids[st] = pg0 + st * kWarps < end_cached ? __ldg(table + pg0 + st * kWarps) : 0;
+  for (int st = 0; st < kStages; ++st) ids[st] = page_id(pg0 + st * kStep);
+  if (!p.cache_is_settled) pdl_wait();
 #pragma unroll
   for (int st = 0; st < kStages - 1; ++st) {
-    if (pg0 + st * kWarps < end_cached) fetch(ids[st], st);
+    fetch(pg0 + st * kStep, ids[st], st * kStageBytes);
     cp_async_commit();
   }
   int32_t id_ahead = ids[kStages - 1];
@@ -163,18 +213,19 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   // Query operands. Lane (g, q) holds, for each group and each of the two words of a key row's chunk, the eight channels
   // 64 group + 16 q + 8 w .. + 7 of query row g of a tile: two k-steps of the score product.
   uint4 qr[kQInRegs ? NT : 1][NG][2];
-  uint32_t qoff[NT];           // operand of the offsets' product: sums of q over (half a group), high and low parts
-  float qneg[NT][NG][2];       // -64 sum_group q of query rows 2 q and 2 q + 1: the accumulators' start values
+  // operands of the product with a key's offsets and scales: sums of q over half a group each, -64 times the sums over the
+  // channels held as 64 + c, high and low parts
+  uint32_t qoff[NT], qscale[NT];
   uint8_t* q_s = smem + S::kUnion;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = nt * 8 + g;
     uint4 v[NG][2];
-    float sum[NG];
+    float sum[NG], sum64[NG];
     const int t = (row0 + r) / G, hq = (row0 + r) % G;
 #pragma unroll
     for (int grp = 0; grp < NG; ++grp) {
-      sum[grp] = 0.f;
+      sum[grp] = sum64[grp] = 0.f;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         v[grp][w] = make_uint4(0, 0, 0, 0);
@@ -185,27 +236,25 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
         for (int i = 0; i < 4; ++i) {
           const float2 f = unpack_f16x2(word(v[grp][w], i));
           sum[grp] += f.x + f.y;
+          if (i & 1) sum64[grp] += f.x + f.y;
         }
         if (kQInRegs) qr[nt][grp][w] = v[grp][w];
         else if (warp == 0) *reinterpret_cast<uint4*>(q_s + ((nt * NG + grp) * 2 + w) * 512 + lane * 16) = v[grp][w];
       }
       sum[grp] += __shfl_xor_sync(0xffffffffu, sum[grp], 1);     // lanes q = 0, 1 and q = 2, 3: half a group each
+      sum64[grp] += __shfl_xor_sync(0xffffffffu, sum64[grp], 1);
     }
-    // A half group's sum in two fp16 parts (22 bits); the four lanes of a row give the four slots of the k = 8 product.
-    float part[2];
+    // A sum in two fp16 parts (22 bits): the lanes q of a row give a half group's high part, its low part, and the other half's.
+    float part[2], part64[2];
 #pragma unroll
     for (int grp = 0; grp < 2; ++grp) {
-      const float f = grp < NG ? sum[grp < NG ? grp : 0] : 0.f;
-      const float hi = __half2float(__float2half_rn(f));
+      const float f = grp < NG ? sum[grp < NG ? grp : 0] : 0.f, f64 = grp < NG ? -64.f * sum64[grp < NG ? grp : 0] : 0.f;
+      const float hi = __half2float(__float2half_rn(f)), hi64 = __half2float(__float2half_rn(f64));
       part[grp] = q & 1 ? f - hi : hi;
+      part64[grp] = q & 1 ? f64 - hi64 : hi64;
     }
     qoff[nt] = pack_f16x2(part[0], part[1]);
-#pragma unroll
-    for (int grp = 0; grp < NG; ++grp) {
-      const float total = sum[grp] + __shfl_xor_sync(0xffffffffu, sum[grp], 2);
-      qneg[nt][grp][0] = -64.f * __shfl_sync(0xffffffffu, total, 8 * q);
-      qneg[nt][grp][1] = -64.f * __shfl_sync(0xffffffffu, total, 8 * q + 4);
-    }
+    qscale[nt] = pack_f16x2(part64[0], part64[1]);
   }
   if (!kQInRegs) __syncthreads();
   auto q_words = [&](int nt, int grp, int w) -> uint4 {
@@ -213,39 +262,45 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     return *reinterpret_cast<const uint4*>(q_s + ((nt * NG + grp) * 2 + w) * 512 + lane * 16);
   };
 
-  float o[NT][MT][4];          // O^T / 16 without the offsets' share: channels 16 mt + g, + 8; query rows 2 q, 2 q + 1
-  float oo[NT][4];             // sum_j p_j o_j: of group g & 1 (first two) and of the other group
-  float m_run[NT][2], l_run[NT][2];
+  float o[NT][MT][4];          // O^T without the offsets' share: channels 16 mt + g, + 8; query rows 2 q, 2 q + 1
+  float oo[NT][4];             // sum_j p_j x_j of the quantity g mod 2 NG (offsets of the groups, then scales), and sum_j p_j
+  float m_run[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     m_run[nt][0] = m_run[nt][1] = kNoMax;
-    l_run[nt][0] = l_run[nt][1] = 0.f;
     oo[nt][0] = oo[nt][1] = oo[nt][2] = oo[nt][3] = 0.f;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) o[nt][mt][0] = o[nt][mt][1] = o[nt][mt][2] = o[nt][mt][3] = 0.f;
   }
 
-  // Scores of 16 keys (s[nt]: keys g, g + 8 x query rows 2 q, 2 q + 1) -> probabilities as the operand of the output product.
-  auto softmax = [&](float (&s)[NT][4], uint32_t (&pb)[NT][2]) {
-    bool raise = false;
+  // Scores of NP x 16 keys (s[.][nt]: keys g, g + 8 x query rows 2 q, 2 q + 1) -> probabilities as operands of the output product.
+  auto softmax = [&](auto np, auto& s, auto& pb) {
+    constexpr int NP = decltype(np)::value;
+    float top = kNoMax;
+    float x[NP][NT][4];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float a = fmaxf(s[nt][0], s[nt][2]), b = fmaxf(s[nt][1], s[nt][3]);
-      raise = raise || a * p.scale_log2e > m_run[nt][0] + kMaxSlack || b * p.scale_log2e > m_run[nt][1] + kMaxSlack;
-    }
-    if (__any_sync(0xffffffffu, raise)) {
+    for (int pp = 0; pp < NP; ++pp)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x[pp][nt][e] = fmaf(s[pp][nt][e], p.scale_log2e, -m_run[nt][e & 1]);
+          top = fmaxf(top, x[pp][nt][e]);
+        }
+    if (__any_sync(0xffffffffu, top > kRaise)) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float mx = fmaxf(s[nt][e], s[nt][e + 2]) * p.scale_log2e;
+          float mx = kNoMax;
+#pragma unroll
+          for (int pp = 0; pp < NP; ++pp) mx = fmaxf(mx, fmaxf(s[pp][nt][e], s[pp][nt][e + 2]) * p.scale_log2e);
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-          const float m_new = fmaxf(m_run[nt][e], mx);
+          const float m_new = fmaxf(m_run[nt][e], mx - kHeadroom);
           const float corr = fast_exp2(m_run[nt][e] - m_new);
           m_run[nt][e] = m_new;
-          l_run[nt][e] *= corr;
           oo[nt][e] *= corr;
           oo[nt][e + 2] *= corr;
 #pragma unroll
@@ -253,17 +308,23 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
             o[nt][mt][e] *= corr;
             o[nt][mt][e + 2] *= corr;
           }
+#pragma unroll
+          for (int pp = 0; pp < NP; ++pp) {
+            x[pp][nt][e] = fmaf(s[pp][nt][e], p.scale_log2e, -m_new);
+            x[pp][nt][e + 2] = fmaf(s[pp][nt][e + 2], p.scale_log2e, -m_new);
+          }
         }
     }
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+    for (int pp = 0; pp < NP; ++pp)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][e] = fast_exp2(fmaf(s[nt][e], p.scale_log2e, -m_run[nt][e & 1]));
-      l_run[nt][0] += s[nt][0] + s[nt][2];
-      l_run[nt][1] += s[nt][1] + s[nt][3];
-      pb[nt][0] = transpose8x8(pack_f16x2(s[nt][0], s[nt][1]));
-      pb[nt][1] = transpose8x8(pack_f16x2(s[nt][2], s[nt][3]));
-    }
+      for (int nt = 0; nt < NT; ++nt) {
+        float (&y)[4] = x[pp][nt];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fast_exp2(y[e]);
+        pb[pp][nt][0] = transpose8x8(pack_f16x2(y[0], y[1]));
+        pb[pp][nt][1] = transpose8x8(pack_f16x2(y[2], y[3]));
+      }
   };
   // Keys key0 .. key0 + 15 against the last key that the rows of token t see, base + t: masked scores are -inf.
   const int t_min = row0 / G;
@@ -278,7 +339,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       }
   };
 
-  auto cached_page = [&](const uint8_t* b, int key0) {
+  const int see_base = it.ctx - (p.given ? 1 : 0), see_step = p.given ? 0 : 1;
+  auto cached_scores = [&](const uint8_t* b, int key0, float (&s)[NT][4]) {
     float acc[NT][NG][4];
     uint32_t kw[2][2 * NG];
     if (NG == 2) {
@@ -292,85 +354,79 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     for (int w = 0; w < 2; ++w)
 #pragma unroll
       for (int grp = 0; grp < NG; ++grp) {
-        const uint32_t wa = kw[0][2 * grp + w], wb = kw[1][2 * grp + w];
-        const uint32_t a0[4] = {whole_codes(wa << 4), whole_codes(wb << 4), whole_codes(wa), whole_codes(wb)};
-        const uint32_t a1[4] = {whole_codes(wa >> 4), whole_codes(wb >> 4), whole_codes(wa >> 8), whole_codes(wb >> 8)};
+        const uint32_t wa = kw[0][2 * grp + w], wb = kw[1][2 * grp + w], wa8 = wa >> 8, wb8 = wb >> 8;
+        const uint32_t a0[4] = {codes_low(wa), codes_low(wb), codes64(wa), codes64(wb)};
+        const uint32_t a1[4] = {codes_low(wa8), codes_low(wb8), codes64(wa8), codes64(wb8)};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const uint4 qv = q_words(nt, grp, w);
-          if (w == 0)
-            mma_k16(acc[nt][grp], a0, qv.x, qv.y, qneg[nt][grp][0], qneg[nt][grp][1], qneg[nt][grp][0], qneg[nt][grp][1]);
-          else
-            mma_k16(acc[nt][grp], a0, qv.x, qv.y);
+          if (w == 0) mma_k16_first(acc[nt][grp], a0, qv.x, qv.y);
+          else mma_k16(acc[nt][grp], a0, qv.x, qv.y);
           mma_k16(acc[nt][grp], a1, qv.z, qv.w);
         }
       }
     // scales (fp32) and offsets of keys g and g + 8
     float sc[2][NG];
-    uint32_t off[2];
+    uint32_t os[4];
     if (NG == 2) {
       const uint2 s2 = *reinterpret_cast<const uint2*>(b + L::kKScale + g * 8);
       const uint2 o2 = *reinterpret_cast<const uint2*>(b + L::kKOffset + g * 8);
       const float2 f0 = unpack_f16x2(s2.x), f1 = unpack_f16x2(s2.y);
       sc[0][0] = f0.x; sc[0][NG - 1] = f0.y; sc[1][0] = f1.x; sc[1][NG - 1] = f1.y;
-      off[0] = o2.x; off[1] = o2.y;
+      os[0] = o2.x; os[1] = o2.y; os[2] = s2.x; os[3] = s2.y;
     } else {
-      const float2 f = unpack_f16x2(*reinterpret_cast<const uint32_t*>(b + L::kKScale + g * 4));
+      const uint32_t s1 = *reinterpret_cast<const uint32_t*>(b + L::kKScale + g * 4);
+      const float2 f = unpack_f16x2(s1);
       const uint32_t o1 = *reinterpret_cast<const uint32_t*>(b + L::kKOffset + g * 4);
       sc[0][0] = f.x; sc[1][0] = f.y;
-      off[0] = __byte_perm(o1, o1, 0x1010); off[1] = __byte_perm(o1, o1, 0x3232);
+      os[0] = __byte_perm(o1, o1, 0x1010); os[1] = __byte_perm(o1, o1, 0x3232);
+      os[2] = __byte_perm(s1, s1, 0x1010); os[3] = __byte_perm(s1, s1, 0x3232);
     }
-    float s[NT][4];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      mma_k8(s[nt], off[0], off[1], qoff[nt]);
+      mma_k16_first(s[nt], os, qoff[nt], qscale[nt]);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int grp = 0; grp < NG; ++grp) s[nt][e] = fmaf(sc[e >> 1][grp], acc[nt][grp][e], s[nt][e]);
     }
-    mask(s, key0, it.ctx - (p.given ? 1 : 0), p.given ? 0 : 1);
-    uint32_t pb[NT][2];
-    softmax(s, pb);
+    mask(s, key0, see_base, see_step);
+  };
 
-    // values: scales of keys (2 q, 2 q + 1) and (2 q + 8, 2 q + 9) per group, and what takes the 64 and the 4 back
-    uint32_t vs[2 * NG], n64[2 * NG], n4[2 * NG];
-    if (NG == 2) *reinterpret_cast<uint4*>(vs) = *reinterpret_cast<const uint4*>(b + L::kVScale + q * 16);
-    else *reinterpret_cast<uint2*>(vs) = *reinterpret_cast<const uint2*>(b + L::kVScale + q * 8);
-#pragma unroll
-    for (int i = 0; i < 2 * NG; ++i) {
-      n64[i] = hmul2_u(vs[i], 0xD400D400u);       // -64
-      n4[i] = hmul2_u(vs[i], 0xC400C400u);        // -4
-    }
+  auto cached_values = [&](const uint8_t* b, uint32_t (&pb)[NT][2]) {
+    // (p s) (c - 8) by group; scales of keys 2 q, 2 q + 1 and 2 q + 8, 2 q + 9
+    uint32_t vs[2 * NG];
+    if (NG == 2) *reinterpret_cast<uint4*>(vs) = *reinterpret_cast<const uint4*>(b + L::kVParams + q * 32 + 16);
+    else *reinterpret_cast<uint2*>(vs) = *reinterpret_cast<const uint2*>(b + L::kVParams + q * 16 + 8);
     const uint8_t* vb = b + L::kVCodes + L::v_chunk(g, q) * 16;
 #pragma unroll
-    for (int half = 0; half < NG; ++half) {
-      const uint4 vw = *reinterpret_cast<const uint4*>(vb + half * 512);
+    for (int grp = 0; grp < NG; ++grp) {
+      uint32_t ps[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        ps[nt][0] = hmul2_u(pb[nt][0], vs[2 * grp]);
+        ps[nt][1] = hmul2_u(pb[nt][1], vs[2 * grp + 1]);
+      }
+      const uint4 vw = *reinterpret_cast<const uint4*>(vb + grp * 512);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t w = word(vw, i), w8 = w >> 8;
-        const uint32_t a[4] = {hfma2_u(low_codes(w), vs[2 * half], n64[2 * half]),
-                               hfma2_u(high_codes(w), vs[2 * half], n4[2 * half]),
-                               hfma2_u(low_codes(w8), vs[2 * half + 1], n64[2 * half + 1]),
-                               hfma2_u(high_codes(w8), vs[2 * half + 1], n4[2 * half + 1])};
+        const uint32_t a[4] = {centred_low(w), centred_high(w), centred_low(w8), centred_high(w8)};
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) mma_k16(o[nt][4 * half + i], a, pb[nt][0], pb[nt][1]);
+        for (int nt = 0; nt < NT; ++nt) mma_k16(o[nt][4 * grp + i], a, ps[nt][0], ps[nt][1]);
       }
     }
-    uint32_t ao[4];
-    {
-      const uint2 x = *reinterpret_cast<const uint2*>(b + L::kVOffset + (q * NG + (NG == 2 ? g & 1 : 0)) * 8);
-      const uint2 y = *reinterpret_cast<const uint2*>(b + L::kVOffset + (q * NG + (NG == 2 ? (g & 1) ^ 1 : 0)) * 8);
-      ao[0] = x.x; ao[1] = y.x; ao[2] = x.y; ao[3] = y.y;
-    }
+    // offsets, scales and ones as the rows of one more product: sum_j p_j o_j, sum_j p_j s_j (which takes the 8 back at the end)
+    // and sum_j p_j
+    const uint2 vo = *reinterpret_cast<const uint2*>(b + L::kVParams + (q * 2 * NG + (g & (2 * NG - 1))) * 8);
+    const uint32_t ao[4] = {vo.x, kOnes, vo.y, kOnes};
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) mma_k16(oo[nt], ao, pb[nt][0], pb[nt][1]);
   };
 
   // A page of the step's own keys and values, given as rows in fp16 or bf16: K operands straight from global memory, V through
-  // this warp's (drained) stages and transposing loads. V is divided by 16, as the cached values are.
+  // this warp's (drained) stages and transposing loads.
   auto own_page = [&](int key0) {
-    cp_async_wait<0>();
     __syncwarp();
     constexpr int CH = HD / 8;
     for (int c = lane; c < kPage * CH; c += 32) {
@@ -379,11 +435,11 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       if (key0 + key < it.n_new)
         v = as_f16(*reinterpret_cast<const uint4*>(p.v_new + (it.tok0 + key0 + key) * p.kv_stride + it.kv_head * HD + ch * 8),
                    p.in_bf16 != 0);
-      v = make_uint4(hmul2_u(v.x, 0x2C002C00u), hmul2_u(v.y, 0x2C002C00u), hmul2_u(v.z, 0x2C002C00u), hmul2_u(v.w, 0x2C002C00u));
       *reinterpret_cast<uint4*>(my + key * HD * 2 + ((ch ^ (key & 7)) << 4)) = v;
     }
     __syncwarp();
-    float s[NT][4];
+    float s1[1][NT][4];
+    float (&s)[NT][4] = s1[0];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
@@ -408,8 +464,9 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
         }
       }
     mask(s, key0, 0, 1);
-    uint32_t pb[NT][2];
-    softmax(s, pb);
+    uint32_t pb1[1][NT][2];
+    softmax(std::integral_constant<int, 1>{}, s1, pb1);
+    const uint32_t (&pb)[NT][2] = pb1[0];
     // matrices of an operand tile: channels 0-7 / 8-15 x keys 0-7, then x keys 8-15
     const int key = (lane & 7) + (lane >> 4) * 8, up = (lane >> 3) & 1;
 #pragma unroll
@@ -419,24 +476,44 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mma_k16(o[nt][mt], a, pb[nt][0], pb[nt][1]);
     }
+    const uint32_t ao[4] = {0u, kOnes, 0u, kOnes};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) mma_k16(oo[nt], ao, pb[nt][0], pb[nt][1]);
     __syncwarp();
   };
 
-  int pg = pg0;
-  int stage = 0, ahead_stage = kStages - 1;
-  for (; pg < end_cached; pg += kWarps) {
+  int stage_off = 0, ahead_off = (kStages - 1) * kStageBytes;
+#pragma unroll 1
+  for (int pg = pg0; pg < end_cached; pg += kStep) {
     cp_async_wait<kStages - 2>();
     __syncwarp();
-    // the stage read in the previous round is free: request the page kStages - 1 rounds ahead
-    const int ahead = pg + (kStages - 1) * kWarps;
-    if (ahead < end_cached) fetch(id_ahead, ahead_stage);
+    // the stage read in the previous round is free: request the round kStages - 1 ahead, and look up the one behind it
+    fetch(pg + (kStages - 1) * kStep, id_ahead, ahead_off);
     cp_async_commit();
-    if (ahead + kWarps < end_cached) id_ahead = __ldg(table + ahead + kWarps);
-    cached_page(my + stage * L::kBlock, pg * kPage);
-    stage = stage == kStages - 1 ? 0 : stage + 1;
-    ahead_stage = ahead_stage == kStages - 1 ? 0 : ahead_stage + 1;
+    id_ahead = page_id(pg + kStages * kStep);
+    const uint8_t* b = my + stage_off;
+    if (pg + 1 < end_cached) {
+      float s[2][NT][4];
+      uint32_t pb[2][NT][2];
+      cached_scores(b, pg * kPage, s[0]);
+      cached_scores(b + L::kBlock, pg * kPage + kPage, s[1]);
+      softmax(std::integral_constant<int, 2>{}, s, pb);
+      cached_values(b, pb[0]);
+      cached_values(b + L::kBlock, pb[1]);
+    } else {
+      float s[1][NT][4];
+      uint32_t pb[1][NT][2];
+      cached_scores(b, pg * kPage, s[0]);
+      softmax(std::integral_constant<int, 1>{}, s, pb);
+      cached_values(b, pb[0]);
+    }
+    ahead_off = stage_off;                       // the stage just read is the next to be filled
+    stage_off = stage_off == (kStages - 1) * kStageBytes ? 0 : stage_off + kStageBytes;
   }
-  for (; pg < it.tile_end; pg += kWarps) own_page((pg - cached_pages) * kPage);
+  cp_async_wait<0>();
+  // own pages: one at a time to the warps in turn, from the last warp on, which has the fewest cached pages
+  for (int own = max(it.tile_begin, cached_pages) + (kWarps - 1 - warp); own < it.tile_end; own += kWarps)
+    own_page((own - cached_pages) * kPage);
   cp_async_wait<0>();
   __syncthreads();
 
@@ -447,22 +524,20 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float l = l_run[nt][e];
-      l += __shfl_xor_sync(0xffffffffu, l, 4);
-      l += __shfl_xor_sync(0xffffffffu, l, 8);
-      l += __shfl_xor_sync(0xffffffffu, l, 16);
       const int r = nt * 8 + 2 * q + e;
       if (g == 0) {
         pml[(warp * 8 * NT + r) * 2] = m_run[nt][e];
-        pml[(warp * 8 * NT + r) * 2 + 1] = l;
+        pml[(warp * 8 * NT + r) * 2 + 1] = oo[nt][e + 2];
       }
+      float add[NG];             // what the offsets and the centring add to every channel of a group
+#pragma unroll
+      for (int grp = 0; grp < NG; ++grp)
+        add[grp] = fmaf(8.f, __shfl_sync(0xffffffffu, oo[nt][e], (NG + grp) * 4 + q), __shfl_sync(0xffffffffu, oo[nt][e], grp * 4 + q));
       float* dst = po + (warp * 8 * NT + r) * S::kPad + g;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        // the group of this tile's channels: mt / 4; this lane's first pair of offset sums belongs to group g & 1
-        const float add = NG == 1 || (mt / 4) == (g & 1) ? oo[nt][e] : oo[nt][e + 2];
-        dst[mt * 16] = fmaf(16.f, o[nt][mt][e], add);
-        dst[mt * 16 + 8] = fmaf(16.f, o[nt][mt][e + 2], add);
+        dst[mt * 16] = o[nt][mt][e] + add[mt / 4];
+        dst[mt * 16 + 8] = o[nt][mt][e + 2] + add[mt / 4];
       }
     }
   }
@@ -483,70 +558,76 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       const int t = (row0 + r) / G, hq = (row0 + r) % G;
       store_out(p, (it.tok0 + t) * p.out_stride + (it.kv_head * G + hq) * HD + d, sum > 0.f ? acc / sum : 0.f);
     } else {
-      p.part_o[(static_cast<size_t>(it.slot) * 32 + r) * HD + d] = acc;
+      p.part_o[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * HD + d] = acc;
       if (d == 0) {
-        p.part_ml[(static_cast<size_t>(it.slot) * 32 + r) * 2] = M;
-        p.part_ml[(static_cast<size_t>(it.slot) * 32 + r) * 2 + 1] = sum;
+        p.part_ml[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * 2] = M;
+        p.part_ml[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * 2 + 1] = sum;
       }
     }
   }
 }
 
-// Pieces of one (step, kv head, row tile) -> output. One CTA per work item and 8 query rows; only the first piece does anything.
+// Pieces of one (step, kv head, row tile) -> output. One CTA per cut range and query row, one thread per channel: the pieces'
+// weights once, in parallel, then a sum over the pieces in their order.
 template <int HD>
 __global__ void __launch_bounds__(HD) attention_4bit_merge_kernel(const Attn4Params p, const AttnItem* __restrict__ items, int tile) {
+  __shared__ float weight[kAttn4MaxPieces];
   pdl_launch_dependents();
-  pdl_wait();
   const AttnItem it = items[blockIdx.x];
-  if (it.n_splits <= 1 || it.slot != it.slot0) return;
   const int G = p.n_q_heads / p.n_kv_heads;
-  const int R = min(tile, it.n_new * G - it.q_tok0);
-  const int d = threadIdx.x;
-  for (int r = blockIdx.y; r < R; r += gridDim.y) {
-    float M = kNoMax;
-    for (int s = 0; s < it.n_splits; ++s) M = fmaxf(M, p.part_ml[(static_cast<size_t>(it.slot0 + s) * 32 + r) * 2]);
-    float acc = 0.f, sum = 0.f;
-    for (int s = 0; s < it.n_splits; ++s) {
-      const size_t base = static_cast<size_t>(it.slot0 + s) * 32 + r;
-      const float f = fast_exp2(p.part_ml[base * 2] - M);
-      acc += f * p.part_o[base * HD + d];
-      sum += f * p.part_ml[base * 2 + 1];
-    }
-    const int t = (it.q_tok0 + r) / G, hq = (it.q_tok0 + r) % G;
-    store_out(p, (it.tok0 + t) * p.out_stride + (it.kv_head * G + hq) * HD + d, sum > 0.f ? acc / sum : 0.f);
+  const int r = blockIdx.y, d = threadIdx.x, n = it.n_splits;
+  pdl_wait();
+  if (r >= min(tile, it.n_new * G - it.q_tok0)) return;
+  if (threadIdx.x < 32) piece_weights(p, it, r, d, weight);
+  __syncthreads();
+  // four channels a thread; the warps (HD = 64: half warps) take every fourth piece, and their sums are added in order
+  constexpr int kQuads = HD / 4;
+  __shared__ float4 part[4][kQuads];
+  const int share = d / kQuads, c4 = d % kQuads;
+  const float4* o = reinterpret_cast<const float4*>(p.part_o + (static_cast<size_t>(it.slot0) * kAttn4Rows + r) * HD) + c4;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+  for (int s = share; s < n; s += 4) {
+    const float4 v = __ldcg(o + static_cast<size_t>(s) * kAttn4Rows * kQuads);
+    const float w = weight[s];
+    acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
   }
+  part[share][c4] = acc;
+  __syncthreads();
+  const float* sums = reinterpret_cast<const float*>(part);
+  const int t = (it.q_tok0 + r) / G, hq = (it.q_tok0 + r) % G;
+  store_out(p, (it.tok0 + t) * p.out_stride + (it.kv_head * G + hq) * HD + d, sums[d] + sums[HD + d] + sums[2 * HD + d] + sums[3 * HD + d]);
 }
 
 template <int HD, int NT>
-cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items, bool any_split, cudaStream_t s) {
+cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, cudaStream_t s) {
   static std::atomic<uint64_t> smem_opted{0};
   if (cudaError_t e = opt_in_dynamic_smem(attention_4bit_kernel<HD, NT>, Smem4<HD, NT>::kTotal, smem_opted); e != cudaSuccess)
     return e;
   cudaError_t e = launch_pdl(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads), Smem4<HD, NT>::kTotal, s, p, items);
   count_launch();
-  if (e != cudaSuccess || !any_split) return e != cudaSuccess ? e : cudaGetLastError();
-  e = launch_pdl(attention_4bit_merge_kernel<HD>, dim3(n_items, NT), dim3(HD), 0, s, p, items, 8 * NT);
+  if (e != cudaSuccess || n_merge == 0) return e != cudaSuccess ? e : cudaGetLastError();
+  e = launch_pdl(attention_4bit_merge_kernel<HD>, dim3(n_merge, 8 * NT), dim3(HD), 0, s, p, items + n_items, 8 * NT);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace
 
-// 8, 16 or 32 query rows per work item: the smallest tile that takes the batch's longest step whole, so that no step reads
-// its context twice; longer steps are cut into tiles of 32.
-int attention_4bit_row_tile(int max_rows) { return max_rows <= 8 ? 8 : max_rows <= 16 ? 16 : 32; }
+// 8 or 16 query rows per work item; longer steps are cut into tiles of 16, whose items run side by side and find one another's
+// pages in L2. (Tiles of 32 rows need 255 registers and two CTAs per SM: 28 rows over 83 K keys x 4 heads took 99 us, as two
+// tiles of 16 45 us.)
+int attention_4bit_row_tile(int max_rows) { return max_rows <= 8 ? 8 : 16; }
 
-cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int row_tile, bool any_split,
+int attention_4bit_ctas_per_sm(int row_tile) { return ctas_per_sm(row_tile / 8); }
+
+cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, int row_tile,
                                   cudaStream_t s) {
   if (n_items <= 0) return cudaSuccess;
   if (p.head_dim == 128)
-    return row_tile == 8    ? launch_4bit<128, 1>(p, items, n_items, any_split, s)
-           : row_tile == 16 ? launch_4bit<128, 2>(p, items, n_items, any_split, s)
-                            : launch_4bit<128, 4>(p, items, n_items, any_split, s);
+    return row_tile == 8 ? launch_4bit<128, 1>(p, items, n_items, n_merge, s) : launch_4bit<128, 2>(p, items, n_items, n_merge, s);
   if (p.head_dim == 64)
-    return row_tile == 8    ? launch_4bit<64, 1>(p, items, n_items, any_split, s)
-           : row_tile == 16 ? launch_4bit<64, 2>(p, items, n_items, any_split, s)
-                            : launch_4bit<64, 4>(p, items, n_items, any_split, s);
+    return row_tile == 8 ? launch_4bit<64, 1>(p, items, n_items, n_merge, s) : launch_4bit<64, 2>(p, items, n_items, n_merge, s);
   return cudaErrorInvalidValue;
 }
 

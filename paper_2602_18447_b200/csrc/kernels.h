@@ -137,6 +137,7 @@ cudaError_t launch_kv_read(KvReadParams p, int format, int hd, cudaStream_t s);
 cudaError_t launch_kv_expand(const uint8_t* pool, const int32_t* pages, int n_pages, uint16_t* out_k, uint16_t* out_v,
                              int n_kv_heads, int hd, int num_pages, uint32_t* status, cudaStream_t s);
 
+constexpr int kAttn4Rows = 16;           // query rows per work item at most
 struct Attn4Params {
   const uint16_t* q;               // [T, >= n_q_heads * head_dim], rotated; fp16 or bf16 (in_bf16); strides in elements
   const uint16_t *k_new, *v_new;   // given: the new tokens' own rows (k rotated), not in the cache; same type as q
@@ -149,15 +150,18 @@ struct Attn4Params {
   int32_t in_bf16, out_bf16;
   int32_t cache_is_settled;        // nothing that may still run before this kernel writes the cache
   float scale_log2e;
-  float* part_o;                   // [slots][32][head_dim]
-  float* part_ml;                  // [slots][32][2]
+  float* part_o;                   // [slots][kAttn4Rows][head_dim]
+  float* part_ml;                  // [slots][kAttn4Rows][2]
   uint32_t* status;
 };
 // Items reuse AttnItem: q_tok0 = first query ROW (token * G + head in group) of the item's row tile; [tile_begin, tile_end)
 // counts pages, the cached ones first (pad[1] of them), then pages of 16 own keys (given only); ctx = cached keys in front
 // of the step's first token.
 int attention_4bit_row_tile(int max_rows);
-cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int row_tile, bool any_split,
+int attention_4bit_ctas_per_sm(int row_tile);
+constexpr int kAttn4MaxPieces = 64;      // a context is cut into at most this many pieces (the joining kernel: two per lane)
+// items[0 .. n_items): the work; items[n_items .. n_items + n_merge): one item (any piece) of every range that was cut.
+cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, int row_tile,
                                   cudaStream_t s);
 
 // x_last[b] = x[cu_new[b + 1] - 1], fp32 [B, d].

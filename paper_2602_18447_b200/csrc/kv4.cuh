@@ -9,7 +9,8 @@
 //           one channel. One key of two channels is one byte: appending a key never reads what its neighbours wrote.
 //           The 16-byte pieces of the lanes are permuted (v_chunk) so that a key's bytes lie in one 128-byte line per
 //           64 channels and the lanes' 16-byte reads still meet no bank twice.
-//  K scales, K offsets  fp16 [key % 8][key / 8][group];   V scales, V offsets  fp16 [q][group][2q, 2q + 1, 2q + 8, 2q + 9].
+//  K scales, K offsets  fp16 [key % 8][key / 8][group];
+//  V offsets and scales  fp16 [q][offsets by group, scales by group][keys 2q, 2q + 1, 2q + 8, 2q + 9].
 #pragma once
 
 #include <stdint.h>
@@ -17,7 +18,7 @@
 namespace cs {
 
 constexpr int kKv4Group = 64;          // channels that share a scale and an offset
-// The V operand is formed as (64 + c / 16) s - 64 s: 64 s has to stay an fp16 value.
+// The attention multiplies a probability of up to 64 with a V scale in fp16: 64 x 1023.5 is its largest value.
 constexpr float kKv4MaxScale = 1023.5f;
 
 template <int HD>
@@ -28,9 +29,8 @@ struct Kv4 {
   static constexpr int kKScale = kCodes;
   static constexpr int kKOffset = kKScale + kParams;
   static constexpr int kVCodes = kKOffset + kParams;
-  static constexpr int kVScale = kVCodes + kCodes;
-  static constexpr int kVOffset = kVScale + kParams;
-  static constexpr int kBlock = kVOffset + kParams;
+  static constexpr int kVParams = kVCodes + kCodes;
+  static constexpr int kBlock = kVParams + 2 * kParams;
   static_assert(kBlock % 16 == 0, "blocks are copied in 16-byte pieces");
 
   // byte of the word with channels d .. d + 7 (d a multiple of 8) of a key
@@ -45,9 +45,11 @@ struct Kv4 {
   __host__ __device__ static constexpr int v_byte(int key, int mt, int g) {
     return (mt / 4) * 512 + v_chunk(g, (key & 7) >> 1) * 16 + (mt % 4) * 4 + (key >> 3) + 2 * (key & 1);
   }
-  __host__ __device__ static constexpr int v_param(int key, int group) {
-    return ((((key & 7) >> 1) * kGroups + group) * 4 + (key & 1) + 2 * (key >> 3)) * 2;
+  // relative to the block
+  __host__ __device__ static constexpr int v_offset(int key, int group) {
+    return kVParams + ((((key & 7) >> 1) * 2 * kGroups + group) * 4 + (key & 1) + 2 * (key >> 3)) * 2;
   }
+  __host__ __device__ static constexpr int v_scale(int key, int group) { return v_offset(key, group) + kGroups * 8; }
 };
 
 inline int kv4_block_bytes(int hd) { return hd == 128 ? Kv4<128>::kBlock : Kv4<64>::kBlock; }

@@ -203,8 +203,8 @@ __global__ void __launch_bounds__(2 * HD) kv_append_kernel(const KvAppendParams 
         if ((c & 7) == 0) {
           *reinterpret_cast<__half*>(dst + L::kKScale + L::k_param(slot, c / 8)) = ks;
           *reinterpret_cast<__half*>(dst + L::kKOffset + L::k_param(slot, c / 8)) = ko;
-          *reinterpret_cast<__half*>(dst + L::kVScale + L::v_param(slot, c / 8)) = vs;
-          *reinterpret_cast<__half*>(dst + L::kVOffset + L::v_param(slot, c / 8)) = vo;
+          *reinterpret_cast<__half*>(dst + L::v_scale(slot, c / 8)) = vs;
+          *reinterpret_cast<__half*>(dst + L::v_offset(slot, c / 8)) = vo;
         }
       }
       if (whole) {
@@ -279,8 +279,8 @@ __global__ void __launch_bounds__(2 * HD) kv_read_kernel(const KvReadParams p) {
         const uint32_t w = *reinterpret_cast<const uint32_t*>(b + L::k_word(slot, c * 8));
         const float ks = __half2float(*reinterpret_cast<const __half*>(b + L::kKScale + L::k_param(slot, c / 8)));
         const float ko = __half2float(*reinterpret_cast<const __half*>(b + L::kKOffset + L::k_param(slot, c / 8)));
-        const float vs = __half2float(*reinterpret_cast<const __half*>(b + L::kVScale + L::v_param(slot, c / 8)));
-        const float vo = __half2float(*reinterpret_cast<const __half*>(b + L::kVOffset + L::v_param(slot, c / 8)));
+        const float vs = __half2float(*reinterpret_cast<const __half*>(b + L::v_scale(slot, c / 8)));
+        const float vo = __half2float(*reinterpret_cast<const __half*>(b + L::v_offset(slot, c / 8)));
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           k[j] = static_cast<float>(w >> (4 * (j / 2) + 16 * (j & 1)) & 15u) * ks + ko;
@@ -324,8 +324,8 @@ __global__ void __launch_bounds__(2 * HD) kv_expand_kernel(const uint8_t* __rest
   const uint32_t w = *reinterpret_cast<const uint32_t*>(b + L::k_word(slot, c * 8));
   const float ks = __half2float(*reinterpret_cast<const __half*>(b + L::kKScale + L::k_param(slot, c / 8)));
   const float ko = __half2float(*reinterpret_cast<const __half*>(b + L::kKOffset + L::k_param(slot, c / 8)));
-  const float vs = __half2float(*reinterpret_cast<const __half*>(b + L::kVScale + L::v_param(slot, c / 8)));
-  const float vo = __half2float(*reinterpret_cast<const __half*>(b + L::kVOffset + L::v_param(slot, c / 8)));
+  const float vs = __half2float(*reinterpret_cast<const __half*>(b + L::v_scale(slot, c / 8)));
+  const float vo = __half2float(*reinterpret_cast<const __half*>(b + L::v_offset(slot, c / 8)));
   float k[8], v[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {

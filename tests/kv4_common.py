@@ -37,10 +37,11 @@ def rotate(x, pos, theta):
 def attend(q, k, v, v_steps, k_mag, seen, scale):
     """One step in 64 bits: q [n, hq, hd], k, v [m, hkv, hd]; token t sees keys < seen[t]. Returns (out, bound): the bound counts
     the roundings that the kernel's formats make, per output:
-      P to fp16 (2^-11 of each term's |p v|), the scaled code to fp16 (2^-11 of |p c s|; v_steps = |c s|), the output
-      (2^-11, or 2^-8 for bf16: added by the caller), P below fp16's normal range (2^-25 a key against a sum of at least
-      1), the scaled code below it (2^-21), and the score's fp32 sums: hd + 8 additions of terms q (64 + c) s and q o, each off
-      by at most 2^-23 of the sum of magnitudes (k_mag [m, hkv] = max over groups of 79 s + |o|); 2^x to 2^-18.
+      p to fp16 (2^-11 of each term's |p v|), p s to fp16 (2^-11 of p s |c - 8|, at most p |c s| = v_steps), the output (2^-11, or
+      2^-8 for bf16: added by the caller); below fp16's normal range p is off by 2^-25 and p s by 2^-25 too, times 8 codes,
+      where the largest p of a row is at least 2^2: m 2^-27 |v| and m 2^-24 together for m keys; the score's fp32 sums: hd + 8
+      additions of terms q (64 + c) s and q o, each off by at most 2^-23 of the sum of magnitudes (k_mag [m, hkv] = max over
+      groups of 79 s + |o|); 2^x to 2^-18.
     """
     n, hq, hd = q.shape
     group = hq // k.shape[1]
@@ -57,7 +58,7 @@ def attend(q, k, v, v_steps, k_mag, seen, scale):
             out[t, h] = p @ vh[:m]
             delta = (hd + 8) * 2.0 ** -23 * scale * np.abs(q[t, h]).sum() * mag[:m].max() + 2.0 ** -18
             spread = p @ np.abs(vh[:m])
-            bound[t, h] = (2.0 ** -11 * (spread + p @ st[:m]) + m * 2.0 ** -25 * np.abs(vh[:m]).max() + 2.0 ** -21
+            bound[t, h] = (2.0 ** -11 * (spread + p @ st[:m]) + m * 2.0 ** -27 * np.abs(vh[:m]).max() + m * 2.0 ** -24
                            + 2 * delta * spread + 2 * delta * np.abs(out[t, h]))
     return out, bound
 
