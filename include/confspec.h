@@ -152,9 +152,9 @@ int cs_kv_alloc_8bit(const cs_model* model, int num_pages, int page_size, int ma
  *   pool bytes = n_layers * num_pages * n_kv_heads * 18 * head_dim, library-owned.
  * Every call takes it: cs_verify_steps, cs_verify_cascade, cs_prefill and cs_append_accepted (steps of any length), cs_kv_fill
  * (bf16 rows, quantised on the way in), and the calls on a plan below. Within a pass the new tokens see one another's keys and
- * values as computed (fp16); what is appended is quantised. Steps of more than 32 query rows per kv head (tokens x heads in the
- * group) have their contexts expanded to fp16 layer by layer, into a scratch pool that the cache allocates at the first such
- * step and keeps: 4 * num_pages * n_kv_heads * 16 * head_dim bytes.
+ * values as computed (fp16); what is appended is quantised. Steps of more than 96 query rows per kv head (tokens x heads in the
+ * group) have their contexts expanded to fp16 layer by layer, into a workspace of the model (or of the plan) that holds one
+ * layer of the batch's contexts: 64 * n_kv_heads * head_dim bytes a page.
  */
 int cs_kv_alloc_4bit(const cs_model* model, int num_pages, int page_size, int max_seqs, int max_pages_per_seq,
                      cs_kv** out);
@@ -239,8 +239,9 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
  *   scale              0: 1 / sqrt(head_dim); else > 0 and finite.
  * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; queries up to 2047 in magnitude),
- * sums and the softmax are fp32, probabilities and dequantised values are rounded to fp16 once. Any number of new tokens; it is
- * made for up to 32 query rows per kv head (longer steps read the cache once per 32 rows). Deterministic.
+ * sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number of new tokens:
+ * up to 96 query rows per kv head read the 4-bit pages directly; a batch with a longer step has its rows and contexts put together
+ * as fp16 in the plan (values rounded to fp16 once) for the pass's tensor-core attention. Deterministic.
  */
 int cs_attention_4bit(cs_plan* plan, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new,
                       const uint16_t* v_new, int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype, float scale,

@@ -146,7 +146,8 @@ def _dev_ptr(t) -> Optional[int]:
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        # the current stream's handle without the Stream object around it (0.1 us instead of 3)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

@@ -115,6 +115,7 @@ struct cs_model {
   CUtensorMap tm_lm;
   // workspace
   DevBuf x, x_last, a, qkv, attn_o, hmlp, rope, h_last, lm_part, vlogits, logits, lse, attn_part_o, attn_part_ml, attn_counters;
+  DevBuf expanded;              // a 4-bit cache's pages of one layer in the 16-bit layout, for steps of many query rows
   uint32_t* status = nullptr;
   // fixed order of the residual projections' additions (bit-identical passes); see TurnOrder
   uint32_t* turn_flags = nullptr;
@@ -149,9 +150,6 @@ struct cs_kv {
   cudaEvent_t upload_ev = nullptr;
   bool upload_pending = false;
   DevBuf fill_tmp;
-  DevBuf expanded;            // 4-bit cache: one layer's pages in the 16-bit layout, for steps of many tokens
-  CUtensorMap tm_expanded;
-  void* tm_expanded_of = nullptr;
   size_t layer4_bytes() const {
     return static_cast<size_t>(num_pages) * model->d.n_kv_heads * kv4_block_bytes(model->d.head_dim);
   }
@@ -167,6 +165,12 @@ struct cs_plan {
   std::vector<int32_t> seqs, lens, ctx;
   Staging stg;
   DevBuf rope, part_o, part_ml;
+  // steps of many query rows: expanded context pages, the fused fp16 matrix and output of the tensor-core attention, its counters
+  bool expand = false;
+  int n_pages = 0, x_width = 0;
+  size_t off_pages = 0, off_xtable = 0;
+  DevBuf expanded, fused, attn_o, counters;
+  CUtensorMap tm_pool, tm_kv_new, tm_q3d;
 };
 
 namespace {
@@ -217,10 +221,11 @@ int ensure_readback(cs_model* m, size_t ints) {
 struct BatchLayout {
   int B = 0, T = 0;
   size_t off_cu, off_pos, off_tseq, off_tok, off_items, total;
-  size_t off_blocks = 0, off_pages = 0;
+  size_t off_blocks = 0, off_pages = 0, off_xtable = 0;
   int n_items = 0, n_slots = 0;
   int n_blocks = 0;        // 4-bit cache: page-wise blocks of the new tokens (appending passes)
-  int n_pages = 0;         // 4-bit cache, expand: pages to expand
+  int n_pages = 0;         // 4-bit cache, expand: pages to expand ...
+  int x_width = 0;         // ... and the row length of the expanded pages' table
   bool expand = false;     // 4-bit cache: the tensor-core attention runs over expanded pages (else the 4-bit kernel)
   int row_tile = 8;        // 4-bit cache: query rows per work item of the 4-bit kernel
   int n_merge = 0;         // 4-bit kernel: ranges cut into pieces (listed behind the n_items items)
@@ -246,9 +251,11 @@ constexpr double kAttnMergePerSplit = 0.5;
 constexpr int kAttn4MinPages = 8;
 constexpr double kAttn4Fixed = 28;
 constexpr double kAttn4Join = 8;
-// Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves; longer
-// ones have them expanded to fp16 for the tensor-core kernel.
-constexpr int kAttn4MaxRows = 32;
+// Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves, once per 16
+// rows; a batch with a longer one has its contexts expanded to fp16 for the tensor-core kernel. Measured, 64 contexts of 2 K to
+// 8 K keys x 8 heads: 64 rows 402 us against 592, 96 rows 594 against 597; 8 contexts of 1 K to 4 K keys x 4 heads: 84 rows 33
+// against 42, up to 672 rows 110 against 67.
+constexpr int kAttn4MaxRows = 96;
 
 // Time at which the last SM finishes when the items, sorted by decreasing cost, are handed to whichever of
 // `machines` SMs is free first (what the hardware does with one CTA per SM and the grid in that order).
@@ -533,6 +540,43 @@ void prof_end(cs_model* m, cudaStream_t s) {
     if (e__ != cudaSuccess) return cuda_fail(e__, #call); \
   } while (0)
 
+// Which pages of a 4-bit cache a batch of long steps reads, once per sequence, and a page table over the scratch pool that holds them
+// in this order.
+struct ExpandList {
+  std::vector<int32_t> pages, table;   // cache pages in scratch order; [rows][width] scratch pages
+  std::vector<int32_t> row;            // by step
+  int width = 1;
+};
+ExpandList list_expansion(const cs_kv* kv, int B, const int32_t* seqs, const int32_t* ctx) {
+  ExpandList x;
+  std::vector<int32_t> row_of(kv->max_seqs, -1);
+  int rows = 0;
+  for (int i = 0; i < B; ++i) {
+    if (row_of[seqs[i]] < 0) row_of[seqs[i]] = rows++;
+    x.row.push_back(row_of[seqs[i]]);
+    x.width = std::max(x.width, (ctx[i] + kPageSize - 1) / kPageSize);
+  }
+  x.table.assign(static_cast<size_t>(rows) * x.width, 0);
+  std::vector<char> done(rows, 0);
+  for (int i = 0; i < B; ++i) {
+    if (done[x.row[i]]) continue;                    // steps that share a sequence share its pages
+    done[x.row[i]] = 1;
+    const int32_t* src = kv->table_host + static_cast<size_t>(seqs[i]) * kv->max_pages_per_seq;
+    for (int j = 0; j < (ctx[i] + kPageSize - 1) / kPageSize; ++j) {
+      x.table[static_cast<size_t>(x.row[i]) * x.width + j] = static_cast<int32_t>(x.pages.size());
+      x.pages.push_back(src[j]);
+    }
+  }
+  return x;
+}
+// Elements of the K or V plane of a scratch pool of n pages (at least one, for the tensor map's sake).
+size_t expanded_plane(const cs_model* m, int n_pages) {
+  return static_cast<size_t>(std::max(1, n_pages)) * m->d.n_kv_heads * kPageSize * m->d.head_dim;
+}
+bool make_expanded_map(CUtensorMap* tm, const cs_model* m, void* pool, int n_pages) {
+  return make_kv_group_map(tm, pool, 2ull * std::max(1, n_pages) * m->d.n_kv_heads * kPageSize, m->d.head_dim, kPageSize / 8);
+}
+
 // The forward over all layers for a staged batch. When `append_kv` is given the new K/V of every layer are
 // also written to that cache's pages.
 int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout& L, const int32_t* dev_meta,
@@ -551,7 +595,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
   uint16_t* hmlp = static_cast<uint16_t*>(m->hmlp.p);
   float2* rope = static_cast<float2*>(m->rope.p);
 
-  CUtensorMap tm_a, tm_o, tm_h, tm_qkv_attn, tm_q3d;
+  CUtensorMap tm_a, tm_o, tm_h, tm_qkv_attn, tm_q3d, tm_expanded;
   const int group = d.n_q_heads / d.n_kv_heads;
   if (!make_gemm_operand_map(&tm_a, a, T, d.d_model) || !make_gemm_operand_map(&tm_o, attn_o, T, m->q_dim) ||
       !make_gemm_operand_map(&tm_h, hmlp, T, d.d_ffn) ||
@@ -559,6 +603,10 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
       !make_tensor_map_heads3d(&tm_q3d, qkv, T, d.n_q_heads + 2 * d.n_kv_heads, d.head_dim, m->n_qkv, 128 / group,
                                group)) {
     g_cuda_error = "cuTensorMapEncodeTiled failed for an activation buffer";
+    return CS_ECUDA;
+  }
+  if (L.expand && !make_expanded_map(&tm_expanded, m, m->expanded.p, L.n_pages)) {
+    g_cuda_error = "cuTensorMapEncodeTiled failed for the expanded kv pages";
     return CS_ECUDA;
   }
 
@@ -627,14 +675,17 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
       const uint8_t* layer4 = reinterpret_cast<const uint8_t*>(kv->pool) + static_cast<size_t>(l) * kv->layer4_bytes();
       if (L.expand) {
         // many query rows: the pages once more as fp16, and the tensor-core kernel over those
-        uint16_t* kx = static_cast<uint16_t*>(kv->expanded.p);
-        uint16_t* vx = kx + kv->plane_elems;
-        CS_STEP(kProfOther, launch_kv_expand(layer4, dev_meta + L.off_pages, L.n_pages, kx, vx, d.n_kv_heads, d.head_dim,
-                                             kv->num_pages, m->status, s));
-        ap.k_group_base = 0;
-        ap.v_group_base = plane_groups;
-        ap.pages_just_written = 1;
-        CS_STEP(kProfAttn, launch_attention(ap, kv->tm_expanded, tm_qkv_attn, tm_q3d, d_items, L.n_items, s));
+        uint16_t* kx = static_cast<uint16_t*>(m->expanded.p);
+        CS_STEP(kProfOther, launch_kv_expand(layer4, dev_meta + L.off_pages, L.n_pages, kx, kx + expanded_plane(m, L.n_pages),
+                                             d.n_kv_heads, d.head_dim, kv->num_pages, m->status, s));
+        AttnParams ax = ap;
+        ax.page_table = dev_meta + L.off_xtable;
+        ax.max_pages_per_seq = L.x_width;
+        ax.num_pages = std::max(1, L.n_pages);
+        ax.k_group_base = 0;
+        ax.v_group_base = ax.num_pages * d.n_kv_heads * kPageSize / 8;
+        ax.pages_just_written = 1;
+        CS_STEP(kProfAttn, launch_attention(ax, tm_expanded, tm_qkv_attn, tm_q3d, d_items, L.n_items, s));
       } else {
         Attn4Params a4 = {};
         a4.q = qkv;
@@ -715,22 +766,6 @@ int ensure_workspace(cs_model* m, int B, int T) {
   return CS_OK;
 }
 
-// Scratch pages of the 4-bit cache for the tensor-core attention: one layer's pool in the 16-bit layout (zero where nothing
-// has been expanded yet: slots behind a context are multiplied by zero probabilities) and its tensor map.
-int ensure_expanded(cs_kv* kv) {
-  int rc;
-  if ((rc = kv->expanded.ensure(2 * kv->plane_elems * 2, true))) return rc;
-  if (kv->tm_expanded_of != kv->expanded.p) {
-    const uint64_t rows = 2ull * kv->num_pages * kv->model->d.n_kv_heads * kPageSize;
-    if (!make_kv_group_map(&kv->tm_expanded, kv->expanded.p, rows, kv->model->d.head_dim, kPageSize / 8)) {
-      g_cuda_error = "cuTensorMapEncodeTiled failed for the expanded kv pages";
-      return CS_ECUDA;
-    }
-    kv->tm_expanded_of = kv->expanded.p;
-  }
-  return CS_OK;
-}
-
 // Checks a batch, writes its metadata into a staging slot and enqueues the upload.
 int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int32_t* tokens,
                 int tokens_on_device, const int32_t* lens, bool appends, BatchLayout* out, const int32_t** dev_meta,
@@ -753,7 +788,7 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   int n_slots = 0, max_rows = 0;
   bool any_split = false;
   std::vector<KvBlock> blocks;
-  std::vector<int32_t> pages;
+  ExpandList expand;
   Attn4Work work4;
   if (kv->format == CS_KV_FMT_INT4) {
     const int G = m->d.n_q_heads / m->d.n_kv_heads;
@@ -761,13 +796,7 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
     if (appends) build_append_blocks(B, seq_ids, lens, ctx.data(), blocks);
     if (max_rows > kAttn4MaxRows) {
       build_attention_work(m, B, lens, ctx.data(), items, &n_slots);
-      std::vector<char> seen(kv->max_seqs, 0);        // candidates that share a sequence share its pages
-      for (int i = 0; i < B; ++i) {
-        if (seen[seq_ids[i]]) continue;
-        seen[seq_ids[i]] = 1;
-        const int32_t* row = kv->table_host + static_cast<size_t>(seq_ids[i]) * kv->max_pages_per_seq;
-        pages.insert(pages.end(), row, row + (ctx[i] + kPageSize - 1) / kPageSize);
-      }
+      expand = list_expansion(kv, B, seq_ids, ctx.data());
     } else {
       work4 = build_4bit_work(m, B, lens, ctx.data(), true);
       n_slots = work4.n_slots;
@@ -793,12 +822,14 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   L.off_tok = take(tokens_on_device ? 0 : T);
   L.off_items = take(items.size() * (sizeof(AttnItem) / 4));
   L.off_blocks = take(blocks.size() * (sizeof(KvBlock) / 4));
-  L.off_pages = take(pages.size());
+  L.off_pages = take(expand.pages.size());
+  L.off_xtable = take(expand.table.size());
   L.total = o;
   L.n_items = static_cast<int>(items.size()) - work4.n_merge;
   L.n_merge = work4.n_merge;
   L.n_blocks = static_cast<int>(blocks.size());
-  L.n_pages = static_cast<int>(pages.size());
+  L.n_pages = static_cast<int>(expand.pages.size());
+  L.x_width = expand.width;
   L.row_tile = work4.row_tile;
   L.expand = kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows;
   L.n_slots = n_slots;
@@ -812,7 +843,7 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   if ((rc = m->attn_part_ml.ensure(static_cast<size_t>(std::max(1, n_slots)) * 128 * 2 * 4))) return rc;
   // One counter per split query tile; every launch leaves them at zero again.
   if ((rc = m->attn_counters.ensure(static_cast<size_t>(std::max(1, n_slots)) * 4, true))) return rc;
-  if (kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows && (rc = ensure_expanded(kv))) return rc;
+  if (L.expand && (rc = m->expanded.ensure(2 * expanded_plane(m, L.n_pages) * 2))) return rc;
   if ((rc = m->stg.dev.ensure(L.total * 4))) return rc;
   int slot;
   if ((rc = staging_slot(m->stg, L.total, &slot))) return rc;
@@ -829,11 +860,12 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   if (!tokens_on_device) std::memcpy(h + L.off_tok, tokens, sizeof(int32_t) * T);
   for (AttnItem& it : items) {
     it.tok0 = cu[it.step];
-    it.seq = seq_ids[it.step];
+    it.seq = L.expand ? expand.row[it.step] : seq_ids[it.step];
   }
   if (!items.empty()) std::memcpy(h + L.off_items, items.data(), items.size() * sizeof(AttnItem));
   if (!blocks.empty()) std::memcpy(h + L.off_blocks, blocks.data(), blocks.size() * sizeof(KvBlock));
-  if (!pages.empty()) std::memcpy(h + L.off_pages, pages.data(), pages.size() * sizeof(int32_t));
+  if (!expand.pages.empty()) std::memcpy(h + L.off_pages, expand.pages.data(), expand.pages.size() * sizeof(int32_t));
+  if (!expand.table.empty()) std::memcpy(h + L.off_xtable, expand.table.data(), expand.table.size() * sizeof(int32_t));
   CS_CUDA(cudaMemcpyAsync(m->stg.dev.p, h, L.total * 4, cudaMemcpyHostToDevice, s));
   m->last_h2d_bytes = static_cast<int64_t>(L.total) * 4;
   CS_CUDA(cudaEventRecord(m->stg.ev[slot], s));
@@ -1004,7 +1036,7 @@ int cs_model_free(cs_model* m) {
   for (void* p : m->owned) cudaFree(p);
   DevBuf* bufs[] = {&m->x, &m->x_last, &m->a, &m->qkv, &m->attn_o, &m->hmlp, &m->rope, &m->h_last, &m->lm_part, &m->vlogits,
                     &m->logits, &m->lse, &m->attn_part_o, &m->attn_part_ml, &m->attn_counters, &m->stg.dev,
-                    &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept};
+                    &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded};
   for (DevBuf* b : bufs) b->release();
   if (m->casc_host) cudaFreeHost(m->casc_host);
   for (cudaEvent_t e : m->prof.pool) cudaEventDestroy(e);
@@ -1122,7 +1154,6 @@ int cs_kv_free(cs_kv* kv) {
   if (kv->table_dev) cudaFree(kv->table_dev);
   if (kv->upload_ev) cudaEventDestroy(kv->upload_ev);
   kv->fill_tmp.release();
-  kv->expanded.release();
   delete kv;
   return CS_OK;
 }
@@ -1251,7 +1282,7 @@ int cs_plan_create(cs_kv* kv, int max_steps, int max_tokens, cs_plan** out) {
 int cs_plan_free(cs_plan* p) {
   if (!p) return CS_OK;
   cudaDeviceSynchronize();
-  DevBuf* bufs[] = {&p->stg.dev, &p->rope, &p->part_o, &p->part_ml};
+  DevBuf* bufs[] = {&p->stg.dev, &p->rope, &p->part_o, &p->part_ml, &p->expanded, &p->fused, &p->attn_o, &p->counters};
   for (DevBuf* b : bufs) b->release();
   for (int i = 0; i < kStagingRing; ++i) {
     if (p->stg.host[i]) cudaFreeHost(p->stg.host[i]);
@@ -1296,21 +1327,48 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
     std::sort(written.begin(), written.end());
     distinct = std::adjacent_find(written.begin(), written.end()) == written.end();
   }
+  const int G = m->d.n_q_heads / m->d.n_kv_heads;
+  int max_rows = 0;
+  for (int i = 0; i < B; ++i) max_rows = std::max(max_rows, lens[i] * G);
+  const bool expand = kv->format == CS_KV_FMT_INT4 && max_rows > kAttn4MaxRows;
   Attn4Work work;
-  if (kv->format == CS_KV_FMT_INT4 && B > 0) work = build_4bit_work(m, B, lens, ctx.data(), given != 0);
+  ExpandList x;
+  if (expand) {
+    build_attention_work(m, B, lens, ctx.data(), work.items, &work.n_slots);
+    work.n_items = static_cast<int>(work.items.size());
+    x = list_expansion(kv, B, seq_ids, ctx.data());
+  } else if (kv->format == CS_KV_FMT_INT4 && B > 0) {
+    work = build_4bit_work(m, B, lens, ctx.data(), given != 0);
+  }
   std::vector<AttnItem>& items = work.items;
-  const int n_slots = work.n_slots;
+  const int n_slots = work.n_slots, part_rows = expand ? 128 : kAttn4Rows;
   size_t o = 0;
   auto take = [&o](size_t n) { size_t r = o; o += (n + 3) & ~size_t(3); return r; };
   const size_t off_pos = take(T);
   const size_t off_blocks = take(blocks.size() * (sizeof(KvBlock) / 4));
   const size_t off_items = take(items.size() * (sizeof(AttnItem) / 4));
+  const size_t off_pages = take(x.pages.size());
+  const size_t off_xtable = take(x.table.size());
+  const int n_pages = static_cast<int>(x.pages.size());
   int rc;
   p->set = false;
   const int hd = m->d.head_dim;
   if ((rc = p->rope.ensure(static_cast<size_t>(std::max(1L, T)) * (hd / 2) * sizeof(float2)))) return rc;
-  if ((rc = p->part_o.ensure(static_cast<size_t>(n_slots) * kAttn4Rows * hd * 4))) return rc;
-  if ((rc = p->part_ml.ensure(static_cast<size_t>(n_slots) * kAttn4Rows * 2 * 4))) return rc;
+  if ((rc = p->part_o.ensure(static_cast<size_t>(n_slots) * part_rows * hd * 4))) return rc;
+  if ((rc = p->part_ml.ensure(static_cast<size_t>(n_slots) * part_rows * 2 * 4))) return rc;
+  if (expand) {
+    // as in the pass: 128 rows behind the tokens, zero when made, because a box of keys may reach past the last one
+    if ((rc = p->fused.ensure(static_cast<size_t>(T + 128) * m->n_qkv * 2, true))) return rc;
+    if ((rc = p->attn_o.ensure(static_cast<size_t>(T) * m->q_dim * 2))) return rc;
+    if ((rc = p->counters.ensure(static_cast<size_t>(std::max(1, n_slots)) * 4, true))) return rc;
+    if ((rc = p->expanded.ensure(2 * expanded_plane(m, n_pages) * 2))) return rc;
+    if (!make_expanded_map(&p->tm_pool, m, p->expanded.p, n_pages) ||
+        !make_kv_rows_map(&p->tm_kv_new, p->fused.p, T, m->n_qkv, hd) ||
+        !make_tensor_map_heads3d(&p->tm_q3d, p->fused.p, T, m->d.n_q_heads + 2 * m->d.n_kv_heads, hd, m->n_qkv, 128 / G, G)) {
+      g_cuda_error = "cuTensorMapEncodeTiled failed for a plan's buffers";
+      return CS_ECUDA;
+    }
+  }
   if ((rc = p->stg.dev.ensure(o * 4))) return rc;
   if (o > 0) {
     int slot;
@@ -1324,8 +1382,10 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
     }
     for (AttnItem& it : items) {
       it.tok0 = first[it.step];
-      it.seq = seq_ids[it.step];
+      it.seq = expand ? x.row[it.step] : seq_ids[it.step];
     }
+    if (!x.pages.empty()) std::memcpy(h + off_pages, x.pages.data(), x.pages.size() * sizeof(int32_t));
+    if (!x.table.empty()) std::memcpy(h + off_xtable, x.table.data(), x.table.size() * sizeof(int32_t));
     if (!blocks.empty()) std::memcpy(h + off_blocks, blocks.data(), blocks.size() * sizeof(KvBlock));
     if (!items.empty()) std::memcpy(h + off_items, items.data(), items.size() * sizeof(AttnItem));
     CS_CUDA(cudaMemcpyAsync(p->stg.dev.p, h, o * 4, cudaMemcpyHostToDevice, s));
@@ -1347,6 +1407,11 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
   p->off_pos = off_pos;
   p->off_blocks = off_blocks;
   p->off_items = off_items;
+  p->expand = expand;
+  p->n_pages = n_pages;
+  p->x_width = x.width;
+  p->off_pages = off_pages;
+  p->off_xtable = off_xtable;
   p->seqs.assign(seq_ids, seq_ids + B);
   p->lens.assign(lens, lens + B);
   p->ctx = ctx;
@@ -1414,6 +1479,53 @@ int cs_kv_commit(cs_plan* p) {
   return CS_OK;
 }
 
+// Long steps: the context's pages and the new tokens' rows as fp16, and the tensor-core attention over them.
+static int attention_expanded(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new,
+                              const uint16_t* v_new, int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype,
+                              float scale_log2e, cudaStream_t s) {
+  cs_kv* kv = p->kv;
+  const cs_model* m = kv->model;
+  const cs_model_desc& d = m->d;
+  const bool bf16 = dtype == CS_BF16;
+  const int32_t* meta = static_cast<const int32_t*>(p->stg.dev.p);
+  const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv->pool) + layer * kv->layer4_bytes();
+  uint16_t* fused = static_cast<uint16_t*>(p->fused.p);
+  uint16_t* kx = static_cast<uint16_t*>(p->expanded.p);
+  RowsCopy in = {{q, k_new, v_new}, {q_stride, kv_stride, kv_stride}, {m->q_dim / 8, 0, 0}, fused, m->n_qkv};
+  if (p->given) in.cols[1] = in.cols[2] = m->kv_dim / 8;
+  CS_CUDA(launch_rows_copy(in, bf16, false, p->T, s));
+  if (!p->given)
+    CS_CUDA(launch_kv_blocks(pool, reinterpret_cast<const KvBlock*>(meta + p->off_blocks), p->n_blocks, kv->table_dev,
+                             kv->max_pages_per_seq, fused + m->q_dim, fused + m->q_dim + m->kv_dim, m->n_qkv, d.n_kv_heads,
+                             d.head_dim, kv->num_pages, m->status, s));
+  CS_CUDA(launch_kv_expand(pool, meta + p->off_pages, p->n_pages, kx, kx + expanded_plane(m, p->n_pages), d.n_kv_heads,
+                           d.head_dim, kv->num_pages, m->status, s));
+  const bool direct = !bf16 && out_stride == m->q_dim;
+  AttnParams a = {};
+  a.qkv = fused;
+  a.out = direct ? out : static_cast<uint16_t*>(p->attn_o.p);
+  a.page_table = meta + p->off_xtable;
+  a.max_pages_per_seq = p->x_width;
+  a.n_q_heads = d.n_q_heads;
+  a.n_kv_heads = d.n_kv_heads;
+  a.head_dim = d.head_dim;
+  a.n_qkv = m->n_qkv;
+  a.num_pages = std::max(1, p->n_pages);
+  a.v_group_base = a.num_pages * d.n_kv_heads * kPageSize / 8;
+  a.scale_log2e = scale_log2e;
+  a.part_o = static_cast<float*>(p->part_o.p);
+  a.part_ml = static_cast<float*>(p->part_ml.p);
+  a.counters = static_cast<int32_t*>(p->counters.p);
+  a.status = m->status;
+  a.n_rows = p->T;
+  a.pages_just_written = 1;
+  CS_CUDA(launch_attention(a, p->tm_pool, p->tm_kv_new, p->tm_q3d, reinterpret_cast<const AttnItem*>(meta + p->off_items),
+                           p->n_items, s));
+  const RowsCopy back = {{static_cast<const uint16_t*>(p->attn_o.p)}, {m->q_dim}, {m->q_dim / 8, 0, 0}, out, out_stride};
+  if (!direct) CS_CUDA(launch_rows_copy(back, false, bf16, p->T, s));
+  return CS_OK;
+}
+
 int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new, const uint16_t* v_new,
                       int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype, float scale, void* stream) {
   int rc;
@@ -1428,6 +1540,9 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   if (p->given && (!rows_ok(k_new, kv_stride, kv_row) || !rows_ok(v_new, kv_stride, kv_row))) return CS_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((rc = table_ready(kv, s))) return rc;
+  const double sc = scale > 0.f ? static_cast<double>(scale) : 1.0 / std::sqrt(static_cast<double>(d.head_dim));
+  const float scale_log2e = static_cast<float>(1.4426950408889634 * sc);
+  if (p->expand) return attention_expanded(p, layer, q, q_stride, k_new, v_new, kv_stride, out, out_stride, dtype, scale_log2e, s);
   Attn4Params a = {};
   a.q = q;
   a.k_new = k_new;
@@ -1445,8 +1560,7 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   a.head_dim = d.head_dim;
   a.given = p->given;
   a.in_bf16 = a.out_bf16 = dtype == CS_BF16;
-  const double sc = scale > 0.f ? static_cast<double>(scale) : 1.0 / std::sqrt(static_cast<double>(d.head_dim));
-  a.scale_log2e = static_cast<float>(1.4426950408889634 * sc);
+  a.scale_log2e = scale_log2e;
   a.part_o = static_cast<float*>(p->part_o.p);
   a.part_ml = static_cast<float*>(p->part_ml.p);
   a.status = kv->model->status;
@@ -1763,7 +1877,7 @@ int cs_check_workspace(cs_model* m, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const DevBuf* bufs[] = {&m->x, &m->x_last, &m->a, &m->qkv, &m->attn_o, &m->hmlp, &m->rope, &m->h_last, &m->lm_part,
                           &m->vlogits, &m->logits, &m->lse, &m->attn_part_o, &m->attn_part_ml, &m->attn_counters,
-                          &m->stg.dev, &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept};
+                          &m->stg.dev, &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded};
   for (const DevBuf* b : bufs) {
     const int st = b->canary_state(s);
     if (st < 0) return cuda_fail(cudaGetLastError(), "workspace canary read-back");

@@ -129,13 +129,26 @@ struct KvReadParams {
   const int32_t *table, *tok_seq, *tok_pos;
   uint16_t *out_k, *out_v;         // [T, n_kv_heads, head_dim], fp16 or bf16 (dst_bf16)
   int32_t T, max_seqs, max_pages_per_seq, num_pages, n_kv_heads, dst_bf16;
-  int32_t heads_per_part;          // set by the launcher
   uint32_t* status;
 };
-cudaError_t launch_kv_read(KvReadParams p, int format, int hd, cudaStream_t s);
-// The listed pages of a layer of the 4-bit cache as fp16 pages [num_pages][kv heads][16][head_dim] of a scratch pool.
+cudaError_t launch_kv_read(const KvReadParams& p, int format, int hd, cudaStream_t s);
+// The listed pages of a layer of the 4-bit cache as fp16 pages [n_pages][kv heads][16][head_dim] of a scratch pool, in list order.
 cudaError_t launch_kv_expand(const uint8_t* pool, const int32_t* pages, int n_pages, uint16_t* out_k, uint16_t* out_v,
                              int n_kv_heads, int hd, int num_pages, uint32_t* status, cudaStream_t s);
+
+// Keys and values of the blocks' tokens out of the 4-bit cache into columns of a fused fp16 matrix (row stride in elements).
+cudaError_t launch_kv_blocks(const uint8_t* pool, const KvBlock* blocks, int n_blocks, const int32_t* table, int max_pages_per_seq,
+                             uint16_t* out_k, uint16_t* out_v, int64_t stride, int n_kv_heads, int hd, int num_pages,
+                             uint32_t* status, cudaStream_t s);
+// Up to three row sources of 16-bit values side by side into one matrix, fp16 or bf16 on either side.
+struct RowsCopy {
+  const uint16_t* src[3];
+  int64_t stride[3];        // elements between rows
+  int32_t cols[3];          // in pieces of 8 elements; 0: no such source
+  uint16_t* dst;
+  int64_t dst_stride;
+};
+cudaError_t launch_rows_copy(const RowsCopy& p, bool from_bf16, bool to_bf16, int rows, cudaStream_t s);
 
 constexpr int kAttn4Rows = 16;           // query rows per work item at most
 struct Attn4Params {

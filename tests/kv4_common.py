@@ -34,7 +34,7 @@ def rotate(x, pos, theta):
     return np.concatenate([x[..., :half] * c - x[..., half:] * s, x[..., half:] * c + x[..., :half] * s], -1)
 
 
-def attend(q, k, v, v_steps, k_mag, seen, scale):
+def attend(q, k, v, v_steps, k_mag, seen, scale, expanded=False):
     """One step in 64 bits: q [n, hq, hd], k, v [m, hkv, hd]; token t sees keys < seen[t]. Returns (out, bound): the bound counts
     the roundings that the kernel's formats make, per output:
       p to fp16 (2^-11 of each term's |p v|), p s to fp16 (2^-11 of p s |c - 8|, at most p |c s| = v_steps), the output (2^-11, or
@@ -42,6 +42,8 @@ def attend(q, k, v, v_steps, k_mag, seen, scale):
       where the largest p of a row is at least 2^2: m 2^-27 |v| and m 2^-24 together for m keys; the score's fp32 sums: hd + 8
       additions of terms q (64 + c) s and q o, each off by at most 2^-23 of the sum of magnitudes (k_mag [m, hkv] = max over
       groups of 79 s + |o|); 2^x to 2^-18.
+    expanded: the keys and values were rounded to fp16 first: 2^-11 of every |q_d k_d| in the score, 2^-11 of every |p v|; the sums
+    run over the values themselves.
     """
     n, hq, hd = q.shape
     group = hq // k.shape[1]
@@ -58,7 +60,9 @@ def attend(q, k, v, v_steps, k_mag, seen, scale):
             out[t, h] = p @ vh[:m]
             delta = (hd + 8) * 2.0 ** -23 * scale * np.abs(q[t, h]).sum() * mag[:m].max() + 2.0 ** -18
             spread = p @ np.abs(vh[:m])
-            bound[t, h] = (2.0 ** -11 * (spread + p @ st[:m]) + m * 2.0 ** -27 * np.abs(vh[:m]).max() + m * 2.0 ** -24
+            if expanded:
+                delta += 2.0 ** -11 * scale * (np.abs(kh[:m]) @ np.abs(q[t, h])).max()
+            bound[t, h] = (2.0 ** -11 * (spread * (2 if expanded else 1) + p @ st[:m]) + m * 2.0 ** -27 * np.abs(vh[:m]).max() + m * 2.0 ** -24
                            + 2 * delta * spread + 2 * delta * np.abs(out[t, h]))
     return out, bound
 

@@ -18,9 +18,8 @@ def _np(t):
 
 
 def _held(c, s, o):
-    """What cs_kv_read gives for these codes: the value rounded to fp16 (from fp32: the product is exact there)."""
-    g = (c.reshape(*c.shape[:-1], -1, K.GROUP) * s[..., None]).astype(np.float32) + o[..., None].astype(np.float32)
-    return g.reshape(c.shape).astype(np.float16).astype(np.float64)
+    """What cs_kv_read gives for these codes: the value, exact in 64 bits, rounded to fp16 once."""
+    return K.values(c, s, o).astype(np.float16).astype(np.float64)
 
 
 @pytest.mark.parametrize("hd", [64, 128])
@@ -231,7 +230,7 @@ def _attention_case(hq, hkv, hd, ctx, lens, given, dtype, q_scale=1.0, kv_scale=
             own_k, own_v = _np(kn[at]), _np(vn[at])
             parts = [np.concatenate(z) for z in zip(parts, (own_k, own_v, np.abs(own_v), np.abs(own_k).max(-1)))]
         seen = int(ctx[i]) + np.arange(lens[i]) + 1
-        want, bound = K.attend(_np(q[at]), *parts, seen, scale or hd ** -0.5)
+        want, bound = K.attend(_np(q[at]), *parts, seen, scale or hd ** -0.5, max(lens) * hq // hkv > 96)
         bound = bound + (2.0 ** -11 if dtype == "float16" else 2.0 ** -8) * np.abs(want) + 2.0 ** -25
         err = np.abs(got[at] - want)
         assert np.all(err <= bound), (i, float(np.nanmax(err / bound)), np.argwhere(~(err <= bound))[:4])
@@ -249,8 +248,9 @@ def test_attention_one_token(hq, hkv, hd, given):
 @pytest.mark.parametrize("hq,hkv,hd,dtype", [(12, 2, 128, "float16"), (14, 2, 128, "bfloat16"), (4, 4, 64, "bfloat16"),
                                              (16, 8, 128, "float16")])
 def test_attention_steps_of_every_length(hq, hkv, hd, dtype, given):
-    """Row tiles of 8, 16 and 32 in use: steps of 1 to 40 tokens, pages that end inside a step, contexts down to nothing."""
-    for lens in ([1, 2, 1, 1], [1, 2, 3, 2], [5, 4, 1, 3], [8, 1, 17, 40]):
+    """Row tiles of 8 and 16, several tiles, and the expanded form: steps of 1 to 100 tokens, pages that end inside a step,
+    contexts down to nothing."""
+    for lens in ([1, 2, 1, 1], [1, 2, 3, 2], [5, 4, 1, 3], [8, 1, 3, 13], [8, 1, 17, 100]):
         _attention_case(hq, hkv, hd, [0, 7, 48, 130], lens, given, dtype, seed=sum(lens))
 
 
@@ -295,18 +295,20 @@ def test_attention_reads_nothing_behind_a_sequence():
     assert torch.equal(*outs)
 
 
-def test_attention_on_slices_and_in_place():
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("n1", [5, 60])                                 # 15 and 180 query rows: the 4-bit and the expanded form
+def test_attention_on_slices_and_in_place(n1, dtype):
     import torch
     rng = np.random.default_rng(10)
-    hq, hkv, hd, n = 6, 2, 128, 9
+    hq, hkv, hd, n = 6, 2, 128, 4 + n1
     with K.Cache(hq, hkv, hd, n_seqs=2) as c:
-        fused = _rows(rng, n, hq + 2 * hkv, hd, "float16")
+        fused = _rows(rng, n, hq + 2 * hkv, hd, dtype)
         q, k, v = fused[:, :hq], fused[:, hq:hq + hkv], fused[:, hq + hkv:]
         c.B.cs_plan_set(c.plan, [0, 1], [30, 50])
         c.B.cs_kv_append(c.plan, 0, *(_rows(rng, 80, hkv, hd, "float16") for _ in range(2)))
         c.set([30, 50])
-        c.B.cs_plan_set(c.plan, [0, 1], [4, 5], given=True)
-        plain = torch.empty(n, hq, hd, dtype=torch.float16, device="cuda")
+        c.B.cs_plan_set(c.plan, [0, 1], [4, n1], given=True)
+        plain = torch.empty(n, hq, hd, dtype=fused.dtype, device="cuda")
         # given keys of the fused matrix share one row stride
         c.B.cs_attention_4bit(c.plan, 0, q.contiguous(), plain, k.contiguous(), v.contiguous())
         c.B.cs_attention_4bit(c.plan, 0, q, q, k, v)
@@ -335,6 +337,44 @@ def test_the_same_context_for_several_steps():
             c.B.cs_attention_4bit(c.plan, 0, q[a:b], one[a:b], k[a:b], v[a:b])
         torch.cuda.synchronize()
         assert torch.equal(out, one)
+
+
+def test_a_long_step_in_a_graph_and_a_plan_set_anew():
+    """The expanded form captured and replayed, then the same plan for another batch (fewer rows, then more than before)."""
+    import torch
+    rng = np.random.default_rng(15)
+    hq, hkv, hd = 8, 2, 64
+    with K.Cache(hq, hkv, hd, n_seqs=3, pages_each=20) as c:
+        c.B.cs_plan_set(c.plan, [0, 1, 2], [100, 37, 300])
+        c.B.cs_kv_append(c.plan, 0, *(_rows(rng, 437, hkv, hd, "float16") for _ in range(2)))
+        q = _rows(rng, 120, hq, hd, "float16")
+        k, v = _rows(rng, 120, hkv, hd, "float16"), _rows(rng, 120, hkv, hd, "float16")
+        c.set([100, 37, 300])
+
+        def attend(lens, given):
+            n = sum(lens)
+            out = torch.full_like(q, 3.0)
+            c.B.cs_plan_set(c.plan, [0, 1, 2], lens, given=given)
+            new = (k[:n], v[:n]) if given else (None, None)
+            c.B.cs_attention_4bit(c.plan, 0, q[:n], out[:n], *new)
+            torch.cuda.synchronize()
+            assert bool((out[n:] == 3.0).all())                          # rows behind the last token stay
+            graph, again = torch.cuda.CUDAGraph(), torch.full_like(q, 3.0)
+            with torch.cuda.graph(graph):
+                c.B.cs_attention_4bit(c.plan, 0, q[:n], again[:n], *new)
+            for _ in range(2):
+                graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, again)
+            return out[:n]
+
+        first = attend([30, 2, 40], True)
+        attend([1, 1, 2], True)
+        attend([50, 30, 40], True)
+        assert torch.equal(attend([30, 2, 40], True), first)
+        c.set([70, 35, 260])                                             # the new tokens' keys out of the cache
+        attend([30, 2, 40], False)
+        attend([1, 1, 1], False)
 
 
 def test_decoding_step_by_step_eager_and_as_a_graph():
