@@ -160,7 +160,7 @@ struct cs_plan {
   cs_kv* kv;
   int device = 0;
   bool set = false, given = false, appendable = false, committed = false;
-  int B = 0, T = 0, n_blocks = 0, n_items = 0, n_merge = 0, row_tile = 8;
+  int B = 0, T = 0, n_blocks = 0, n_items = 0, n_merge = 0, row_tile = 8, cluster = 1;
   size_t off_pos = 0, off_blocks = 0, off_items = 0;      // int32 offsets into the staged block
   std::vector<int32_t> seqs, lens, ctx;
   Staging stg;
@@ -229,6 +229,7 @@ struct BatchLayout {
   bool expand = false;     // 4-bit cache: the tensor-core attention runs over expanded pages (else the 4-bit kernel)
   int row_tile = 8;        // 4-bit cache: query rows per work item of the 4-bit kernel
   int n_merge = 0;         // 4-bit kernel: ranges cut into pieces (listed behind the n_items items)
+  int cluster = 1;         // 4-bit kernel: CTAs of a cluster
   int max_rows = 0;        // 8-bit cache: the largest number of query rows (new tokens x heads per kv head) of a step
   bool any_split = false;  // 8-bit cache: some context is cut into pieces
 };
@@ -247,10 +248,12 @@ constexpr double kAttnMergePerSplit = 0.5;
 // 4-bit attention, in pages of one CTA among as many as fit on its SM (0.28 us at 8 query rows): the smallest piece worth an item
 // of its own; what an item costs besides its pages (alone 3.2 us from launch to end, most of it latencies in a row; counted higher
 // because long pieces proved faster wherever there is more than one wave: 64 contexts of 2 K to 8 K keys 66.9 us with 28, 69.4 with
-// 12); what joining pieces adds to a launch.
+// 12); what joining pieces adds to a
+// launch, by a second kernel or inside a cluster.
 constexpr int kAttn4MinPages = 8;
 constexpr double kAttn4Fixed = 28;
 constexpr double kAttn4Join = 8;
+constexpr double kAttn4ClusterJoin = 3;
 // Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves, once per 16
 // rows; a batch with a longer one has its contexts expanded to fp16 for the tensor-core kernel. Measured, 64 contexts of 2 K to
 // 8 K keys x 8 heads: 64 rows 402 us against 592, 96 rows 594 against 597; 8 contexts of 1 K to 4 K keys x 4 heads: 84 rows 33
@@ -385,6 +388,7 @@ void build_short_work(const cs_model* m, int B, const int32_t* lens, const int32
 struct Attn4Work {
   std::vector<AttnItem> items;   // the work, and behind it one item (the last piece) of each of the n_merge ranges that were cut
   int n_items = 0, n_merge = 0, n_slots = 0, row_tile = 8;
+  int cluster = 1;               // > 1: every range is cut into this many pieces, one cluster (nothing is left to join)
 };
 
 // One item per (step, kv head, tile of query rows, piece of the pages). Pages are the cached ones and, when the new tokens' keys
@@ -453,6 +457,25 @@ Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const i
   const double share = total / machines;           // pages per slot
   for (double f : {4.0, 2.0, 1.5, 1.33, 1.2, 1.12, 1.06, 1.0, 0.8, 0.65, 0.55, 0.5, 0.4, 0.33, 0.25, 0.2})
     consider(static_cast<int>(std::ceil(share * f)));
+  // One range per cluster, with an SM for every CTA: clusters that have to share SMs start late (148 ranges of 63 pages as pairs took
+  // 12.3 us, uncut 8.3).
+  for (int c : {2, 4, 8}) {
+    const double n_ctas = static_cast<double>(units.size()) * heads * c;
+    if (n_ctas > kNumSMs || (longest + c - 1) / c < kAttn4MinPages / 2) break;
+    const double e = kAttn4Fixed + (longest + c - 1) / c * 0.35 + kAttn4ClusterJoin;
+    if (e < best) { best = e; w.cluster = c; }
+  }
+  if (w.cluster > 1) {
+    std::stable_sort(units.begin(), units.end(), [](const Unit& a, const Unit& b) { return a.pages > b.pages; });
+    for (const Unit& u : units)
+      for (int h = 0; h < heads; ++h)
+        for (int c = 0; c < w.cluster; ++c)
+          w.items.push_back(AttnItem{u.step, h, u.row0, static_cast<int>(static_cast<long>(u.pages) * c / w.cluster),
+                                     static_cast<int>(static_cast<long>(u.pages) * (c + 1) / w.cluster), 0, 0, 1, 0, lens[u.step],
+                                     ctx[u.step], 0, {0, u.cached, 0, 0}});
+    w.n_items = static_cast<int>(w.items.size());
+    return w;
+  }
   std::vector<AttnItem> merge;
   for (const Unit& u : units) {
     const int n = pieces(u.pages, best_cap);
@@ -704,6 +727,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
         a4.given = 1;
         a4.cache_is_settled = 1;      // this layer's pages were written by an earlier call, and an upload stands in between
         a4.scale_log2e = ap.scale_log2e;
+        a4.cluster = L.cluster;
         a4.part_o = ap.part_o;
         a4.part_ml = ap.part_ml;
         a4.status = m->status;
@@ -827,6 +851,7 @@ int stage_batch(cs_model* m, cs_kv* kv, const int32_t* seq_ids, int B, const int
   L.total = o;
   L.n_items = static_cast<int>(items.size()) - work4.n_merge;
   L.n_merge = work4.n_merge;
+  L.cluster = work4.cluster;
   L.n_blocks = static_cast<int>(blocks.size());
   L.n_pages = static_cast<int>(expand.pages.size());
   L.x_width = expand.width;
@@ -1401,6 +1426,7 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
   p->appendable = room && distinct;
   p->committed = false;
   p->n_merge = work.n_merge;
+  p->cluster = work.cluster;
   p->row_tile = work.row_tile;
   p->n_blocks = static_cast<int>(blocks.size());
   p->n_items = work.n_items;
@@ -1561,6 +1587,7 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   a.given = p->given;
   a.in_bf16 = a.out_bf16 = dtype == CS_BF16;
   a.scale_log2e = scale_log2e;
+  a.cluster = p->cluster;
   a.part_o = static_cast<float*>(p->part_o.p);
   a.part_ml = static_cast<float*>(p->part_ml.p);
   a.status = kv->model->status;

@@ -20,8 +20,9 @@
 //     q . k = sum_groups s (sum_d q_d h_d) + o (sum_d q_d) - 64 s (sum over those channels of q_d),
 // whose operands are the offsets and scales as they are stored; one packed addition makes c (keys) or c - 8 (values) of the
 // others. The product that sums the values' offsets has rows of ones besides, which sum the probabilities.
-// A piece of a long context leaves (max, sum, O) in fp32 and a second kernel, one CTA per query row, joins the pieces in their
-// order. (Joining by the last piece to finish saves that launch but takes longer, even for few pieces: the fence, the counter
+// Pieces of a context are joined in their order. Where a few per context fill the machine, they are the CTAs of one cluster, which
+// read one another's (max, sum, O) through shared memory: one launch. Else a piece leaves them in global memory and a second kernel,
+// one CTA per query row, joins them. (Joining by the last piece to finish saves that launch but takes longer, even for few pieces: the fence, the counter
 // and the reads follow one another at the end of the chain, while the second kernel's start overlaps this one. One token on 512
 // keys 7.9 us against 6.0, 16 sequences of up to 2048 10.7 against 9.2.)
 #include <type_traits>
@@ -112,6 +113,41 @@ __device__ __forceinline__ void store_out(const Attn4Params& p, size_t at, float
   else reinterpret_cast<__half*>(p.out)[at] = __float2half_rn(v);
 }
 
+__device__ __forceinline__ void store_out4(const Attn4Params& p, size_t at, float4 v) {
+  *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.out) + at) =
+      p.out_bf16 ? make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w)) : make_uint2(pack_f16x2(v.x, v.y), pack_f16x2(v.z, v.w));
+}
+__device__ __forceinline__ void add_scaled(float4& a, float f, const float4& v) {
+  a.x += f * v.x; a.y += f * v.y; a.z += f * v.z; a.w += f * v.w;
+}
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Another CTA's shared memory at the same place as this CTA's `addr`.
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, int cta) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+  return r;
+}
+__device__ __forceinline__ float2 load_peer2(uint32_t addr, int cta) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(peer_addr(addr, cta)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 load_peer4(uint32_t addr, int cta) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(peer_addr(addr, cta))
+               : "memory");
+  return v;
+}
+
 // CTAs that an SM holds at once (128 and 168 registers a thread).
 __host__ __device__ constexpr int ctas_per_sm(int nt) { return nt == 1 ? 4 : 3; }
 
@@ -122,11 +158,14 @@ struct Smem4 {
   static constexpr int kPad = HD + 4;                                  // row stride of the partial results, in floats
   static constexpr int kPartBytes = kWarps * 8 * NT * kPad * 4;
   static constexpr int kStatBytes = kWarps * 8 * NT * 2 * 4;
-  static constexpr int kUnion = kStagesBytes > kPartBytes + kStatBytes ? kStagesBytes : kPartBytes + kStatBytes;
+  static constexpr int kJoinBytes = 8 * NT * (HD * 4 + 8);             // one CTA's results, for the others of its cluster
+  static constexpr int kEnd = kPartBytes + kStatBytes + kJoinBytes;
+  static constexpr int kUnion = kStagesBytes > kEnd ? kStagesBytes : kEnd;
+  static_assert((kPartBytes + kStatBytes) % 16 == 0, "the joined rows are read in 16-byte pieces");
   // from 16 query rows on, the query operands do not fit the registers beside the accumulators
   static constexpr int kQBytes = NT > 1 ? 8 * NT * HD * 2 : 0;
   static constexpr int kTotal = kUnion + kQBytes;
-  static_assert(kWarp >= kPage * HD * 2, "a page of own values must fit in one warp's stages");
+  static_assert(2 * Kv4<HD>::kBlock >= kPage * HD * 2, "a page of own values must fit in one stage");
 };
 
 // What each piece of a cut range weighs in the output of query row r: 2^(its reference - the largest) / the whole sum. One warp,
@@ -425,7 +464,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   };
 
   // A page of the step's own keys and values, given as rows in fp16 or bf16: K operands straight from global memory, V through
-  // this warp's (drained) stages and transposing loads.
+  // this warp's last stage, which is not in use yet, and transposing loads.
+  uint8_t* own_v = my + (kStages - 1) * kStageBytes;
   auto own_page = [&](int key0) {
     __syncwarp();
     constexpr int CH = HD / 8;
@@ -435,7 +475,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       if (key0 + key < it.n_new)
         v = as_f16(*reinterpret_cast<const uint4*>(p.v_new + (it.tok0 + key0 + key) * p.kv_stride + it.kv_head * HD + ch * 8),
                    p.in_bf16 != 0);
-      *reinterpret_cast<uint4*>(my + key * HD * 2 + ((ch ^ (key & 7)) << 4)) = v;
+      *reinterpret_cast<uint4*>(own_v + key * HD * 2 + ((ch ^ (key & 7)) << 4)) = v;
     }
     __syncwarp();
     float s1[1][NT][4];
@@ -472,7 +512,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       uint32_t a[4];
-      ldmatrix_x4_trans(a, my_u + key * HD * 2 + (((2 * mt + up) ^ (key & 7)) << 4));
+      ldmatrix_x4_trans(a, smem_u32(own_v) + key * HD * 2 + (((2 * mt + up) ^ (key & 7)) << 4));
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) mma_k16(o[nt][mt], a, pb[nt][0], pb[nt][1]);
     }
@@ -481,6 +521,10 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     for (int nt = 0; nt < NT; ++nt) mma_k16(oo[nt], ao, pb[nt][0], pb[nt][1]);
     __syncwarp();
   };
+
+  // own pages first, while the cached ones are on their way, from the last warp on, which has the fewest of those
+  for (int own = max(it.tile_begin, cached_pages) + (kWarps - 1 - warp); own < it.tile_end; own += kWarps)
+    own_page((own - cached_pages) * kPage);
 
   int stage_off = 0, ahead_off = (kStages - 1) * kStageBytes;
 #pragma unroll 1
@@ -511,10 +555,6 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     stage_off = stage_off == (kStages - 1) * kStageBytes ? 0 : stage_off + kStageBytes;
   }
   cp_async_wait<0>();
-  // own pages: one at a time to the warps in turn, from the last warp on, which has the fewest cached pages
-  for (int own = max(it.tile_begin, cached_pages) + (kWarps - 1 - warp); own < it.tile_end; own += kWarps)
-    own_page((own - cached_pages) * kPage);
-  cp_async_wait<0>();
   __syncthreads();
 
   // ------------------------------------------------------------------ the warps' results, joined in warp order
@@ -542,29 +582,60 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     }
   }
   __syncthreads();
-  for (int idx = threadIdx.x; idx < R * HD; idx += kThreads) {
-    const int r = idx / HD, d = idx % HD;
+  constexpr int kQuads = HD / 4;
+  float4* joined = reinterpret_cast<float4*>(smem + S::kPartBytes + S::kStatBytes);      // cluster: [8 NT rows][HD / 4] of this CTA
+  float2* joined_ml = reinterpret_cast<float2*>(joined + 8 * NT * kQuads);
+  auto write_out = [&](int r, int c4, float4 v, float scale) {
+    const int t = (row0 + r) / G, hq = (row0 + r) % G;
+    store_out4(p, (it.tok0 + t) * p.out_stride + (it.kv_head * G + hq) * HD + 4 * c4,
+               make_float4(v.x * scale, v.y * scale, v.z * scale, v.w * scale));
+  };
+  for (int idx = threadIdx.x; idx < R * kQuads; idx += kThreads) {
+    const int r = idx / kQuads, c4 = idx % kQuads;
     float M = kNoMax;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) M = fmaxf(M, pml[(w * 8 * NT + r) * 2]);
-    float acc = 0.f, sum = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
       const float f = fast_exp2(pml[(w * 8 * NT + r) * 2] - M);
-      acc += f * po[(w * 8 * NT + r) * S::kPad + d];
+      add_scaled(acc, f, *reinterpret_cast<const float4*>(po + (w * 8 * NT + r) * S::kPad + 4 * c4));
       sum += f * pml[(w * 8 * NT + r) * 2 + 1];
     }
-    if (it.n_splits == 1) {
-      const int t = (row0 + r) / G, hq = (row0 + r) % G;
-      store_out(p, (it.tok0 + t) * p.out_stride + (it.kv_head * G + hq) * HD + d, sum > 0.f ? acc / sum : 0.f);
+    if (p.cluster > 1) {
+      joined[r * kQuads + c4] = acc;
+      if (c4 == 0) joined_ml[r] = make_float2(M, sum);
+    } else if (it.n_splits == 1) {
+      write_out(r, c4, acc, sum > 0.f ? 1.f / sum : 0.f);
     } else {
-      p.part_o[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * HD + d] = acc;
-      if (d == 0) {
-        p.part_ml[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * 2] = M;
-        p.part_ml[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * 2 + 1] = sum;
-      }
+      reinterpret_cast<float4*>(p.part_o)[(static_cast<size_t>(it.slot) * kAttn4Rows + r) * kQuads + c4] = acc;
+      if (c4 == 0)
+        reinterpret_cast<float2*>(p.part_ml)[static_cast<size_t>(it.slot) * kAttn4Rows + r] = make_float2(M, sum);
     }
   }
+  if (p.cluster <= 1) return;
+
+  // ------------------------------------------------------------------ the cluster's CTAs hold the pieces of one range
+  cluster_barrier();
+  const uint32_t rank = cluster_rank();
+  const uint32_t joined_u = smem_u32(joined), ml_u = smem_u32(joined_ml);
+  for (int idx = rank * kThreads + threadIdx.x; idx < R * kQuads; idx += kThreads * p.cluster) {
+    const int r = idx / kQuads, c4 = idx % kQuads;
+    float M = kNoMax;
+    for (int c = 0; c < p.cluster; ++c) M = fmaxf(M, load_peer2(ml_u + r * 8, c).x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < p.cluster; ++c) {
+      const float2 ml = load_peer2(ml_u + r * 8, c);
+      const float f = fast_exp2(ml.x - M);
+      add_scaled(acc, f, load_peer4(joined_u + (r * kQuads + c4) * 16, c));
+      sum += f * ml.y;
+    }
+    write_out(r, c4, acc, sum > 0.f ? 1.f / sum : 0.f);
+  }
+  cluster_barrier();                 // nobody leaves while its results may still be read
 }
 
 // Pieces of one (step, kv head, row tile) -> output. One CTA per cut range and query row, one thread per channel: the pieces'
@@ -604,7 +675,10 @@ cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items
   static std::atomic<uint64_t> smem_opted{0};
   if (cudaError_t e = opt_in_dynamic_smem(attention_4bit_kernel<HD, NT>, Smem4<HD, NT>::kTotal, smem_opted); e != cudaSuccess)
     return e;
-  cudaError_t e = launch_pdl(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads), Smem4<HD, NT>::kTotal, s, p, items);
+  cudaError_t e = p.cluster > 1 ? launch_pdl_cluster(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads),
+                                                     Smem4<HD, NT>::kTotal, s, p.cluster, p, items)
+                                : launch_pdl(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads), Smem4<HD, NT>::kTotal, s,
+                                             p, items);
   count_launch();
   if (e != cudaSuccess || n_merge == 0) return e != cudaSuccess ? e : cudaGetLastError();
   e = launch_pdl(attention_4bit_merge_kernel<HD>, dim3(n_merge, 8 * NT), dim3(HD), 0, s, p, items + n_items, 8 * NT);
