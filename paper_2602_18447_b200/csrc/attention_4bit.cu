@@ -649,20 +649,25 @@ __global__ void __launch_bounds__(HD) attention_4bit_merge_kernel(const Attn4Par
   const int r = blockIdx.y, d = threadIdx.x, n = it.n_splits;
   pdl_wait();
   if (r >= min(tile, it.n_new * G - it.q_tok0)) return;
-  if (threadIdx.x < 32) piece_weights(p, it, r, d, weight);
-  __syncthreads();
-  // four channels a thread; the warps (HD = 64: half warps) take every fourth piece, and their sums are added in order
-  constexpr int kQuads = HD / 4;
+  // four channels a thread; the warps (HD = 64: half warps) take every fourth piece, and their sums are added in order. The first
+  // pieces are requested before the weights are known.
+  constexpr int kQuads = HD / 4, kAhead = 4;
   __shared__ float4 part[4][kQuads];
   const int share = d / kQuads, c4 = d % kQuads;
   const float4* o = reinterpret_cast<const float4*>(p.part_o + (static_cast<size_t>(it.slot0) * kAttn4Rows + r) * HD) + c4;
+  float4 first[kAhead];
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (share + 4 * j < n) first[j] = __ldcg(o + static_cast<size_t>(share + 4 * j) * kAttn4Rows * kQuads);
+  if (threadIdx.x < 32) piece_weights(p, it, r, d, weight);
+  __syncthreads();
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int j = 0; j < kAhead; ++j)
+    if (share + 4 * j < n) add_scaled(acc, weight[share + 4 * j], first[j]);
 #pragma unroll 8
-  for (int s = share; s < n; s += 4) {
-    const float4 v = __ldcg(o + static_cast<size_t>(s) * kAttn4Rows * kQuads);
-    const float w = weight[s];
-    acc.x += w * v.x; acc.y += w * v.y; acc.z += w * v.z; acc.w += w * v.w;
-  }
+  for (int s = share + 4 * kAhead; s < n; s += 4)
+    add_scaled(acc, weight[s], __ldcg(o + static_cast<size_t>(s) * kAttn4Rows * kQuads));
   part[share][c4] = acc;
   __syncthreads();
   const float* sums = reinterpret_cast<const float*>(part);
