@@ -365,10 +365,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
         pb[pp][nt][1] = transpose8x8(pack_f16x2(y[2], y[3]));
       }
   };
-  // Keys key0 .. key0 + 15 against the last key that the rows of token t see, base + t: masked scores are -inf.
-  const int t_min = row0 / G;
+  // Keys key0 .. key0 + 15 against the last key that the rows of token t see, base + per_token t: masked scores are -inf.
   auto mask = [&](float (&s)[NT][4], int key0, int base, int per_token) {
-    if (key0 + kPage - 1 <= base + per_token * t_min) return;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -379,7 +377,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   };
 
   const int see_base = it.ctx - (p.given ? 1 : 0), see_step = p.given ? 0 : 1;
-  auto cached_scores = [&](const uint8_t* b, int key0, float (&s)[NT][4]) {
+  const int all_see = see_base + see_step * (row0 / G);        // the last key that every row of this tile sees
+  auto cached_scores = [&](const uint8_t* b, float (&s)[NT][4]) {
     float acc[NT][NG][4];
     uint32_t kw[2][2 * NG];
     if (NG == 2) {
@@ -429,7 +428,6 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
 #pragma unroll
         for (int grp = 0; grp < NG; ++grp) s[nt][e] = fmaf(sc[e >> 1][grp], acc[nt][grp][e], s[nt][e]);
     }
-    mask(s, key0, see_base, see_step);
   };
 
   auto cached_values = [&](const uint8_t* b, uint32_t (&pb)[NT][2]) {
@@ -539,15 +537,20 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     if (pg + 1 < end_cached) {
       float s[2][NT][4];
       uint32_t pb[2][NT][2];
-      cached_scores(b, pg * kPage, s[0]);
-      cached_scores(b + L::kBlock, pg * kPage + kPage, s[1]);
+      cached_scores(b, s[0]);
+      cached_scores(b + L::kBlock, s[1]);
+      if (pg * kPage + 2 * kPage - 1 > all_see) {
+        mask(s[0], pg * kPage, see_base, see_step);
+        mask(s[1], pg * kPage + kPage, see_base, see_step);
+      }
       softmax(std::integral_constant<int, 2>{}, s, pb);
       cached_values(b, pb[0]);
       cached_values(b + L::kBlock, pb[1]);
     } else {
       float s[1][NT][4];
       uint32_t pb[1][NT][2];
-      cached_scores(b, pg * kPage, s[0]);
+      cached_scores(b, s[0]);
+      mask(s[0], pg * kPage, see_base, see_step);
       softmax(std::integral_constant<int, 1>{}, s, pb);
       cached_values(b, pb[0]);
     }
