@@ -186,8 +186,8 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
  *
  * A plan is a batch of steps over one cache, staged on the device once and used for every layer: the new tokens' places, their
  * rotary table (cos and sin of pos * theta^(-2j/head_dim), computed in 64 bits), and the attention's work items.
- *   cs_plan_create     max_tokens sizes the rotary table ahead (0: grown on demand); max_steps is a hint. A plan belongs to
- *                      the cache and to the device that is current now; free it before the cache.
+ *   cs_plan_create     max_tokens sizes the rotary table ahead (0: grown on demand). A plan belongs to the cache and its
+ *                      device, which has to be the current one here and in every call on it; free it before the cache.
  *   cs_plan_set        lens[i] >= 1 new tokens of sequence seq_ids[i], at positions ctx_len .. ctx_len + lens[i] - 1 (host
  *                      arrays, read before the call returns). B = 0 is an empty plan. given = 0: the keys of the new tokens
  *                      are in the cache when attention runs (cs_kv_append comes first), so every sequence needs pages for
@@ -209,7 +209,7 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
 #define CS_F16 0
 #define CS_BF16 1
 typedef struct cs_plan cs_plan;
-int cs_plan_create(cs_kv* kv, int max_steps, int max_tokens, cs_plan** out);
+int cs_plan_create(cs_kv* kv, int max_tokens, cs_plan** out);
 int cs_plan_set(cs_plan* plan, const int32_t* seq_ids, const int32_t* lens, int B, int given, void* stream);
 int cs_plan_free(cs_plan* plan);
 int cs_kv_commit(cs_plan* plan);
@@ -235,7 +235,8 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  * over the ctx_len cached keys of the token's sequence and the step's own keys up to the token itself.
  *   q                  device rows [T, n_q_heads, head_dim], already turned.
  *   k_new, v_new       device rows [T, n_kv_heads, head_dim] of the new tokens (keys turned), for a plan with given = 1; NULL
- *                      for given = 0, where they are read from the cache.
+ *                      for given = 0, where they are read from the cache. Non-finite values count as cs_kv_append stores them
+ *                      (no token's row can spoil the tokens in front of it).
  *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
  *   scale              0: 1 / sqrt(head_dim); else > 0 and finite.
  * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; queries up to 2047 in magnitude),

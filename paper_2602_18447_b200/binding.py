@@ -72,7 +72,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "cs_kv_alloc": (C.c_int, [vp, i32, i32, i32, i32, vp, C.POINTER(vp)]),
         "cs_kv_alloc_8bit": (C.c_int, [vp, i32, i32, i32, i32, i32, C.POINTER(vp)]),
         "cs_kv_alloc_4bit": (C.c_int, [vp, i32, i32, i32, i32, C.POINTER(vp)]),
-        "cs_plan_create": (C.c_int, [vp, i32, i32, C.POINTER(vp)]),
+        "cs_plan_create": (C.c_int, [vp, i32, C.POINTER(vp)]),
         "cs_plan_set": (C.c_int, [vp, vp, vp, i32, i32, vp]),
         "cs_plan_free": (C.c_int, [vp]),
         "cs_kv_commit": (C.c_int, [vp]),
@@ -262,8 +262,8 @@ def _dtype_code(t) -> int:
 
 def _rows(t, like=None):
     """(device address, elements between rows) of a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim] whose rows are
-    contiguous; the rows themselves may lie apart (a slice of a fused projection). `like`: a tensor whose type and row count
-    it has to have."""
+    contiguous; the rows themselves may lie apart (a slice of a fused projection). `like`: a tensor whose type, device and row
+    count it has to have; without one, the current device."""
     if t is None:
         return None, 0
     shape, stride = t.shape, t.stride()
@@ -273,16 +273,20 @@ def _rows(t, like=None):
     n = shape[0]
     if n and (stride[-1] != 1 or (nd == 3 and stride[1] != shape[2] and shape[1] != 1)):
         raise ValueError("the heads of a row have to be contiguous")
-    if like is not None and (t.dtype != like.dtype or n != like.shape[0] or t.get_device() != like.get_device()):
+    if like is None:
+        import torch
+        if t.get_device() != torch.cuda.current_device():
+            raise ValueError("the rows have to be on the current device")
+    elif t.dtype != like.dtype or n != like.shape[0] or t.get_device() != like.get_device():
         raise ValueError("the rows of one call have one type, one device and one count")
     if n > 1:
         return t.data_ptr(), stride[0]
     return t.data_ptr(), max(shape[1] * (shape[2] if nd == 3 else 1), stride[0])      # the stride of one row says nothing
 
 
-def cs_plan_create(kv: int, max_steps: int = 0, max_tokens: int = 0) -> int:
+def cs_plan_create(kv: int, max_tokens: int = 0) -> int:
     out = C.c_void_p()
-    _check(load_library().cs_plan_create(kv, max_steps, max_tokens, C.byref(out)), "cs_plan_create")
+    _check(load_library().cs_plan_create(kv, max_tokens, C.byref(out)), "cs_plan_create")
     return out.value
 
 

@@ -136,6 +136,7 @@ struct cs_model {
 struct cs_kv {
   const cs_model* model;
   int num_pages, page_size, max_seqs, max_pages_per_seq;
+  int device = 0;
   uint16_t* pool = nullptr;   // 16-bit cells (bf16 values in the fp16 encoding), or 8-bit codes when format == 1
   bool own_pool = false;
   // CS_KV_FMT_*: 16-bit cells, 8-bit codes (CS_KV_E4M3 / CS_KV_E5M2; read-only for the pass), or 4-bit blocks (kv4.cuh:
@@ -1129,8 +1130,11 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
   const uint64_t rows = static_cast<uint64_t>(m->d.n_layers) * 2 * num_pages * m->d.n_kv_heads * page_size;
   if (rows >= (1ull << 31)) return CS_EINVAL;
   if (dev_pool && (reinterpret_cast<uintptr_t>(dev_pool) & 255)) return CS_EINVAL;
+  int dev = 0;
+  CS_CUDA(cudaGetDevice(&dev));
   cs_kv* kv = new (std::nothrow) cs_kv();
   if (!kv) return CS_ENOMEM;
+  kv->device = dev;
   kv->model = m;
   kv->format = format;
   kv->num_pages = num_pages;
@@ -1288,12 +1292,14 @@ static bool rows_ok(const void* p, int64_t stride, int64_t row) {
   return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride >= row && stride % 8 == 0;
 }
 
-int cs_plan_create(cs_kv* kv, int max_steps, int max_tokens, cs_plan** out) {
+int cs_plan_create(cs_kv* kv, int max_tokens, cs_plan** out) {
   if (!out) return CS_EINVAL;
   *out = nullptr;
-  if (!kv || max_steps < 0 || max_tokens < 0 || max_tokens > (1 << 24)) return CS_EINVAL;
+  if (!kv || max_tokens < 0 || max_tokens > (1 << 24)) return CS_EINVAL;
   int dev = 0;
   CS_CUDA(cudaGetDevice(&dev));
+  if (dev != kv->device) return CS_EINVAL;
+  if (kv->format == CS_KV_FMT_INT4) CS_CUDA(prepare_attention_4bit(kv->model->d.head_dim));
   cs_plan* p = new (std::nothrow) cs_plan();
   if (!p) return CS_ENOMEM;
   p->kv = kv;
@@ -1602,8 +1608,10 @@ int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_
     return CS_EINVAL;
   if (T == 0) return CS_OK;
   if (!tok_seq || !tok_pos || !rows_ok(out_k, 8, 8) || !rows_ok(out_v, 8, 8)) return CS_EINVAL;
+  int dev = 0, rc;
+  CS_CUDA(cudaGetDevice(&dev));
+  if (dev != kv->device) return CS_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  int rc;
   if ((rc = table_ready(kv, s))) return rc;
   const cs_model_desc& d = kv->model->d;
   const uint8_t* pool = reinterpret_cast<const uint8_t*>(kv->pool);

@@ -106,6 +106,12 @@ __device__ __forceinline__ uint32_t centred_high(uint32_t w) { return hadd2_u(co
 __device__ __forceinline__ uint4 as_f16(uint4 v, bool bf16) {
   return bf16 ? make_uint4(bf16x2_to_f16x2(v.x), bf16x2_to_f16x2(v.y), bf16x2_to_f16x2(v.z), bf16x2_to_f16x2(v.w)) : v;
 }
+// The same for own keys and values, held as the cache would hold them: NaN counts as 0 and magnitudes saturate, because a token's
+// row is multiplied by the zero probabilities of the tokens in front of it.
+__device__ __forceinline__ uint4 as_held(uint4 v, bool bf16) {
+  v = as_f16(v, bf16);
+  return make_uint4(finite_f16x2(v.x), finite_f16x2(v.y), finite_f16x2(v.z), finite_f16x2(v.w));
+}
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 __device__ __forceinline__ void store_out(const Attn4Params& p, size_t at, float v) {
@@ -471,7 +477,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       const int key = c / CH, ch = c % CH;
       uint4 v = make_uint4(0, 0, 0, 0);
       if (key0 + key < it.n_new)
-        v = as_f16(*reinterpret_cast<const uint4*>(p.v_new + (it.tok0 + key0 + key) * p.kv_stride + it.kv_head * HD + ch * 8),
+        v = as_held(*reinterpret_cast<const uint4*>(p.v_new + (it.tok0 + key0 + key) * p.kv_stride + it.kv_head * HD + ch * 8),
                    p.in_bf16 != 0);
       *reinterpret_cast<uint4*>(own_v + key * HD * 2 + ((ch ^ (key & 7)) << 4)) = v;
     }
@@ -490,7 +496,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
           const int key = key0 + g + 8 * j;
           x[j] = make_uint4(0, 0, 0, 0);
           if (key < it.n_new)
-            x[j] = as_f16(*reinterpret_cast<const uint4*>(p.k_new + (it.tok0 + key) * p.kv_stride + it.kv_head * HD + grp * 64 +
+            x[j] = as_held(*reinterpret_cast<const uint4*>(p.k_new + (it.tok0 + key) * p.kv_stride + it.kv_head * HD + grp * 64 +
                                                           q * 16 + w * 8), p.in_bf16 != 0);
         }
         const uint32_t a0[4] = {x[0].x, x[1].x, x[0].y, x[1].y}, a1[4] = {x[0].z, x[1].z, x[0].w, x[1].w};
@@ -679,10 +685,14 @@ __global__ void __launch_bounds__(HD) attention_4bit_merge_kernel(const Attn4Par
 }
 
 template <int HD, int NT>
-cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, cudaStream_t s) {
+cudaError_t opt_in() {
   static std::atomic<uint64_t> smem_opted{0};
-  if (cudaError_t e = opt_in_dynamic_smem(attention_4bit_kernel<HD, NT>, Smem4<HD, NT>::kTotal, smem_opted); e != cudaSuccess)
-    return e;
+  return opt_in_dynamic_smem(attention_4bit_kernel<HD, NT>, Smem4<HD, NT>::kTotal, smem_opted);
+}
+
+template <int HD, int NT>
+cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, cudaStream_t s) {
+  if (cudaError_t e = opt_in<HD, NT>(); e != cudaSuccess) return e;
   cudaError_t e = p.cluster > 1 ? launch_pdl_cluster(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads),
                                                      Smem4<HD, NT>::kTotal, s, p.cluster, p, items)
                                 : launch_pdl(attention_4bit_kernel<HD, NT>, dim3(n_items), dim3(kThreads), Smem4<HD, NT>::kTotal, s,
@@ -700,6 +710,12 @@ cudaError_t launch_4bit(const Attn4Params& p, const AttnItem* items, int n_items
 // pages in L2. (Tiles of 32 rows need 255 registers and two CTAs per SM: 28 rows over 83 K keys x 4 heads took 99 us, as two
 // tiles of 16 45 us.)
 int attention_4bit_row_tile(int max_rows) { return max_rows <= 8 ? 8 : 16; }
+
+cudaError_t prepare_attention_4bit(int head_dim) {
+  cudaError_t e = head_dim == 128 ? opt_in<128, 1>() : opt_in<64, 1>();
+  if (e == cudaSuccess) e = head_dim == 128 ? opt_in<128, 2>() : opt_in<64, 2>();
+  return e;
+}
 
 int attention_4bit_ctas_per_sm(int row_tile) { return ctas_per_sm(row_tile / 8); }
 

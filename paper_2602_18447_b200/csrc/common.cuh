@@ -200,6 +200,15 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t v) {
   const float2 f = unpack_f16x2(v);
   return pack_bf16x2(f.x, f.y);
 }
+// Two fp16 values with NaN as 0 and infinities as the largest finite magnitude.
+__device__ __forceinline__ uint32_t finite_f16x2(uint32_t v) {
+  const __half2 x = *reinterpret_cast<const __half2*>(&v);
+  v &= __heq2_mask(x, x);
+  const uint32_t hi = 0x7BFF7BFFu, lo = 0xFBFFFBFFu;
+  const __half2 r = __hmax2(__hmin2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&hi)),
+                            *reinterpret_cast<const __half2*>(&lo));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); }
 

@@ -173,6 +173,8 @@ struct Attn4Params {
 // of the step's first token.
 int attention_4bit_row_tile(int max_rows);
 int attention_4bit_ctas_per_sm(int row_tile);
+// What the kernels need once per device before a launch inside a stream capture.
+cudaError_t prepare_attention_4bit(int head_dim);
 constexpr int kAttn4MaxPieces = 64;      // a context is cut into at most this many pieces (the joining kernel: two per lane)
 // items[0 .. n_items): the work; items[n_items .. n_items + n_merge): one item (any piece) of every range that was cut.
 cudaError_t launch_attention_4bit(const Attn4Params& p, const AttnItem* items, int n_items, int n_merge, int row_tile,

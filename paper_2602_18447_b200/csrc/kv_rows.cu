@@ -587,7 +587,7 @@ __global__ void __launch_bounds__(128) kv_blocks_kernel(const uint8_t* __restric
 }
 
 // Up to three row sources side by side into one matrix, in 16-byte pieces, fp16 or bf16 on either side (bf16 -> fp16 is exact for
-// magnitudes in [2^-14, 65504]).
+// magnitudes in [2^-14, 65504]). Sources behind the first are keys and values: non-finite ones are held as the cache holds them.
 template <bool FROM_BF16, bool TO_BF16>
 __global__ void rows_copy_kernel(const RowsCopy p, int64_t total) {
   pdl_launch_dependents();
@@ -601,6 +601,9 @@ __global__ void rows_copy_kernel(const RowsCopy p, int64_t total) {
     const int at = c - (which > 0 ? p.cols[0] : 0) - (which > 1 ? p.cols[1] : 0);
     float x[8];
     widen8<FROM_BF16>(*reinterpret_cast<const uint4*>(p.src[which] + row * p.stride[which] + at * 8), x);
+    if (which > 0)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = storable(x[j], kF16Max);
     *reinterpret_cast<uint4*>(p.dst + row * p.dst_stride + c * 8) = narrow8<TO_BF16>(x);
   }
 }

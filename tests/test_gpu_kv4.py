@@ -217,6 +217,13 @@ def _attention_case(hq, hkv, hd, ctx, lens, given, dtype, q_scale=1.0, kv_scale=
         c.B.cs_attention_4bit(c.plan, 0, q, out, *new, scale=scale)
         torch.cuda.synchronize()
         assert torch.equal(first, out)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.B.cs_attention_4bit(c.plan, 0, q, out, *new, scale=scale)
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(first, out)
         c.B.cs_last_status(c.model)
     got = _np(out)
     (ck, sk, ok), (cv, sv, ov) = K.quantise(_np(kc)), K.quantise(_np(vc))
@@ -252,6 +259,14 @@ def test_attention_steps_of_every_length(hq, hkv, hd, dtype, given):
     contexts down to nothing."""
     for lens in ([1, 2, 1, 1], [1, 2, 3, 2], [5, 4, 1, 3], [8, 1, 3, 13], [8, 1, 17, 100]):
         _attention_case(hq, hkv, hd, [0, 7, 48, 130], lens, given, dtype, seed=sum(lens))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ctx", [[100], [600], [1500, 40], [250, 3, 700]])
+def test_attention_of_few_contexts_shared_by_clusters(ctx, hd):
+    """One to three conversations: the pieces of a context are the CTAs of one cluster (2, 4 or 8 of them)."""
+    _attention_case(12, 2, hd, ctx, [1] * len(ctx), False, "float16")
+    _attention_case(6, 2, hd, ctx, [5] * len(ctx), True, "bfloat16")
 
 
 @pytest.mark.parametrize("given", [False, True])
@@ -293,6 +308,37 @@ def test_attention_reads_nothing_behind_a_sequence():
             assert bool((out[1:] == 5.0).all()) and bool(torch.isfinite(out).all())
             outs.append(out.clone())
     assert torch.equal(*outs)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("n", [6, 40])                                  # 12 and 120 query rows: the 4-bit and the expanded form
+def test_a_token_does_not_meet_what_later_tokens_hold(n, dtype):
+    """Given keys and values of the later tokens of a step are NaN and infinite: the earlier tokens' outputs are the same bits as
+    with finite ones, and the later tokens' are what the saturated values give."""
+    import torch
+    rng = np.random.default_rng(11)
+    with K.Cache(6, 2, 128, n_seqs=1) as c:
+        c.B.cs_plan_set(c.plan, [0], [33])
+        c.B.cs_kv_append(c.plan, 0, *(_rows(rng, 33, 2, 128, dtype) for _ in range(2)))
+        c.B.cs_kv_commit(c.plan)
+        q, k, v = _rows(rng, n, 6, 128, dtype), _rows(rng, n, 2, 128, dtype), _rows(rng, n, 2, 128, dtype)
+        c.B.cs_plan_set(c.plan, [0], [n], given=True)
+        clean, out = torch.empty_like(q), torch.empty_like(q)
+        c.B.cs_attention_4bit(c.plan, 0, q, clean, k, v)
+        most = 65504.0 if dtype == "float16" else 65280.0
+        bad_v, held_v, bad_k = v.clone(), v.clone(), k.clone()
+        for at, value, held in (((3, 0, 5), float("nan"), 0.0), ((4, 1, 6), float("inf"), most), ((5, 0, 7), float("-inf"), -most)):
+            bad_v[at], held_v[at] = value, held
+        bad_k[4, 0, 0] = float("nan")
+        c.B.cs_attention_4bit(c.plan, 0, q, out, bad_k, bad_v)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:3], clean[:3]) and bool(torch.isfinite(out).all())
+        held_k = k.clone()
+        held_k[4, 0, 0] = 0.0
+        c.B.cs_attention_4bit(c.plan, 0, q, clean, held_k, held_v)
+        torch.cuda.synchronize()
+        # bf16 has no 65504: an infinity saturates at fp16's largest value, 0.35% above the 65280 compared with
+        assert float((out.double() - clean.double()).abs().max()) <= (0.0 if dtype == "float16" else 0.02 * most)
 
 
 @pytest.mark.parametrize("dtype", ["float16", "bfloat16"])

@@ -15,7 +15,7 @@ def test_null_handles_are_refused(B):
     lib, out = B.load_library(), ctypes.c_void_p(5)
     assert lib.cs_kv_alloc_4bit(None, 4, 16, 1, 4, ctypes.byref(out)) == B.CS_EINVAL and not out.value
     out = ctypes.c_void_p(5)
-    assert lib.cs_plan_create(None, 0, 0, ctypes.byref(out)) == B.CS_EINVAL and not out.value
+    assert lib.cs_plan_create(None, 0, ctypes.byref(out)) == B.CS_EINVAL and not out.value
     assert lib.cs_plan_set(None, None, None, 0, 0, None) == B.CS_EINVAL
     assert lib.cs_plan_free(None) == B.CS_OK
     assert lib.cs_kv_commit(None) == B.CS_EINVAL
