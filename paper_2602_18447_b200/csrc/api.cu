@@ -247,17 +247,17 @@ constexpr double kAttnMergeFixed = 1.0;
 constexpr double kAttnMergePerSplit = 0.5;
 
 // 4-bit attention, in pages of one CTA among as many as fit on its SM (0.28 us at 8 query rows): the smallest piece worth an item
-// of its own; what an item costs besides its pages (alone 3.2 us from launch to end, most of it latencies in a row; counted higher
-// because long pieces proved faster wherever there is more than one wave: 64 contexts of 2 K to 8 K keys 66.9 us with 28, 69.4 with
-// 12); what joining pieces adds to a
-// launch, by a second kernel or inside a cluster.
+// of its own; the pages of a round; what an item costs besides its pages (alone 2.6 us from launch to end, most of it latencies in a
+// row; counted higher because long pieces proved faster wherever there is more than one wave: 64 contexts of 2 K to 8 K keys 66.9 us
+// with 28, 69.4 with 12); what joining pieces adds to a launch, by a second kernel or inside a cluster.
 constexpr int kAttn4MinPages = 8;
+constexpr int kAttn4Round = 8;
 constexpr double kAttn4Fixed = 28;
 constexpr double kAttn4Join = 8;
-constexpr double kAttn4ClusterJoin = 3;
+constexpr double kAttn4ClusterJoin = 5;
 // Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves, once per 16
 // rows; a batch with a longer one has its contexts expanded to fp16 for the tensor-core kernel. Measured, 64 contexts of 2 K to
-// 8 K keys x 8 heads: 64 rows 402 us against 592, 96 rows 594 against 597; 8 contexts of 1 K to 4 K keys x 4 heads: 84 rows 33
+// 8 K keys x 8 heads: 64 rows 379 us against 592, 96 rows 561 against 597; 8 contexts of 1 K to 4 K keys x 4 heads: 84 rows 31
 // against 42, up to 672 rows 110 against 67.
 constexpr int kAttn4MaxRows = 96;
 
@@ -419,7 +419,12 @@ Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const i
       longest = std::max(longest, pages);
     }
   const int fit = attention_4bit_ctas_per_sm(w.row_tile), slots = kNumSMs * fit;
-  auto pieces = [](int pages, int cap) { return std::min<int>(cs::kAttn4MaxPieces, (pages + cap - 1) / cap); };
+  // Pieces of a range are alike and whole rounds of a CTA (kAttn4Round pages: its warps take two each), but for the last one.
+  auto whole_rounds = [](int pages) { return (pages + kAttn4Round - 1) / kAttn4Round * kAttn4Round; };
+  auto piece_pages = [&](int pages, int cap) {
+    const int n = std::min<int>(cs::kAttn4MaxPieces, (pages + cap - 1) / cap);
+    return whole_rounds((pages + n - 1) / n);
+  };
   // the heads of a unit cost the same: one head's items on the slots' share
   const double machines = std::max(1.0, static_cast<double>(slots) / heads);
   std::vector<double> cost;
@@ -428,12 +433,13 @@ Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const i
     double longest_item = 0.0, sum = 0.0;
     bool cut = false;
     for (const Unit& u : units) {
-      const int n = pieces(u.pages, cap);
-      cut = cut || n > 1;
-      const double c = kAttn4Fixed + static_cast<double>(u.pages) / n;
-      for (int s = 0; s < n; ++s) cost.push_back(c);
-      longest_item = std::max(longest_item, c);
-      sum += n * c;
+      const int piece = piece_pages(u.pages, cap);
+      cut = cut || u.pages > piece;
+      for (int at = 0; at < u.pages; at += piece) {
+        cost.push_back(kAttn4Fixed + whole_rounds(std::min(piece, u.pages - at)));
+        longest_item = std::max(longest_item, cost.back());
+        sum += cost.back();
+      }
     }
     const double join = cut ? kAttn4Join : 0.0;
     if (cost.size() <= machines) {
@@ -449,7 +455,7 @@ Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const i
   double best = estimate(longest, 1e300);
   int last_cap = longest;
   auto consider = [&](int cap) {
-    cap = std::max(cap, kAttn4MinPages);
+    cap = whole_rounds(std::max(cap, kAttn4MinPages));
     if (cap >= last_cap) return;
     last_cap = cap;
     const double e = estimate(cap, best);
@@ -479,11 +485,10 @@ Attn4Work build_4bit_work(const cs_model* m, int B, const int32_t* lens, const i
   }
   std::vector<AttnItem> merge;
   for (const Unit& u : units) {
-    const int n = pieces(u.pages, best_cap);
+    const int piece = piece_pages(u.pages, best_cap), n = (u.pages + piece - 1) / piece;
     for (int h = 0; h < heads; ++h) {
       for (int s = 0; s < n; ++s) {
-        const int b = static_cast<int>(static_cast<long>(u.pages) * s / n);
-        const int e = static_cast<int>(static_cast<long>(u.pages) * (s + 1) / n);
+        const int b = s * piece, e = std::min(u.pages, b + piece);
         w.items.push_back(AttnItem{u.step, h, u.row0, b, e, n > 1 ? w.n_slots + s : 0, n > 1 ? w.n_slots : 0, n, 0, lens[u.step],
                                    ctx[u.step], 0, {0, u.cached, 0, 0}});
       }
