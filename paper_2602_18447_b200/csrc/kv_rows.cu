@@ -98,22 +98,23 @@ __device__ __forceinline__ void group_params(float lo, float hi, __half& scale, 
 // The codes of eight channels. code[i]: kRoundBits + the code.
 __device__ __forceinline__ void codes8(const float (&v)[8], __half scale, __half offset, uint32_t (&code)[8]) {
   const float s = __half2float(scale), o = __half2float(offset);
-  const float inv = s > 0.f ? __fdividef(1.f, s) : 0.f;
+  const float inv15 = s > 0.f ? __fdividef(1.f / 15.f, s) : 0.f;
   float r[8], worst = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float d = __fsub_rn(v[i], o);
-    r[i] = __fmaf_rn(d, inv, kRound);
-    worst = fmaxf(worst, fabsf(__fmaf_rn(d, inv, -__fsub_rn(r[i], kRound))));
+    const float u = __saturatef(__fmul_rn(__fsub_rn(v[i], o), inv15));       // the share of the range, 0 .. 1: clamped for nothing
+    r[i] = __fmaf_rn(u, 15.f, kRound);
+    worst = fmaxf(worst, fabsf(__fmaf_rn(u, 15.f, -__fsub_rn(r[i], kRound))));
   }
-  // The reciprocal is off by 2^-22 of itself, which moves a quotient of up to 15.5 by less than 4e-6: only that close to a border
-  // does the quotient itself have to decide.
+  // The reciprocal's 2^-22 and two roundings of 2^-24 move a quotient of up to 15 by less than 6e-6: only that close to a border does
+  // the quotient itself have to decide.
   if (worst > 0.49999f && s > 0.f) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r[i] = __fadd_rn(__fdiv_rn(__fsub_rn(v[i], o), s), kRound);
+    for (int i = 0; i < 8; ++i)
+      r[i] = fminf(fmaxf(__fadd_rn(__fdiv_rn(__fsub_rn(v[i], o), s), kRound), kRound), kRound + 15.f);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) code[i] = __float_as_uint(fminf(fmaxf(r[i], kRound), kRound + 15.f));
+  for (int i = 0; i < 8; ++i) code[i] = __float_as_uint(r[i]);
 }
 // The codes of a thread's two chunks (eight channels each, half a head apart) and the parameters of their groups, which for
 // HD = 64 are one. NaN, infinities and what the format cannot hold are rare: the whole warp goes round again with storable values.
