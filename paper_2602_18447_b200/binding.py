@@ -143,11 +143,23 @@ def _dev_ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+_torch = None
+
+
+def _t():
+    """torch, imported at the first call that needs it (an import statement in every call costs more than what it is for)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
 def _stream_ptr(stream) -> Optional[int]:
     if stream is None:
-        import torch
+        t = _torch or _t()
         # the current stream's handle without the Stream object around it (0.1 us instead of 3)
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return t._C._cuda_getCurrentRawStream(t.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -252,7 +264,7 @@ _dtype_codes: dict = {}
 
 def _dtype_code(t) -> int:
     if not _dtype_codes:
-        import torch
+        torch = _t()
         _dtype_codes.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16})
     code = _dtype_codes.get(t.dtype)
     if code is None:
@@ -274,8 +286,7 @@ def _rows(t, like=None):
     if n and (stride[-1] != 1 or (nd == 3 and stride[1] != shape[2] and shape[1] != 1)):
         raise ValueError("the heads of a row have to be contiguous")
     if like is None:
-        import torch
-        if t.get_device() != torch.cuda.current_device():
+        if t.get_device() != (_torch or _t()).cuda.current_device():
             raise ValueError("the rows have to be on the current device")
     elif t.dtype != like.dtype or n != like.shape[0] or t.get_device() != like.get_device():
         raise ValueError("the rows of one call have one type, one device and one count")
@@ -328,7 +339,7 @@ def cs_attention_4bit(plan: int, layer: int, q, out, k_new=None, v_new=None, sca
 
 def cs_kv_read(kv: int, layer: int, tok_seq, tok_pos, out_k, out_v, stream=None) -> None:
     """tok_seq, tok_pos: CUDA int32 tensors [T]; out_k, out_v: contiguous CUDA tensors [T, n_kv_heads, head_dim] of one type."""
-    import torch
+    torch = _torch or _t()
     if tok_seq.dtype != torch.int32 or tok_pos.dtype != torch.int32 or tok_seq.shape != tok_pos.shape:
         raise ValueError("tok_seq and tok_pos are int32 tensors of one length")
     if out_k.dtype != out_v.dtype or out_k.shape != out_v.shape or out_k.shape[0] != tok_seq.shape[0]:
