@@ -188,10 +188,10 @@ __device__ __forceinline__ void put_v4(uint8_t* dst, int slot, int c, uint32_t o
 // One CTA: the tokens of one block (consecutive positions of one page). A thread has two chunks of eight channels half a head apart,
 // which turn against each other, of one token, and loops over the CTA's share of the heads with the token's cosines and sines in
 // registers and the next head's rows on their way. blockIdx.y < kv_parts: K and V heads; behind them, query heads.
-// Bound by memory and instructions alike: 4-bit rows of 20 K tokens x 8 heads with 16 query heads (0.28 GB in and out) take
-// 69 us, 0.63 of the copy bandwidth; 16-bit ones of 2 heads with 12 query heads (0.2 GB) 34 us, 0.89. What counted: two chunks a thread (no exchange between lanes for the turn), rounding by
-// addition with one border check for eight channels (a rounding, range check and branch per channel: 140 us), whole pages through
-// shared memory.
+// Bound by memory and instructions alike: 4-bit rows of 22.9 K tokens x 8 heads with 16 query heads (0.32 GB in and out) take
+// 69 us, 0.71 of the copy bandwidth; 16-bit ones of 2 heads with 12 query heads (0.2 GB) 34.7 us, 0.88. What counted: two chunks a
+// thread (no exchange between lanes for the turn), rounding by addition with one border check for eight channels (a rounding, range
+// check and branch per channel: 140 us), whole pages through shared memory.
 template <int HD, int FMT, bool BF16>
 __global__ void __launch_bounds__(HD, 640 / HD) kv_append_kernel(const KvAppendParams p) {
   constexpr int CH = HD / 8, HALF = CH / 2;          // chunks of a row; threads of a token
@@ -493,9 +493,8 @@ __global__ void __launch_bounds__(2 * HD) kv_read_kernel(const KvReadParams p) {
 }
 
 // The same out of a 4-bit cache. ROWS listed rows a CTA: runs of rows that climb through one page are found first, then a warp takes a
-// run and reads its block's words once for all of them (a V code by itself is half a byte; row by row took 44 us for 20 K rows x 8
-// heads, by runs 26 us, 0.63 of
-// the copy bandwidth).
+// run and reads its block's words once for all of them (a V code by itself is half a byte; row by row took 44 us for 22.9 K
+// rows x 8 heads, by runs 26 us, 0.72 of the copy bandwidth).
 template <int HD, bool BF16, int ROWS, int THREADS>
 __global__ void __launch_bounds__(THREADS) kv_read4_kernel(const KvReadParams p) {
   static_assert(ROWS <= 64 && THREADS >= ROWS, "one thread per row, two ballots");
