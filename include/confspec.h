@@ -195,8 +195,11 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
  *                      read up to ctx_len only (the same sequence may then appear several times, as in cs_verify_steps).
  *                      Uploads on `stream`; growing a buffer synchronises the device. Not inside a stream capture (CS_ESTATE).
  *   cs_kv_commit       host only: the plan's tokens become context (ctx_len += lens[i]), once per cs_plan_set and after the
- *                      last layer's append has been issued. CS_ESTATE if the plan is not set or already committed, or if a
- *                      sequence's ctx_len has changed since.
+ *                      last layer's append has been issued. CS_ESTATE if the plan is not set or already committed.
+ * A plan stands for the sequences as they were at its cs_plan_set. Once cs_kv_set_seq has set one of them anew, every call on the
+ * plan returns CS_ESTATE (its pages may be another sequence's by now); once another call has lengthened a context,
+ * cs_kv_append and cs_kv_commit do (they would overwrite those tokens), while cs_attention_4bit still sees the context of
+ * cs_plan_set. Setting the plan again clears this. Replays of a graph are not checked.
  * Calls on a plan read its device buffers: issue them on the stream of its cs_plan_set, or order the streams yourself, and one
  * at a time (cs_attention_4bit keeps partial results in the plan). They may be captured into a CUDA graph once the page table
  * is on the device (cs_plan_set uploads it; CS_ESTATE if cs_kv_set_seq came after it): a replay does the plan's work as it

@@ -147,6 +147,8 @@ struct cs_kv {
   int32_t* table_host = nullptr;  // pinned [max_seqs, max_pages_per_seq]
   int32_t* table_dev = nullptr;
   std::vector<int32_t> ctx_len, n_pages;  // per sequence; ctx_len < 0 = not set
+  std::vector<uint64_t> set_count;        // how often cs_kv_set_seq has set the sequence
+  uint64_t changes = 0;                   // of any sequence's pages or context
   bool dirty = true;
   cudaEvent_t upload_ev = nullptr;
   bool upload_pending = false;
@@ -164,6 +166,8 @@ struct cs_plan {
   int B = 0, T = 0, n_blocks = 0, n_items = 0, n_merge = 0, row_tile = 8, cluster = 1;
   size_t off_pos = 0, off_blocks = 0, off_items = 0;      // int32 offsets into the staged block
   std::vector<int32_t> seqs, lens, ctx;
+  std::vector<uint64_t> set_count;       // the sequences' counts at cs_plan_set
+  uint64_t changes = 0;                  // kv->changes up to which they are known to be as they were
   Staging stg;
   DevBuf rope, part_o, part_ml;
   // steps of many query rows: expanded context pages, the fused fp16 matrix and output of the tensor-core attention, its counters
@@ -1149,6 +1153,7 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
   kv->plane_elems = static_cast<size_t>(num_pages) * m->d.n_kv_heads * page_size * m->d.head_dim;
   kv->ctx_len.assign(max_seqs, -1);
   kv->n_pages.assign(max_seqs, 0);
+  kv->set_count.assign(max_seqs, 0);
   const uint64_t bytes = format == CS_KV_FMT_INT4 ? kv->layer4_bytes() * m->d.n_layers
                                                   : cs_kv_pool_bytes(m, num_pages, page_size) / (format != 0 ? 2 : 1);
   int rc = CS_OK;
@@ -1224,6 +1229,8 @@ int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int 
   for (int i = 0; i < n_pages; ++i) row[i] = page_ids[i];
   kv->ctx_len[seq] = ctx_len;
   kv->n_pages[seq] = n_pages;
+  ++kv->set_count[seq];
+  ++kv->changes;
   kv->dirty = true;
   return CS_OK;
 }
@@ -1452,6 +1459,9 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
   p->seqs.assign(seq_ids, seq_ids + B);
   p->lens.assign(lens, lens + B);
   p->ctx = ctx;
+  p->set_count.resize(B);
+  for (int i = 0; i < B; ++i) p->set_count[i] = kv->set_count[seq_ids[i]];
+  p->changes = kv->changes;
   p->set = true;
   return CS_OK;
 }
@@ -1473,6 +1483,22 @@ static int plan_ready(const cs_plan* p, int layer, int dtype) {
   return p->set ? CS_OK : CS_ESTATE;
 }
 
+// A plan's places stand only while its sequences have the pages that they had: through a table that has changed since, an append
+// would write into pages that may be another sequence's by now. An append also refuses contexts that another call has lengthened,
+// whose tokens it would overwrite.
+static bool plan_stands(cs_plan* p, bool appends) {
+  const cs_kv* kv = p->kv;
+  if (p->changes == kv->changes) return true;
+  bool same_context = true;
+  for (int i = 0; i < p->B; ++i) {
+    const int seq = p->seqs[i];
+    if (kv->set_count[seq] != p->set_count[i]) return false;
+    same_context = same_context && kv->ctx_len[seq] == p->ctx[i] + (p->committed ? p->lens[i] : 0);
+  }
+  if (same_context) p->changes = kv->changes;
+  return same_context || !appends;
+}
+
 int cs_kv_append(cs_plan* p, int layer, const uint16_t* k, int64_t k_stride, const uint16_t* v, int64_t v_stride,
                  const uint16_t* q, int64_t q_stride, uint16_t* q_out, int64_t q_out_stride, int rotate, int dtype,
                  void* stream) {
@@ -1480,6 +1506,7 @@ int cs_kv_append(cs_plan* p, int layer, const uint16_t* k, int64_t k_stride, con
   if ((rc = plan_ready(p, layer, dtype))) return rc;
   const cs_model_desc& d = p->kv->model->d;
   if (!p->appendable || (q == nullptr) != (q_out == nullptr) || (q && !rotate)) return CS_EINVAL;
+  if (!plan_stands(p, true)) return CS_ESTATE;
   if (p->T == 0) return CS_OK;
   const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
   if (!rows_ok(k, k_stride, kv_row) || !rows_ok(v, v_stride, kv_row)) return CS_EINVAL;
@@ -1507,12 +1534,10 @@ int cs_kv_commit(cs_plan* p) {
   if (!p->set || p->committed) return CS_ESTATE;
   if (!p->appendable) return CS_EINVAL;
   cs_kv* kv = p->kv;
-  for (int i = 0; i < p->B; ++i)               // a sequence that was set anew since
-    if (kv->ctx_len[p->seqs[i]] != p->ctx[i] ||
-        static_cast<long>(p->ctx[i]) + p->lens[i] > static_cast<long>(kv->n_pages[p->seqs[i]]) * kPageSize)
-      return CS_ESTATE;
+  if (!plan_stands(p, true)) return CS_ESTATE;
   for (int i = 0; i < p->B; ++i) kv->ctx_len[p->seqs[i]] += p->lens[i];
   p->committed = true;
+  ++kv->changes;
   return CS_OK;
 }
 
@@ -1571,6 +1596,7 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   const cs_model_desc& d = kv->model->d;
   if (kv->format != CS_KV_FMT_INT4 || !(scale >= 0.f) || scale > 3.0e38f) return CS_EINVAL;
   if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;
+  if (!plan_stands(p, false)) return CS_ESTATE;
   if (p->T == 0) return CS_OK;
   const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
   if (!rows_ok(q, q_stride, q_row) || !rows_ok(out, out_stride, q_row)) return CS_EINVAL;
@@ -1661,6 +1687,7 @@ int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* to
   if ((rc = upload_table(kv, s))) return rc;
   if ((rc = run_layers(m, kv, kv, L, dev_meta, dev_tok, s))) return rc;
   for (int i = 0; i < B; ++i) kv->ctx_len[seq_ids[i]] += lens[i];
+  ++kv->changes;
   return CS_OK;
 }
 

@@ -482,6 +482,56 @@ def test_decoding_step_by_step_eager_and_as_a_graph():
         side.synchronize()
 
 
+@pytest.mark.parametrize("fmt", ["int4", "16bit", "e4m3"])
+def test_a_plan_stands_only_while_its_sequences_do(fmt):
+    """Pages that a sequence has given up, and tokens that another call has committed, are not written through an older plan."""
+    import torch
+    rng = np.random.default_rng(23)
+    k, q = _rows(rng, 2, 2, 128, "float16"), _rows(rng, 2, 4, 128, "float16")
+    out = torch.zeros_like(q)
+    with K.Cache(4, 2, 128, n_seqs=2, pages_each=2, fmt=fmt) as c:
+        B = c.B
+        other = B.cs_plan_create(c.kv)
+
+        def refused(fn, *a):
+            B.cs_take_launch_count()
+            with pytest.raises(B.ConfSpecError) as e:
+                fn(*a)
+            assert e.value.status == B.CS_ESTATE and B.cs_take_launch_count() == 0
+
+        c.set([17, 0])
+        B.cs_plan_set(c.plan, [0], [2])
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0][:1], 16)                      # its second page goes ...
+        B.cs_kv_set_seq(c.kv, 1, c.pages[0][1:], 0)                       # ... to the other sequence
+        B.cs_plan_set(other, [1], [2])
+        B.cs_kv_append(other, 0, k, k, None, None, False)
+        held = c.read([1, 1], [0, 1])
+        refused(B.cs_kv_append, c.plan, 0, -k, -k, None, None, False)
+        if fmt == "int4":
+            refused(B.cs_attention_4bit, c.plan, 0, q, out)
+        refused(B.cs_kv_commit, c.plan)
+        assert all(np.array_equal(x, y) for x, y in zip(held, c.read([1, 1], [0, 1])))
+        # a sequence that is not the plan's may change; the plan's own commit leaves it standing
+        B.cs_kv_set_seq(c.kv, 0, c.pages[1], 3)
+        B.cs_kv_append(other, 0, k, k, None, None, False)
+        B.cs_kv_commit(other)
+        B.cs_kv_append(other, 0, k, k, None, None, False)
+        # another call has lengthened the context: nothing is written over its tokens, while reading goes on
+        B.cs_plan_set(c.plan, [0], [2])
+        B.cs_plan_set(other, [0], [2])
+        B.cs_kv_append(other, 0, k, k, None, None, False)
+        B.cs_kv_commit(other)
+        refused(B.cs_kv_append, c.plan, 0, -k, -k, None, None, False)
+        refused(B.cs_kv_commit, c.plan)
+        if fmt == "int4":
+            B.cs_attention_4bit(c.plan, 0, q, out)
+        B.cs_plan_set(c.plan, [0], [2])
+        B.cs_kv_append(c.plan, 0, k, k, None, None, False)
+        B.cs_kv_commit(c.plan)
+        torch.cuda.synchronize()
+        B.cs_plan_free(other)
+
+
 def test_what_the_calls_refuse():
     import torch
     rng = np.random.default_rng(14)
