@@ -242,9 +242,13 @@ class _Handles:
             B.cs_plan_set(self.plan, some, held[some])
             B.cs_kv_append(self.plan, 0, d["cached_k"], d["cached_v"], rotate=False)
         self.set(d, d["ctx"])
-        if d["new"].sum():
-            B.cs_plan_set(self.plan, np.arange(case["B"]), d["new"], given=case.get("new") == "given")
+        self.seqs, self.lens = np.arange(case["B"], dtype=np.int32), d["new"].astype(np.int32)
+        self.given = case.get("new") == "given"
         torch.cuda.synchronize()
+
+    def set_plan(self):
+        """What a program does anew for every step's lengths, before its layers: here the one layer pays for all of it."""
+        self.B.cs_plan_set(self.plan, self.seqs, self.lens, given=self.given)
 
     def set(self, d, ctx):
         for i in range(d["case"]["B"]):
@@ -377,6 +381,8 @@ def run(state):
 
 def _run_own(state):
     case, B, h = state["case"], state["B"], state["h"]
+    if case["op"] != "read":
+        h.set_plan()
     if case["op"] == "attention":
         new = (state["k"], state["v"]) if case["new"] == "given" else (None, None)
         B.cs_attention_4bit(h.plan, 0, state["q"], state["out"], *new)
