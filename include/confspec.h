@@ -242,8 +242,8 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  *                      (no token's row can spoil the tokens in front of it).
  *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
  *   scale              0: 1 / sqrt(head_dim); else > 0 and finite.
- * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; queries up to 2047 in magnitude),
- * sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number of new tokens:
+ * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; a row with a
+ * larger query comes out as NaN), sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number of new tokens:
  * up to 96 query rows per kv head read the 4-bit pages directly; a batch with a longer step has its rows and contexts put together
  * as fp16 in the plan (values rounded to fp16 once) for the pass's tensor-core attention. Deterministic.
  */

@@ -176,7 +176,8 @@ struct Smem4 {
   static_assert((kPartBytes + kStatBytes) % 16 == 0, "the joined rows are read in 16-byte pieces");
   // from 16 query rows on, the query operands do not fit the registers beside the accumulators
   static constexpr int kQBytes = NT > 1 ? 8 * NT * HD * 2 : 0;
-  static constexpr int kTotal = kUnion + kQBytes;
+  static constexpr int kScaleBytes = kWarps * 8 * NT * 4;
+  static constexpr int kTotal = kUnion + kQBytes + kScaleBytes;
   static_assert(2 * Kv4<HD>::kBlock >= kPage * HD * 2, "a page of own values must fit in one stage");
 };
 
@@ -267,12 +268,16 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   // operands of the product with a key's offsets and scales: sums of q over half a group each, -64 times the sums over the
   // channels held as 64 + c, high and low parts
   uint32_t qoff[NT], qscale[NT];
+  // A row whose sums would leave fp16's range is taken times a power of two below 1, which the scale of its scores takes back:
+  // channels that become subnormal by it lose 2^-25, where the row's largest is at least 2^14 / (64 x 16) = 16. The scales by row lie
+  // in shared memory, a copy for each warp: registers for them are not left (two a tile: spills, 67.9 us for 66.7 on 64 contexts).
+  float* row_scale = reinterpret_cast<float*>(smem + S::kUnion + S::kQBytes) + warp * 8 * NT;
   uint8_t* q_s = smem + S::kUnion;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = nt * 8 + g;
     uint4 v[NG][2];
-    float sum[NG], sum64[NG];
+    float sum[NG], sum64[NG], top = 0.f;
     const int t = (row0 + r) / G, hq = (row0 + r) % G;
 #pragma unroll
     for (int grp = 0; grp < NG; ++grp) {
@@ -289,17 +294,40 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
           sum[grp] += f.x + f.y;
           if (i & 1) sum64[grp] += f.x + f.y;
         }
+      }
+      sum[grp] += __shfl_xor_sync(0xffffffffu, sum[grp], 1);     // lanes q = 0, 1 and q = 2, 3: half a group each
+      sum64[grp] = -64.f * (sum64[grp] + __shfl_xor_sync(0xffffffffu, sum64[grp], 1));
+      top = fmaxf(top, fmaxf(fabsf(sum[grp]), fabsf(sum64[grp])));
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int down = max(0, static_cast<int>(__float_as_uint(top) >> 23) - 127 - 14);      // the sums end below 2^15
+    if (__any_sync(0xffffffffu, down > 0)) {
+      const float f = __uint_as_float(static_cast<uint32_t>(max(1, 127 - down)) << 23);
+      const uint32_t f2 = pack_f16x2(f, f);
+#pragma unroll
+      for (int grp = 0; grp < NG; ++grp) {
+        sum[grp] *= f;
+        sum64[grp] *= f;
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          uint4& x = v[grp][w];
+          x = make_uint4(hmul2_u(x.x, f2), hmul2_u(x.y, f2), hmul2_u(x.z, f2), hmul2_u(x.w, f2));
+        }
+      }
+    }
+    if (q == 0) row_scale[r] = p.scale_log2e * __uint_as_float(static_cast<uint32_t>(127 + down) << 23);
+#pragma unroll
+    for (int grp = 0; grp < NG; ++grp)
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
         if (kQInRegs) qr[nt][grp][w] = v[grp][w];
         else if (warp == 0) *reinterpret_cast<uint4*>(q_s + ((nt * NG + grp) * 2 + w) * 512 + lane * 16) = v[grp][w];
       }
-      sum[grp] += __shfl_xor_sync(0xffffffffu, sum[grp], 1);     // lanes q = 0, 1 and q = 2, 3: half a group each
-      sum64[grp] += __shfl_xor_sync(0xffffffffu, sum64[grp], 1);
-    }
     // A sum in two fp16 parts (22 bits): the lanes q of a row give a half group's high part, its low part, and the other half's.
     float part[2], part64[2];
 #pragma unroll
     for (int grp = 0; grp < 2; ++grp) {
-      const float f = grp < NG ? sum[grp < NG ? grp : 0] : 0.f, f64 = grp < NG ? -64.f * sum64[grp < NG ? grp : 0] : 0.f;
+      const float f = grp < NG ? sum[grp < NG ? grp : 0] : 0.f, f64 = grp < NG ? sum64[grp < NG ? grp : 0] : 0.f;
       const float hi = __half2float(__float2half_rn(f)), hi64 = __half2float(__float2half_rn(f64));
       part[grp] = q & 1 ? f - hi : hi;
       part64[grp] = q & 1 ? f64 - hi64 : hi64;
@@ -307,6 +335,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     qoff[nt] = pack_f16x2(part[0], part[1]);
     qscale[nt] = pack_f16x2(part64[0], part64[1]);
   }
+  __syncwarp();
   if (!kQInRegs) __syncthreads();
   auto q_words = [&](int nt, int grp, int w) -> uint4 {
     if (kQInRegs) return qr[kQInRegs ? nt : 0][grp][w];
@@ -327,6 +356,9 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   // Scores of NP x 16 keys (s[.][nt]: keys g, g + 8 x query rows 2 q, 2 q + 1) -> probabilities as operands of the output product.
   auto softmax = [&](auto np, auto& s, auto& pb) {
     constexpr int NP = decltype(np)::value;
+    float2 scale[NT];            // of query rows 2 q, 2 q + 1
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) scale[nt] = *reinterpret_cast<const float2*>(row_scale + nt * 8 + 2 * q);
     float top = kNoMax;
     float x[NP][NT][4];
 #pragma unroll
@@ -335,7 +367,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          x[pp][nt][e] = fmaf(s[pp][nt][e], p.scale_log2e, -m_run[nt][e & 1]);
+          x[pp][nt][e] = fmaf(s[pp][nt][e], e & 1 ? scale[nt].y : scale[nt].x, -m_run[nt][e & 1]);
           top = fmaxf(top, x[pp][nt][e]);
         }
     if (__any_sync(0xffffffffu, top > kRaise)) {
@@ -343,9 +375,10 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
+          const float sc = e ? scale[nt].y : scale[nt].x;
           float mx = kNoMax;
 #pragma unroll
-          for (int pp = 0; pp < NP; ++pp) mx = fmaxf(mx, fmaxf(s[pp][nt][e], s[pp][nt][e + 2]) * p.scale_log2e);
+          for (int pp = 0; pp < NP; ++pp) mx = fmaxf(mx, fmaxf(s[pp][nt][e], s[pp][nt][e + 2]) * sc);
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -361,8 +394,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
           }
 #pragma unroll
           for (int pp = 0; pp < NP; ++pp) {
-            x[pp][nt][e] = fmaf(s[pp][nt][e], p.scale_log2e, -m_new);
-            x[pp][nt][e + 2] = fmaf(s[pp][nt][e + 2], p.scale_log2e, -m_new);
+            x[pp][nt][e] = fmaf(s[pp][nt][e], sc, -m_new);
+            x[pp][nt][e + 2] = fmaf(s[pp][nt][e + 2], sc, -m_new);
           }
         }
     }
