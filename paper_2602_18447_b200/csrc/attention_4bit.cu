@@ -51,6 +51,9 @@ constexpr uint32_t kOnes = 0x3C003C00u;      // two fp16 ones
 // is set and up to 2^kRaise before it is raised: most pages leave the accumulators alone, small probabilities keep fp16's
 // relative precision down to 2^-16 of the largest, and p s stays in fp16's range for every scale (kKv4MaxScale).
 constexpr float kHeadroom = 2.f, kRaise = 6.f;
+// Value scales are taken times up to 2^15 (as fp16 pairs: the factor, and the largest scale that may be taken times it).
+constexpr int kMaxUp = 15;
+constexpr uint32_t k2Max = 0x78007800u, kMostAt2Max = 0x27FF27FFu;
 
 __device__ __forceinline__ void cp_async_16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -88,6 +91,10 @@ __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t add
 }
 __device__ __forceinline__ uint32_t hmul2_u(uint32_t a, uint32_t b) {
   __half2 r = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t hmax2_u(uint32_t a, uint32_t b) {
+  __half2 r = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<uint32_t*>(&r);
 }
 __device__ __forceinline__ uint32_t hadd2_u(uint32_t a, uint32_t b) {
@@ -475,11 +482,50 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     }
   };
 
-  auto cached_values = [&](const uint8_t* b, uint32_t (&pb)[NT][2]) {
-    // (p s) (c - 8) by group; scales of keys 2 q, 2 q + 1 and 2 q + 8, 2 q + 9
-    uint32_t vs[2 * NG];
+  // Value scales enter the products times 2^k, which the accumulators hold until the end: p s 2^k stays in fp16's normal range for
+  // small values too. k is as large as the largest scale so far allows. (Costs 2 % at 8 query rows, 3 % at 16; a look at a share
+  // of the scales by each lane instead of all of them was no faster.)
+  uint32_t v_up = k2Max, v_most = kMostAt2Max;             // 2^k; kKv4MaxScale 2^-k
+  auto value_scales = [&](const uint8_t* b, uint32_t (&vs)[2 * NG]) {      // of keys 2 q, 2 q + 1 and 2 q + 8, 2 q + 9, by group
     if (NG == 2) *reinterpret_cast<uint4*>(vs) = *reinterpret_cast<const uint4*>(b + L::kVParams + q * 32 + 16);
     else *reinterpret_cast<uint2*>(vs) = *reinterpret_cast<const uint2*>(b + L::kVParams + q * 16 + 8);
+  };
+  auto scale_accumulators = [&](float f) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
+  };
+  auto fit_scales = [&](auto np, const uint8_t* b) {
+    uint32_t top = v_most;
+#pragma unroll
+    for (int pp = 0; pp < decltype(np)::value; ++pp) {
+      uint32_t vs[2 * NG];
+      value_scales(b + pp * L::kBlock, vs);
+#pragma unroll
+      for (int i = 0; i < 2 * NG; ++i) top = hmax2_u(top, vs[i]);
+    }
+    if (!__any_sync(0xffffffffu, top != v_most)) return;
+    const float2 f = unpack_f16x2(top);
+    float most = fmaxf(f.x, f.y);
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+    // the largest ends in [2^7, 2^8): a factor of 4 below where the next one has to give way
+    const int k_was = static_cast<int>(v_up >> 26) - 15;
+    const int k = max(0, min(k_was, 7 + 127 - static_cast<int>(__float_as_uint(most) >> 23)));
+    v_up = (15 + k) * 0x04000400u;
+    const float most_k = kKv4MaxScale * __uint_as_float((127 - k) << 23);
+    v_most = pack_f16x2(most_k, most_k);
+    scale_accumulators(__uint_as_float((127 + k - k_was) << 23));
+  };
+  auto cached_values = [&](const uint8_t* b, uint32_t (&pb)[NT][2]) {
+    // (p s) (c - 8) by group
+    uint32_t vs[2 * NG];
+    value_scales(b, vs);
+#pragma unroll
+    for (int i = 0; i < 2 * NG; ++i) vs[i] = hmul2_u(vs[i], v_up);
     const uint8_t* vb = b + L::kVCodes + L::v_chunk(g, q) * 16;
 #pragma unroll
     for (int grp = 0; grp < NG; ++grp) {
@@ -569,6 +615,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   for (int own = max(it.tile_begin, cached_pages) + (kWarps - 1 - warp); own < it.tile_end; own += kWarps)
     own_page((own - cached_pages) * kPage);
 
+  if (it.tile_end > cached_pages) scale_accumulators(__uint_as_float((127 + kMaxUp) << 23));
   int stage_off = 0, ahead_off = (kStages - 1) * kStageBytes;
 #pragma unroll 1
   for (int pg = pg0; pg < end_cached; pg += kStep) {
@@ -589,6 +636,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
         mask(s[1], pg * kPage + kPage, see_base, see_step);
       }
       softmax(std::integral_constant<int, 2>{}, s, pb);
+      fit_scales(std::integral_constant<int, 2>{}, b);
       cached_values(b, pb[0]);
       cached_values(b + L::kBlock, pb[1]);
     } else {
@@ -597,6 +645,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       cached_scores(b, s[0]);
       mask(s[0], pg * kPage, see_base, see_step);
       softmax(std::integral_constant<int, 1>{}, s, pb);
+      fit_scales(std::integral_constant<int, 1>{}, b);
       cached_values(b, pb[0]);
     }
     ahead_off = stage_off;                       // the stage just read is the next to be filled
@@ -608,6 +657,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   // ------------------------------------------------------------------ the warps' results, joined in warp order
   float* po = reinterpret_cast<float*>(smem);                            // [warp][8 NT rows][HD + 4]
   float* pml = reinterpret_cast<float*>(smem + S::kPartBytes);           // [warp][8 NT rows][2]
+  const float v_down = __uint_as_float((127 + 15 - (v_up >> 26)) << 23);
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -624,8 +674,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       float* dst = po + (warp * 8 * NT + r) * S::kPad + g;
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        dst[mt * 16] = o[nt][mt][e] + add[mt / 4];
-        dst[mt * 16 + 8] = o[nt][mt][e + 2] + add[mt / 4];
+        dst[mt * 16] = fmaf(o[nt][mt][e], v_down, add[mt / 4]);
+        dst[mt * 16 + 8] = fmaf(o[nt][mt][e + 2], v_down, add[mt / 4]);
       }
     }
   }

@@ -92,3 +92,79 @@ def test_queries_of_every_fp16_magnitude(hd, hq, hkv, n, kind, given):
     assert np.all(np.isfinite(got))
     assert np.all(err <= bound), (float(np.max(err / bound)), np.argwhere(~(err <= bound))[:4])
     assert float(np.median(bound)) < 0.1              # the bound says something
+
+
+def _relative_bound(q, k, v, kc, vc, seen, scale, dtype):
+    """64-bit attention over rows k, v and how far an output may be off where no probability is subnormal, so that every term is off
+    in proportion to p |v| and p s: p to fp16 (2^-11 of p |v|), p s to fp16 (2^-11 of p s |c - 8| <= 8 p s); under a larger scale S in
+    the context p s may become subnormal, 2^-25 8 codes in units of 2^-k <= S 2^-7 of a sum of at least 2^2: 2^-31 S a key; the
+    scores as in K.attend; the output's own rounding. kc, vc: the groups' (codes, scales, offsets)."""
+    n, hq, hd = q.shape
+    group = hq // k.shape[1]
+    mag = (79 * kc[1] + np.abs(kc[2])).max(-1)
+    step = np.repeat(vc[1], K.GROUP, axis=-1)
+    out, bound = np.zeros(q.shape), np.zeros(q.shape)
+    for h in range(hq):
+        j = h // group
+        for t in range(n):
+            m = seen[t]
+            s = k[:m, j] @ q[t, h] * scale
+            p = np.exp(s - s.max())
+            assert p.min() > 2.0 ** -14                                   # 2^2 p is a normal number
+            p /= p.sum()
+            out[t, h] = p @ v[:m, j]
+            delta = (hd + 8) * 2.0 ** -23 * scale * np.abs(q[t, h]).sum() * mag[:m, j].max() + 2.0 ** -18
+            spread = p @ np.abs(v[:m, j])
+            bound[t, h] = 2.0 ** -11 * (spread + 8 * p @ step[:m, j]) + m * 2.0 ** -31 * step[:m, j].max() + 2 * delta * (spread + np.abs(out[t, h]))
+    return out, bound + _out_eps(dtype) * np.abs(out) + 2.0 ** -100
+
+
+def _sinks(sigma, hq, hkv, hd, n, ctx, given, lift):
+    """Every sixteenth key draws e^lift times the weight of the others and has no value; the others' values have size sigma
+    (a number, or one for each position)."""
+    import torch
+    rng = np.random.default_rng(hd + hq)
+    held = ctx + (0 if given else n)
+    k, v = np.zeros((held, hkv, hd)), rng.standard_normal((held, hkv, hd)) * np.broadcast_to(sigma, held)[:, None, None]
+    k[::16] = lift / np.sqrt(hd)
+    v[::16] = 0.0
+    q = np.ones((n, hq, hd))
+    q[:, 1::2] = 0.5
+    kn, vn = np.zeros((n, hkv, hd)), rng.standard_normal((n, hkv, hd)) * np.broadcast_to(sigma, held)[-1]
+    q, k, v, kn, vn = (_dev(x, "bfloat16") for x in (q, k, v, kn, vn))
+    with K.Cache(hq, hkv, hd, n_seqs=1, pages_each=(ctx + n) // 16 + 1) as c:
+        c.B.cs_plan_set(c.plan, [0], [held])
+        c.B.cs_kv_append(c.plan, 0, k, v, rotate=False)
+        c.set([ctx])
+        c.B.cs_plan_set(c.plan, [0], [n], given=given)
+        out = torch.full_like(q, float("nan"))
+        c.B.cs_attention_4bit(c.plan, 0, q, out, *((kn, vn) if given else (None, None)))
+        torch.cuda.synchronize()
+    kq, vq = K.quantise(_np(k)), K.quantise(_np(v))
+    xk, xv = K.values(*kq), K.values(*vq)
+    if given:
+        own = (np.zeros((n, hkv, hd)), np.zeros((n, hkv, hd // 64)))
+        xk, xv = np.concatenate([xk, _np(kn)]), np.concatenate([xv, _np(vn)])
+        kq, vq = ([np.concatenate([a, b]) for a, b in zip(z, (own[0], own[1], own[1]))] for z in (kq, vq))
+    want, bound = _relative_bound(_np(q), xk, xv, kq, vq, ctx + np.arange(n) + 1, hd ** -0.5, "bfloat16")
+    err = np.abs(_np(out) - want)
+    assert np.all(err <= bound), (float(np.nanmax(err / bound)), float(np.nanmedian(err / bound)))
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("sigma", [1e-6, 1e-4, 1e-3, 1e-2, 0.1, 1.0, 300.0])
+@pytest.mark.parametrize("hd,hq,hkv,n,ctx", [(128, 2, 1, 1, 600), (64, 2, 1, 1, 600), (128, 6, 2, 5, 333), (64, 6, 2, 5, 333),
+                                             (128, 2, 2, 1, 9000)])
+def test_small_values_beside_keys_that_draw_the_weight(hd, hq, hkv, n, ctx, sigma, given):
+    """Probabilities of 2^-12 of the largest times scales of any size: what is lost is in proportion to the values, not to fp16's
+    smallest number."""
+    _sinks(sigma, hq, hkv, hd, n, ctx, given, 12 * np.log(2.0))
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("order", ["growing", "shrinking", "jumping"])
+@pytest.mark.parametrize("hd,hq,hkv,n,ctx", [(128, 2, 1, 1, 1500), (64, 6, 2, 5, 1500)])
+def test_values_whose_size_changes_along_a_context(hd, hq, hkv, n, ctx, order, given):
+    at = np.arange(ctx + (0 if given else n))
+    power = {"growing": -6 + 9 * at / len(at), "shrinking": 3 - 9 * at / len(at), "jumping": np.where(at // 48 % 2, 3.0, -4.0)}[order]
+    _sinks(10.0 ** power, hq, hkv, hd, n, ctx, given, 6 * np.log(2.0))
