@@ -206,7 +206,8 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
  * stood at the capture, so set the plan anew only to capture anew. Two graphs that may run at the same time need two plans.
  *
  * Types (dtype): CS_F16 or CS_BF16, of every row argument of the call. Rows hold [heads, head_dim] contiguously; strides count
- * elements between rows, are multiples of 8 and at least a row's length; pointers are 16-byte aligned.
+ * elements between rows, are multiples of 8 and at least a row's length; pointers are 16-byte aligned. A call reads and writes a row
+ * for each of the plan's T tokens: the buffers' lengths are the caller's to see to (the Python binding compares shapes).
  * Errors: CS_EINVAL for arguments, before any launch; CS_ESTATE; CS_ECUDA.
  */
 #define CS_F16 0

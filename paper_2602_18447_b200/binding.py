@@ -143,6 +143,10 @@ def _dev_ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
+# What row arguments are held to (the library takes addresses only).
+_heads: dict = {}       # model, cache or plan -> (n_q_heads, n_kv_heads, head_dim)
+_plan_rows: dict = {}   # plan -> the shapes that rows of its last cs_plan_set's tokens may have: (of q, of k and v), or (None, None)
+
 _torch = None
 
 
@@ -204,11 +208,13 @@ def cs_model_load(shape, weights: dict) -> int:
                          per_layer("q_norm", np.float32) if qk else None, per_layer("k_norm", np.float32) if qk else None)
     out = C.c_void_p()
     _check(lib.cs_model_load(C.byref(desc), C.byref(t), 0, C.byref(out)), "cs_model_load")
+    _heads[out.value] = (shape.n_q_heads, shape.n_kv_heads, shape.head_dim)
     return out.value
 
 
 def cs_model_free(model: int) -> None:
     _check(load_library().cs_model_free(model), "cs_model_free")
+    _heads.pop(model, None)
 
 
 def cs_model_set_lm_head_rows(model: int, row_ids, rows_bf16: np.ndarray, stream=None) -> None:
@@ -229,12 +235,18 @@ def cs_kv_pool_bytes(model: int, num_pages: int, page_size: int = 16) -> int:
     return int(load_library().cs_kv_pool_bytes(model, num_pages, page_size))
 
 
+def _on_heads_of(owner: int, handle: int) -> int:
+    """Notes that `handle` (a cache, a plan) has its owner's heads."""
+    _heads[handle] = _heads.get(owner)
+    return handle
+
+
 def cs_kv_alloc(model: int, num_pages: int, page_size: int, max_seqs: int, max_pages_per_seq: int,
                 dev_pool=None) -> int:
     out = C.c_void_p()
     _check(load_library().cs_kv_alloc(model, num_pages, page_size, max_seqs, max_pages_per_seq,
                                       _dev_ptr(dev_pool), C.byref(out)), "cs_kv_alloc")
-    return out.value
+    return _on_heads_of(model, out.value)
 
 
 CS_KV_E4M3, CS_KV_E5M2 = 1, 2
@@ -246,14 +258,14 @@ def cs_kv_alloc_8bit(model: int, num_pages: int, page_size: int, max_seqs: int, 
     code = {"e4m3": CS_KV_E4M3, "e5m2": CS_KV_E5M2}[fmt]
     _check(load_library().cs_kv_alloc_8bit(model, num_pages, page_size, max_seqs, max_pages_per_seq, code,
                                            C.byref(out)), "cs_kv_alloc_8bit")
-    return out.value
+    return _on_heads_of(model, out.value)
 
 
 def cs_kv_alloc_4bit(model: int, num_pages: int, page_size: int, max_seqs: int, max_pages_per_seq: int) -> int:
     out = C.c_void_p()
     _check(load_library().cs_kv_alloc_4bit(model, num_pages, page_size, max_seqs, max_pages_per_seq, C.byref(out)),
            "cs_kv_alloc_4bit")
-    return out.value
+    return _on_heads_of(model, out.value)
 
 
 CS_F16, CS_BF16 = 0, 1
@@ -272,10 +284,17 @@ def _dtype_code(t) -> int:
     return code
 
 
-def _rows(t, like=None):
+def _of(table: dict, handle: int):
+    entry = table.get(handle)
+    if entry is None:
+        raise ValueError("not a cache or plan that is in use")
+    return entry
+
+
+def _rows(t, like=None, shapes=None):
     """(device address, elements between rows) of a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim] whose rows are
     contiguous; the rows themselves may lie apart (a slice of a fused projection). `like`: a tensor whose type, device and row
-    count it has to have; without one, the current device."""
+    count it has to have; without one, the current device. `shapes`: the two that it may have."""
     if t is None:
         return None, 0
     shape, stride = t.shape, t.stride()
@@ -283,6 +302,8 @@ def _rows(t, like=None):
     if not t.is_cuda or nd not in (2, 3):
         raise ValueError("expected a CUDA tensor [T, heads, head_dim] or [T, heads * head_dim]")
     n = shape[0]
+    if shapes is not None and shape != shapes[0] and shape != shapes[1]:
+        raise ValueError(f"rows of shape {tuple(shape)} where the plan has {shapes[0]}")
     if n and (stride[-1] != 1 or (nd == 3 and stride[1] != shape[2] and shape[1] != 1)):
         raise ValueError("the heads of a row have to be contiguous")
     if like is None:
@@ -298,19 +319,25 @@ def _rows(t, like=None):
 def cs_plan_create(kv: int, max_tokens: int = 0) -> int:
     out = C.c_void_p()
     _check(load_library().cs_plan_create(kv, max_tokens, C.byref(out)), "cs_plan_create")
-    return out.value
+    _plan_rows[out.value] = (None, None)
+    return _on_heads_of(kv, out.value)
 
 
 def cs_plan_set(plan: int, seq_ids, lens, given: bool = False, stream=None) -> None:
     s, l = _i32(seq_ids), _i32(lens)
     if s.shape != l.shape:
         raise ValueError("seq_ids and lens have one entry per step")
+    hq, hkv, hd = _of(_heads, plan)
     _check(load_library().cs_plan_set(plan, _np_ptr(s), _np_ptr(l), int(s.shape[0]), 1 if given else 0, _stream_ptr(stream)),
            "cs_plan_set")
+    n = int(l.sum())
+    _plan_rows[plan] = (((n, hq, hd), (n, hq * hd)), ((n, hkv, hd), (n, hkv * hd)))
 
 
 def cs_plan_free(plan: int) -> None:
     _check(load_library().cs_plan_free(plan), "cs_plan_free")
+    _heads.pop(plan, None)
+    _plan_rows.pop(plan, None)
 
 
 def cs_kv_commit(plan: int) -> None:
@@ -319,18 +346,21 @@ def cs_kv_commit(plan: int) -> None:
 
 def cs_kv_append(plan: int, layer: int, k, v, q=None, q_out=None, rotate: bool = True, stream=None) -> None:
     """k, v: CUDA rows [T, n_kv_heads, head_dim] (float16 or bfloat16); q, q_out: [T, n_q_heads, head_dim] or None, of the
-    same type. T, the heads and head_dim are those of the plan and its cache."""
-    (kp, ks), (vp, vs) = _rows(k), _rows(v, k)
-    (qp, qs), (op, os_) = _rows(q, k), _rows(q_out, k)
+    same type. T, the heads and head_dim are those of the plan and its cache (ValueError otherwise)."""
+    q_shapes, kv_shapes = _of(_plan_rows, plan)
+    (kp, ks), (vp, vs) = _rows(k, None, kv_shapes), _rows(v, k, kv_shapes)
+    (qp, qs), (op, os_) = _rows(q, k, q_shapes), _rows(q_out, k, q_shapes)
     _check(load_library().cs_kv_append(plan, layer, kp, ks, vp, vs, qp, qs, op, os_, 1 if rotate else 0, _dtype_code(k),
                                        _stream_ptr(stream)), "cs_kv_append")
 
 
 def cs_attention_4bit(plan: int, layer: int, q, out, k_new=None, v_new=None, scale: float = 0.0, stream=None) -> None:
     """q, out: CUDA rows [T, n_q_heads, head_dim]; k_new, v_new: [T, n_kv_heads, head_dim] of a plan with given=True, with one
-    row stride; all of one type (float16 or bfloat16)."""
-    (qp, qs), (op, os_) = _rows(q), _rows(out, q)
-    (kp, ks), (vp, vs) = _rows(k_new, q), _rows(v_new, q)
+    row stride; all of one type (float16 or bfloat16). T, the heads and head_dim are those of the plan and its cache (ValueError
+    otherwise)."""
+    q_shapes, kv_shapes = _of(_plan_rows, plan)
+    (qp, qs), (op, os_) = _rows(q, None, q_shapes), _rows(out, q, q_shapes)
+    (kp, ks), (vp, vs) = _rows(k_new, q, kv_shapes), _rows(v_new, q, kv_shapes)
     if ks != vs:
         raise ValueError("k_new and v_new have one row stride")
     _check(load_library().cs_attention_4bit(plan, layer, qp, qs, kp, vp, ks, op, os_, _dtype_code(q), float(scale),
@@ -338,18 +368,26 @@ def cs_attention_4bit(plan: int, layer: int, q, out, k_new=None, v_new=None, sca
 
 
 def cs_kv_read(kv: int, layer: int, tok_seq, tok_pos, out_k, out_v, stream=None) -> None:
-    """tok_seq, tok_pos: CUDA int32 tensors [T]; out_k, out_v: contiguous CUDA tensors [T, n_kv_heads, head_dim] of one type."""
+    """tok_seq, tok_pos: CUDA int32 tensors [T]; out_k, out_v: contiguous CUDA tensors [T, n_kv_heads, head_dim] of one type, the
+    heads and head_dim those of the cache (ValueError otherwise). All on the current device."""
     torch = _torch or _t()
-    if tok_seq.dtype != torch.int32 or tok_pos.dtype != torch.int32 or tok_seq.shape != tok_pos.shape:
+    n = tok_seq.shape[0]
+    if tok_seq.dtype != torch.int32 or tok_pos.dtype != torch.int32 or tok_seq.shape != (n,) or tok_pos.shape != (n,):
         raise ValueError("tok_seq and tok_pos are int32 tensors of one length")
-    if out_k.dtype != out_v.dtype or out_k.shape != out_v.shape or out_k.shape[0] != tok_seq.shape[0]:
-        raise ValueError("out_k and out_v have one type, one shape and a row per place")
+    _, hkv, hd = _of(_heads, kv)
+    shape = out_k.shape
+    if out_k.dtype != out_v.dtype or out_v.shape != shape or (shape != (n, hkv, hd) and shape != (n, hkv * hd)):
+        raise ValueError("out_k and out_v have one type, a row per place and the cache's heads")
+    dev = torch.cuda.current_device()
+    if not dev == out_k.get_device() == out_v.get_device() == tok_seq.get_device() == tok_pos.get_device():
+        raise ValueError("places and rows have to be on the current device")
     _check(load_library().cs_kv_read(kv, layer, _dev_ptr(tok_seq), _dev_ptr(tok_pos), int(tok_seq.shape[0]), _dev_ptr(out_k),
                                      _dev_ptr(out_v), _dtype_code(out_k), _stream_ptr(stream)), "cs_kv_read")
 
 
 def cs_kv_free(kv: int) -> None:
     _check(load_library().cs_kv_free(kv), "cs_kv_free")
+    _heads.pop(kv, None)
 
 
 def cs_kv_set_seq(kv: int, seq: int, page_ids, ctx_len: int) -> None:

@@ -168,3 +168,25 @@ def test_values_whose_size_changes_along_a_context(hd, hq, hkv, n, ctx, order, g
     at = np.arange(ctx + (0 if given else n))
     power = {"growing": -6 + 9 * at / len(at), "shrinking": 3 - 9 * at / len(at), "jumping": np.where(at // 48 % 2, 3.0, -4.0)}[order]
     _sinks(10.0 ** power, hq, hkv, hd, n, ctx, given, 6 * np.log(2.0))
+
+
+@pytest.mark.parametrize("n", [1, 3, 5, 40])
+def test_rows_have_to_be_the_plans(n):
+    """A plan of four tokens and rows of another number, or of other heads: refused before anything is launched."""
+    import torch
+    rows = lambda m, h, d=128: torch.zeros(m, h, d, dtype=torch.float16, device="cuda")  # noqa: E731
+    with K.Cache(4, 2, 128, n_seqs=2) as c:
+        B = c.B
+        B.cs_plan_set(c.plan, [0, 1], [1, 3])
+        torch.cuda.synchronize()
+        B.cs_take_launch_count()
+        for call in (lambda: B.cs_kv_append(c.plan, 0, rows(n, 2), rows(n, 2)),
+                     lambda: B.cs_kv_append(c.plan, 0, rows(4, 2), rows(4, 2), q=rows(n, 4), q_out=rows(n, 4)),
+                     lambda: B.cs_kv_append(c.plan, 0, rows(4, 1), rows(4, 1)),
+                     lambda: B.cs_kv_append(c.plan, 0, rows(4, 4, 64), rows(4, 4, 64)),
+                     lambda: B.cs_attention_4bit(c.plan, 0, rows(n, 4), rows(n, 4)),
+                     lambda: B.cs_attention_4bit(c.plan, 0, rows(4, 4), rows(4, 3)),
+                     lambda: B.cs_kv_read(c.kv, 0, *([torch.zeros(4, dtype=torch.int32, device="cuda")] * 2), rows(4, 1), rows(4, 1))):
+            with pytest.raises(ValueError):
+                call()
+        assert B.cs_take_launch_count() == 0
