@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(HD, 640 / HD) kv_append_kernel(const KvAppendP
     const float4* r = reinterpret_cast<const float4*>(p.rope + tok * (HD / 2) + c * 8);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float4 f = __ldg(r + j);
+      const float4 f = r[j];
       cs[2 * j] = make_float2(f.x, f.y);
       cs[2 * j + 1] = make_float2(f.z, f.w);
     }
@@ -398,8 +398,7 @@ __device__ __forceinline__ uint32_t splat(uint32_t halves, int which) {
 // for a slot that is not wanted. The words are the attention's, so that a mask takes two channels (K) or two words give two
 // channels of four keys (V).
 template <int HD, bool BF16, typename Row>
-__device__ __forceinline__ void block_rows(const uint8_t* __restrict__ b, int lane, uint16_t* __restrict__ out_k,
-                                           uint16_t* __restrict__ out_v, Row row) {
+__device__ __forceinline__ void block_rows(const uint8_t* b, int lane, uint16_t* out_k, uint16_t* out_v, Row row) {
   using L = Kv4<HD>;
   constexpr int CH = HD / 8, kRows = 32 / CH, kRounds = kPage / kRows;       // K: rows of 8-channel chunks that a warp has at once
   constexpr int MT = HD / 16;
@@ -450,8 +449,8 @@ __device__ __forceinline__ void block_rows(const uint8_t* __restrict__ b, int la
 
 // Page id of a listed place, or -1 outside the page table.
 __device__ __forceinline__ int listed_page(const KvReadParams& p, int row, int& pos) {
-  const int seq = __ldg(p.tok_seq + row);
-  pos = __ldg(p.tok_pos + row);
+  const int seq = p.tok_seq[row];
+  pos = p.tok_pos[row];
   if (seq < 0 || seq >= p.max_seqs || pos < 0 || pos / kPage >= p.max_pages_per_seq) return -1;
   const int page = __ldg(p.table + static_cast<size_t>(seq) * p.max_pages_per_seq + pos / kPage);
   return page < p.num_pages ? page : -1;
@@ -475,8 +474,8 @@ __global__ void __launch_bounds__(2 * HD) kv_read_kernel(const KvReadParams p) {
     const size_t ph = static_cast<size_t>(page) * p.n_kv_heads + h;
     if (FMT == CS_KV_FMT_16BIT) {
       const size_t at = (ph * kPage + slot) * HD + c * 8;
-      widen8<false>(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.pool_k) + at)), k);
-      widen8<false>(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.pool_v) + at)), v);
+      widen8<false>(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.pool_k) + at), k);
+      widen8<false>(*reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p.pool_v) + at), v);
     } else {
       const uint2 w = *reinterpret_cast<const uint2*>(p.pool_k + (ph * kPage + slot) * HD + c * 8);
       const uint8_t* vt = p.pool_v + ph * kPage * HD;
@@ -551,8 +550,8 @@ __global__ void __launch_bounds__(THREADS) kv_read4_kernel(const KvReadParams p)
 // Whole pages of the 4-bit cache as fp16 pages of a scratch pool (the layout of the 16-bit cache), in the order of the list: what
 // the tensor-core attention of long steps reads. One warp per (listed page, kv head).
 template <int HD>
-__global__ void __launch_bounds__(128) kv_expand_kernel(const uint8_t* __restrict__ pool, const int32_t* __restrict__ pages,
-                                                       int n_pages, uint16_t* __restrict__ out_k, uint16_t* __restrict__ out_v,
+__global__ void __launch_bounds__(128) kv_expand_kernel(const uint8_t* pool, const int32_t* __restrict__ pages,
+                                                       int n_pages, uint16_t* out_k, uint16_t* out_v,
                                                        int n_kv_heads, int num_pages, uint32_t* status) {
   pdl_launch_dependents();
   pdl_wait();
@@ -567,9 +566,9 @@ __global__ void __launch_bounds__(128) kv_expand_kernel(const uint8_t* __restric
 // The new tokens' keys and values out of the 4-bit cache into the K and V columns of a fused fp16 matrix. One warp per (block of
 // tokens of one page, kv head).
 template <int HD>
-__global__ void __launch_bounds__(128) kv_blocks_kernel(const uint8_t* __restrict__ pool, const KvBlock* __restrict__ blocks,
+__global__ void __launch_bounds__(128) kv_blocks_kernel(const uint8_t* pool, const KvBlock* __restrict__ blocks,
                                                        int n_blocks, const int32_t* __restrict__ table, int max_pages_per_seq,
-                                                       uint16_t* __restrict__ out_k, uint16_t* __restrict__ out_v, int64_t stride,
+                                                       uint16_t* out_k, uint16_t* out_v, int64_t stride,
                                                        int n_kv_heads, int num_pages, uint32_t* status) {
   pdl_launch_dependents();
   pdl_wait();

@@ -190,3 +190,46 @@ def test_rows_have_to_be_the_plans(n):
             with pytest.raises(ValueError):
                 call()
         assert B.cs_take_launch_count() == 0
+
+
+@pytest.mark.parametrize("fmt", ["int4", "16bit", "e4m3"])
+def test_rows_are_read_right_behind_their_append(fmt):
+    """Appending and reading back (and, of 4-bit pages, attention by the expanded form) follow one another without a wait, eager and
+    as a graph: every read sees the rows of the append in front of it."""
+    import torch
+    rng = np.random.default_rng(31)
+    n, rounds = 40, 12
+    rows = [_dev(rng.standard_normal((n, 2, 128)), "float16") for _ in range(rounds)]
+    seq, pos = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    q = _dev(rng.standard_normal((n, 8, 128)), "float16")
+    with K.Cache(8, 2, 128, n_seqs=1, fmt=fmt) as c:
+        c.B.cs_plan_set(c.plan, [0], [n])
+        got = [[torch.empty_like(rows[0]) for _ in range(2)] + [torch.empty_like(q)] for _ in range(rounds)]
+
+        def all_rounds(wait):
+            for x, (k, v, out) in zip(rows, got):
+                c.B.cs_kv_append(c.plan, 0, x, -x, rotate=False)
+                c.B.cs_kv_read(c.kv, 0, seq, pos, k, v)
+                if fmt == "int4":
+                    c.B.cs_attention_4bit(c.plan, 0, q, out)
+                if wait:
+                    torch.cuda.synchronize()
+
+        all_rounds(True)
+        want = [[t.clone() for t in g] for g in got]
+        for g in got:
+            for t in g:
+                t.zero_()
+        all_rounds(False)
+        graph = torch.cuda.CUDAGraph()
+        for again in range(2):
+            torch.cuda.synchronize()
+            for g, w in zip(got, want):
+                assert torch.equal(g[0], w[0]) and torch.equal(g[1], w[1]) and (fmt != "int4" or torch.equal(g[2], w[2]))
+                for t in g:
+                    t.zero_()
+            if not again:
+                with torch.cuda.graph(graph):
+                    all_rounds(False)
+                graph.replay()
+        assert not torch.equal(want[0][0], want[1][0])
