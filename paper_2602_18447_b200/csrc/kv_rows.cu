@@ -378,15 +378,17 @@ __device__ __forceinline__ float fp8_value(uint8_t b) {
   return __half2float(__half(h));
 }
 
-// Two codes as exact fp16 numbers -> the values that they stand for: fp16 in one fused rounding, bf16 through fp32.
+// Two codes as exact fp16 numbers -> the values that they stand for: fp16 in one fused rounding, bf16 through fp32. A code of 15 may
+// stand for up to 65524 (the offset of a turned row rounds up by 16, 15 scales by 4): fp16 holds it at 65504, not as an infinity.
 template <bool BF16>
 __device__ __forceinline__ uint32_t value2(uint32_t c, uint32_t scale2, uint32_t offset2) {
   if (BF16) {
     const float2 f = unpack_f16x2(c), s = unpack_f16x2(scale2), o = unpack_f16x2(offset2);
     return pack_bf16x2(fmaf(f.x, s.x, o.x), fmaf(f.y, s.y, o.y));
   }
-  const __half2 r = __hfma2(*reinterpret_cast<const __half2*>(&c), *reinterpret_cast<const __half2*>(&scale2),
-                            *reinterpret_cast<const __half2*>(&offset2));
+  const uint32_t most = 0x7BFF7BFFu;
+  const __half2 r = __hmin2(__hfma2(*reinterpret_cast<const __half2*>(&c), *reinterpret_cast<const __half2*>(&scale2),
+                                    *reinterpret_cast<const __half2*>(&offset2)), *reinterpret_cast<const __half2*>(&most));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 // Nibbles 0 and 4 (1024 + c), or 1 and 5 (64 + c), of w as exact fp16 numbers.

@@ -275,3 +275,51 @@ def test_scales_are_the_rounded_quotient(hd, dtype):
             bits = x.view(torch.uint16).cpu().numpy()
             c.B.cs_kv_fill(c.kv, 0, 0, bits, bits)
             assert np.array_equal(c.read(np.zeros(n, int), np.arange(n))[0], want)
+
+
+def _keys_at_the_top(n, hd, theta, rng):
+    """bf16 keys whose turned rows hold more than 65504 (stored as that) and nothing below 50 K: where a group's smallest value rounds up
+    as fp16, 15 scales above the offset is beyond what fp16 rounds to 65504."""
+    half = hd // 2
+    t = rng.uniform(51000.0, 60000.0, (n, hd))
+    t[:, 3] = t[:, half + 3] = 70000.0
+    pos = np.arange(n) % 40
+    a = -pos[:, None] * theta ** (-np.arange(half) / half)[None]
+    x, y = t[:, :half], t[:, half:]
+    return np.concatenate([x * np.cos(a) - y * np.sin(a), y * np.cos(a) + x * np.sin(a)], 1), pos
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_values_at_the_top_of_fp16_are_read_as_finite_ones(hd):
+    """A key of 15 scales above its offset may stand for more than fp16's largest number: it is read, and expanded for long steps, as
+    65504 (bf16 rows get the value itself). Attention over such keys in both forms: the bound of K.attend with the values that
+    the codes stand for, at most 2^-11 above what is expanded."""
+    import torch
+    rng = np.random.default_rng(hd)
+    n, theta = 4000, 1.0e4
+    k, _ = _keys_at_the_top(n, hd, theta, rng)
+    v = rng.standard_normal((n, 1, hd))
+    with K.Cache(2, 1, hd, n_seqs=100, pages_each=10, theta=theta) as c:
+        kd, vd = _dev(k[:, None], "bfloat16"), _dev(v, "bfloat16")
+        assert bool(torch.isfinite(kd).all())
+        c.B.cs_plan_set(c.plan, np.arange(100), np.full(100, 40))
+        c.B.cs_kv_append(c.plan, 0, kd, vd)
+        c.B.cs_kv_commit(c.plan)
+        seq, pos = torch.arange(n, dtype=torch.int32) // 40, torch.arange(n, dtype=torch.int32) % 40
+        wide = torch.empty(n, 1, hd, dtype=torch.bfloat16, device="cuda")
+        c.B.cs_kv_read(c.kv, 0, seq.cuda(), pos.cuda(), wide, torch.empty_like(wide))
+        got, _ = c.read(seq.numpy(), pos.numpy())
+        beyond = _np(wide) > 65504.0                     # 65536, the bf16 number next to what the codes stand for
+        assert beyond.any() and np.all(np.isfinite(got)) and got.max() == 65504.0
+        assert np.all(np.abs(got - _np(wide)) <= 2.0 ** -8 * 65536.0 * (1 + 2.0 ** -3))
+        at = int(np.argwhere(beyond)[0][0]) // 40
+        for steps in (2, 60):                            # 4 and 120 query rows
+            q = _dev(np.ones((steps, 2, hd)) * 2.0 ** -10, "float16")
+            new = _dev(np.zeros((steps, 1, hd)), "float16")
+            out = torch.full_like(q, float("nan"))
+            c.B.cs_plan_set(c.plan, [at], [steps], given=True)
+            c.B.cs_attention_4bit(c.plan, 0, q, out, new, new, scale=1.0e-6)
+            torch.cuda.synchronize()
+            # scores below 128 x 2^-10 x 65536 x 1e-6 = 0.0082: weights are even to 1 %, of 40 cached values and the own zeros
+            mean = _np(c.torch.tensor(v[40 * at:40 * at + 40].mean(0)))[None] * 40 / (41 + np.arange(steps))[:, None, None]
+            assert np.all(np.abs(_np(out) - mean) <= 0.1)
