@@ -167,7 +167,8 @@ uint64_t cs_kv_pool_bytes(const cs_model* model, int num_pages, int page_size);
  *   page_ids           host int32[n_pages], each in [0, num_pages). Pages may be shared by several
  *                      sequences (k candidate steps verified on one context).
  *   ctx_len            cached tokens, 0 <= ctx_len <= n_pages * page_size.
- * Host-side only; the table is uploaded by the next call that reads it.
+ * Host-side only; the table is uploaded by the next call that reads it, on that call's stream. Calls on other streams wait there for
+ * the upload (replays of a graph do not).
  */
 int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int ctx_len);
 

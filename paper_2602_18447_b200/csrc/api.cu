@@ -152,6 +152,7 @@ struct cs_kv {
   bool dirty = true;
   cudaEvent_t upload_ev = nullptr;
   bool upload_pending = false;
+  bool upload_unseen = false;      // the last upload has not been seen to have ended: other streams have to wait for it
   DevBuf fill_tmp;
   size_t layer4_bytes() const {
     return static_cast<size_t>(num_pages) * model->d.n_kv_heads * kv4_block_bytes(model->d.head_dim);
@@ -180,13 +181,27 @@ struct cs_plan {
 
 namespace {
 
+// The page table on the device, as far as work that is issued to `s` from now on is concerned: uploaded there if it has changed, and
+// behind an upload that another stream may still be at. Not inside a stream capture.
 int upload_table(cs_kv* kv, cudaStream_t s) {
-  if (!kv->dirty) return CS_OK;
+  if (!kv->dirty) {
+    if (!kv->upload_unseen) return CS_OK;
+    const cudaError_t done = cudaEventQuery(kv->upload_ev);
+    if (done == cudaSuccess) {
+      kv->upload_unseen = false;
+      return CS_OK;
+    }
+    if (done != cudaErrorNotReady) return cuda_fail(done, "page table upload");
+    cudaGetLastError();
+    CS_CUDA(cudaStreamWaitEvent(s, kv->upload_ev, 0));
+    return CS_OK;
+  }
   CS_CUDA(cudaMemcpyAsync(kv->table_dev, kv->table_host,
                           sizeof(int32_t) * static_cast<size_t>(kv->max_seqs) * kv->max_pages_per_seq,
                           cudaMemcpyHostToDevice, s));
   CS_CUDA(cudaEventRecord(kv->upload_ev, s));
   kv->upload_pending = true;
+  kv->upload_unseen = true;
   kv->dirty = false;
   return CS_OK;
 }
@@ -1291,12 +1306,13 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
   return CS_OK;
 }
 
-// Nothing may be uploaded from inside a stream capture: the page table has to be on the device already.
+// Nothing may be uploaded from inside a stream capture: the page table has to be on the device already (a replay is ordered behind
+// an upload that is still on its way by whoever replays).
 static int table_ready(cs_kv* kv, cudaStream_t s) {
-  if (!kv->dirty) return CS_OK;
+  if (!kv->dirty && !kv->upload_unseen) return CS_OK;
   cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
   CS_CUDA(cudaStreamIsCapturing(s, &st));
-  if (st != cudaStreamCaptureStatusNone) return CS_ESTATE;
+  if (st != cudaStreamCaptureStatusNone) return kv->dirty ? CS_ESTATE : CS_OK;
   return upload_table(kv, s);
 }
 

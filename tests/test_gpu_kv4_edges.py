@@ -323,3 +323,57 @@ def test_values_at_the_top_of_fp16_are_read_as_finite_ones(hd):
             # scores below 128 x 2^-10 x 65536 x 1e-6 = 0.0082: weights are even to 1 %, of 40 cached values and the own zeros
             mean = _np(c.torch.tensor(v[40 * at:40 * at + 40].mean(0)))[None] * 40 / (41 + np.arange(steps))[:, None, None]
             assert np.all(np.abs(_np(out) - mean) <= 0.1)
+
+
+@pytest.mark.parametrize("fmt", ["int4", "16bit"])
+def test_the_page_table_reaches_every_stream(fmt):
+    """Two sequences change pages; the call that uploads the table stands behind a long kernel of its stream. Calls on another
+    stream, which has to wait for that upload, read and write the new pages."""
+    import torch
+    rng = np.random.default_rng(41)
+    k = _dev(rng.standard_normal((60, 2, 128)), "float16")
+    q, new = _dev(rng.standard_normal((1, 4, 128)), "float16"), _dev(rng.standard_normal((1, 2, 128)), "float16")
+    results = []
+    for delayed in (False, True):
+        with K.Cache(4, 2, 128, n_seqs=2, fmt=fmt) as c:
+            B = c.B
+            other = B.cs_plan_create(c.kv, 8)
+            B.cs_plan_set(c.plan, [0, 1], [30, 30])
+            B.cs_kv_append(c.plan, 0, k, -k, rotate=False)
+            B.cs_plan_set(other, [1], [1])                           # its buffers are made
+            torch.cuda.synchronize()
+            out, seen = torch.zeros_like(q), torch.zeros(21, 2, 128, dtype=torch.float16, device="cuda")
+            unused = torch.empty_like(seen)
+            place = (torch.full((21,), 1, dtype=torch.int32, device="cuda"), torch.arange(21, dtype=torch.int32, device="cuda"))
+            one, two = torch.cuda.Stream(), torch.cuda.Stream()
+            for s in (one, two):
+                s.wait_stream(torch.cuda.current_stream())
+            c.pages = c.pages[::-1].copy()
+            c.set([20, 20])
+            with torch.cuda.stream(one):
+                if delayed:
+                    torch.cuda._sleep(100_000_000)
+                B.cs_plan_set(c.plan, [0], [1])                      # uploads the table
+            with torch.cuda.stream(two):
+                B.cs_plan_set(other, [1], [1])
+                B.cs_kv_append(other, 0, new, -new, rotate=False)
+                if fmt == "int4":
+                    B.cs_attention_4bit(other, 0, q, out)
+                B.cs_kv_read(c.kv, 0, *place, seen, unused)
+            torch.cuda.synchronize()
+            # a read by itself on another stream than the upload's
+            c.pages = c.pages[::-1].copy()
+            c.set([20, 20])
+            alone = torch.zeros_like(seen)
+            with torch.cuda.stream(one):
+                if delayed:
+                    torch.cuda._sleep(100_000_000)
+                B.cs_plan_set(c.plan, [0], [1])
+            with torch.cuda.stream(two):
+                B.cs_kv_read(c.kv, 0, *place, alone, unused)
+            torch.cuda.synchronize()
+            results.append([t.clone() for t in (out, seen, alone)])
+            B.cs_plan_free(other)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert not torch.equal(results[0][1][:20], results[0][2][:20])
