@@ -1611,9 +1611,9 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   cs_kv* kv = p->kv;
   const cs_model_desc& d = kv->model->d;
   if (kv->format != CS_KV_FMT_INT4 || !(scale >= 0.f) || scale > 3.0e38f) return CS_EINVAL;
-  if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;
   if (!plan_stands(p, false)) return CS_ESTATE;
-  if (p->T == 0) return CS_OK;
+  if (p->T == 0) return CS_OK;                  // no tokens, and rows of no tokens may have no address
+  if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;
   const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
   if (!rows_ok(q, q_stride, q_row) || !rows_ok(out, out_stride, q_row)) return CS_EINVAL;
   if (p->given && (!rows_ok(k_new, kv_stride, kv_row) || !rows_ok(v_new, kv_stride, kv_row))) return CS_EINVAL;

@@ -377,3 +377,22 @@ def test_the_page_table_reaches_every_stream(fmt):
     for a, b in zip(*results):
         assert torch.equal(a, b)
     assert not torch.equal(results[0][1][:20], results[0][2][:20])
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("made", ["slice", "empty"])
+def test_an_empty_plan_takes_rows_of_no_tokens(given, made):
+    """Tensors without elements may have no address: nothing is done, and nothing refused."""
+    import torch
+    rows = lambda h: (torch.zeros(3, h, 128, dtype=torch.float16, device="cuda")[:0] if made == "slice"  # noqa: E731
+                      else torch.empty(0, h, 128, dtype=torch.float16, device="cuda"))
+    with K.Cache(4, 2, 128, n_seqs=2) as c:
+        c.B.cs_plan_set(c.plan, [], [], given=given)
+        torch.cuda.synchronize()
+        c.B.cs_take_launch_count()
+        c.B.cs_attention_4bit(c.plan, 0, rows(4), rows(4), *((rows(2), rows(2)) if given else (None, None)))
+        c.B.cs_kv_append(c.plan, 0, rows(2), rows(2), q=rows(4), q_out=rows(4))
+        c.B.cs_kv_commit(c.plan)
+        none = torch.empty(0, dtype=torch.int32, device="cuda")
+        c.B.cs_kv_read(c.kv, 0, none, none, rows(2), rows(2))
+        assert c.B.cs_take_launch_count() == 0
