@@ -30,6 +30,17 @@ int cuda_fail(cudaError_t e, const char* what) {
     if (e__ != cudaSuccess) return cuda_fail(e__, #call); \
   } while (0)
 
+// What a C entry with host lists answers when their memory is not to be had: no exception may leave the library.
+template <typename F>
+int guarded(F&& body) {
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    g_cuda_error.clear();
+    return CS_ENOMEM;
+  }
+}
+
 constexpr int kPageSize = 16;
 constexpr int kStagingRing = 4;
 
@@ -1166,9 +1177,13 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
   kv->max_seqs = max_seqs;
   kv->max_pages_per_seq = max_pages_per_seq;
   kv->plane_elems = static_cast<size_t>(num_pages) * m->d.n_kv_heads * page_size * m->d.head_dim;
-  kv->ctx_len.assign(max_seqs, -1);
-  kv->n_pages.assign(max_seqs, 0);
-  kv->set_count.assign(max_seqs, 0);
+  const int lists = guarded([&] {
+    kv->ctx_len.assign(max_seqs, -1);
+    kv->n_pages.assign(max_seqs, 0);
+    kv->set_count.assign(max_seqs, 0);
+    return CS_OK;
+  });
+  if (lists != CS_OK) { cs_kv_free(kv); return lists; }
   const uint64_t bytes = format == CS_KV_FMT_INT4 ? kv->layer4_bytes() * m->d.n_layers
                                                   : cs_kv_pool_bytes(m, num_pages, page_size) / (format != 0 ? 2 : 1);
   int rc = CS_OK;
@@ -1250,7 +1265,7 @@ int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int 
   return CS_OK;
 }
 
-int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint16_t* host_v, void* stream) {
+static int kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint16_t* host_v, void* stream) {
   if (!kv || seq < 0 || seq >= kv->max_seqs || layer < 0 || layer >= kv->model->d.n_layers) return CS_EINVAL;
   if (kv->ctx_len[seq] < 0) return CS_ESTATE;
   const int c = kv->ctx_len[seq];
@@ -1304,6 +1319,10 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
                             kPageSize, c, 0, kv->num_pages, nullptr, s));
   CS_CUDA(cudaStreamSynchronize(s));
   return CS_OK;
+}
+
+int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint16_t* host_v, void* stream) {
+  return guarded([&] { return kv_fill(kv, seq, layer, host_k, host_v, stream); });
 }
 
 // Nothing may be uploaded from inside a stream capture: the page table has to be on the device already (a replay is ordered behind
@@ -1483,11 +1502,7 @@ static int plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int
 }
 
 int cs_plan_set(cs_plan* p, const int32_t* seq_ids, const int32_t* lens, int B, int given, void* stream) {
-  try {
-    return plan_set(p, seq_ids, lens, B, given, stream);
-  } catch (const std::bad_alloc&) {      // host memory for the work lists
-    return CS_ENOMEM;
-  }
+  return guarded([&] { return plan_set(p, seq_ids, lens, B, given, stream); });
 }
 
 // What every call on a plan checks: set, the right device, a layer of the model, a known type.
@@ -1682,8 +1697,8 @@ int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_
   return CS_OK;
 }
 
-int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* tokens, const int32_t* lens, int B,
-               void* stream) {
+static int prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* tokens, const int32_t* lens, int B,
+                   void* stream) {
   if (!m || !kv || kv->model != m || B < 0) return CS_EINVAL;
   if (kv->format != CS_KV_FMT_16BIT && kv->format != CS_KV_FMT_INT4) return CS_EINVAL;   // the pass does not append to the 8-bit cache
   if (B == 0) return CS_OK;
@@ -1707,9 +1722,14 @@ int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* to
   return CS_OK;
 }
 
-int cs_append_accepted(cs_model* m, cs_kv* kv, int R, const int32_t* req_seq_ids, const int32_t* req_offsets,
-                       const int32_t* dev_prefix_len, const int32_t* step_tokens, const int32_t* step_lens,
-                       const int32_t* draft_lens, int32_t* host_prefix_len, void* stream) {
+int cs_prefill(cs_model* m, cs_kv* kv, const int32_t* seq_ids, const int32_t* tokens, const int32_t* lens, int B,
+               void* stream) {
+  return guarded([&] { return prefill(m, kv, seq_ids, tokens, lens, B, stream); });
+}
+
+static int append_accepted(cs_model* m, cs_kv* kv, int R, const int32_t* req_seq_ids, const int32_t* req_offsets,
+                           const int32_t* dev_prefix_len, const int32_t* step_tokens, const int32_t* step_lens,
+                           const int32_t* draft_lens, int32_t* host_prefix_len, void* stream) {
   if (!m || !kv || kv->model != m || R < 0 || (kv->format != CS_KV_FMT_16BIT && kv->format != CS_KV_FMT_INT4)) return CS_EINVAL;
   if (R == 0) return CS_OK;
   if (!req_seq_ids || !req_offsets || !dev_prefix_len || !step_tokens || !step_lens || !draft_lens) return CS_EINVAL;
@@ -1752,9 +1772,18 @@ int cs_append_accepted(cs_model* m, cs_kv* kv, int R, const int32_t* req_seq_ids
   return cs_prefill(m, kv, seqs.data(), toks.data(), lens.data(), static_cast<int>(seqs.size()), stream);
 }
 
-int cs_verify_steps(cs_model* m, const cs_kv* ckv, const int32_t* seq_ids, int B, const int32_t* step_tokens,
-                    int tokens_on_device, const int32_t* step_lens, const int32_t* verdict_ids, int n_verdict,
-                    float tau, float* out_conf, uint8_t* out_accept, int32_t* out_verdict, void* stream) {
+int cs_append_accepted(cs_model* m, cs_kv* kv, int R, const int32_t* req_seq_ids, const int32_t* req_offsets,
+                       const int32_t* dev_prefix_len, const int32_t* step_tokens, const int32_t* step_lens,
+                       const int32_t* draft_lens, int32_t* host_prefix_len, void* stream) {
+  return guarded([&] {
+    return append_accepted(m, kv, R, req_seq_ids, req_offsets, dev_prefix_len, step_tokens, step_lens, draft_lens,
+                           host_prefix_len, stream);
+  });
+}
+
+static int verify_steps(cs_model* m, const cs_kv* ckv, const int32_t* seq_ids, int B, const int32_t* step_tokens,
+                        int tokens_on_device, const int32_t* step_lens, const int32_t* verdict_ids, int n_verdict,
+                        float tau, float* out_conf, uint8_t* out_accept, int32_t* out_verdict, void* stream) {
   if (!m || !ckv || ckv->model != m || B < 0) return CS_EINVAL;
   if (tau != tau) return CS_EINVAL;
   if (n_verdict < 1 || n_verdict > 8 || !verdict_ids) return CS_EINVAL;
@@ -1804,6 +1833,15 @@ int cs_verify_steps(cs_model* m, const cs_kv* ckv, const int32_t* seq_ids, int B
   return CS_OK;
 }
 
+int cs_verify_steps(cs_model* m, const cs_kv* ckv, const int32_t* seq_ids, int B, const int32_t* step_tokens,
+                    int tokens_on_device, const int32_t* step_lens, const int32_t* verdict_ids, int n_verdict,
+                    float tau, float* out_conf, uint8_t* out_accept, int32_t* out_verdict, void* stream) {
+  return guarded([&] {
+    return verify_steps(m, ckv, seq_ids, B, step_tokens, tokens_on_device, step_lens, verdict_ids, n_verdict, tau, out_conf,
+                        out_accept, out_verdict, stream);
+  });
+}
+
 int cs_escalate_mask(const float* conf, int B, float tau, uint8_t* out_accept, int32_t* out_idx, int32_t* out_count,
                      void* stream) {
   if (B < 0 || B > 65536 || tau != tau || !out_count) return CS_EINVAL;
@@ -1812,11 +1850,11 @@ int cs_escalate_mask(const float* conf, int B, float tau, uint8_t* out_accept, i
   return CS_OK;
 }
 
-int cs_verify_cascade(cs_model* draft, const cs_kv* kv_d, cs_model* target, const cs_kv* kv_t, const int32_t* seq_ids,
-                      int B, const int32_t* step_tokens, const int32_t* step_lens, const int32_t* verdict_ids,
-                      int n_verdict, float tau, float* out_conf_d, uint8_t* out_trusted, int32_t* out_verdict_d,
-                      float* out_conf_t, int32_t* out_verdict_t, int32_t* out_verdict, float* out_conf,
-                      const int32_t* req_offsets, int R, int accept_index, int32_t* host_n_escalated, void* stream) {
+static int verify_cascade(cs_model* draft, const cs_kv* kv_d, cs_model* target, const cs_kv* kv_t, const int32_t* seq_ids,
+                          int B, const int32_t* step_tokens, const int32_t* step_lens, const int32_t* verdict_ids,
+                          int n_verdict, float tau, float* out_conf_d, uint8_t* out_trusted, int32_t* out_verdict_d,
+                          float* out_conf_t, int32_t* out_verdict_t, int32_t* out_verdict, float* out_conf,
+                          const int32_t* req_offsets, int R, int accept_index, int32_t* host_n_escalated, void* stream) {
   if (!draft || !target || draft == target || !kv_d || !kv_t || kv_d->model != draft || kv_t->model != target || B < 0)
     return CS_EINVAL;
   if (tau != tau || n_verdict < 1 || n_verdict > 8 || !verdict_ids) return CS_EINVAL;
@@ -1901,6 +1939,18 @@ int cs_verify_cascade(cs_model* draft, const cs_kv* kv_d, cs_model* target, cons
   CS_CUDA(launch_cascade_scatter(B, out_trusted, out_verdict_d, out_conf_d, idx, count, verdict_c, conf_c, out_verdict_t,
                                  out_conf_t, out_verdict, out_conf, s));
   return CS_OK;
+}
+
+int cs_verify_cascade(cs_model* draft, const cs_kv* kv_d, cs_model* target, const cs_kv* kv_t, const int32_t* seq_ids,
+                      int B, const int32_t* step_tokens, const int32_t* step_lens, const int32_t* verdict_ids,
+                      int n_verdict, float tau, float* out_conf_d, uint8_t* out_trusted, int32_t* out_verdict_d,
+                      float* out_conf_t, int32_t* out_verdict_t, int32_t* out_verdict, float* out_conf,
+                      const int32_t* req_offsets, int R, int accept_index, int32_t* host_n_escalated, void* stream) {
+  return guarded([&] {
+    return verify_cascade(draft, kv_d, target, kv_t, seq_ids, B, step_tokens, step_lens, verdict_ids, n_verdict, tau,
+                          out_conf_d, out_trusted, out_verdict_d, out_conf_t, out_verdict_t, out_verdict, out_conf,
+                          req_offsets, R, accept_index, host_n_escalated, stream);
+  });
 }
 
 int cs_cascade_select(const uint8_t* trusted, const int32_t* verdict_d, const float* conf_d, const int32_t* verdict_t,

@@ -396,3 +396,61 @@ def test_an_empty_plan_takes_rows_of_no_tokens(given, made):
         none = torch.empty(0, dtype=torch.int32, device="cuda")
         c.B.cs_kv_read(c.kv, 0, none, none, rows(2), rows(2))
         assert c.B.cs_take_launch_count() == 0
+
+
+_SHORT_OF_MEMORY = """
+import ctypes, resource, sys
+import numpy as np, torch
+import kv4_common as K
+assert ctypes.CDLL(None).mallopt(-3, 65536)          # lists from 64 KB on are mapped one by one, so that the limit meets each
+pages, n = 32768, 2000
+with K.Cache(2, 1, 64, n_seqs=1, pages_each=pages) as c:
+    B = c.B
+    bits = np.zeros((16 * pages, 1, 64), np.uint16)
+    prompt = np.full(100000, 5, np.int32)
+    steps, ones, toks = np.zeros(n, np.int32), np.ones(n, np.int32), np.full(n, 5, np.int32)
+    conf, acc = torch.empty(n, device="cuda"), torch.empty(n, dtype=torch.uint8, device="cuda")
+    def fill():
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0], 16 * pages)
+        B.cs_kv_fill(c.kv, 0, 0, bits, bits)
+    def verify():
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0], 64)
+        B.cs_verify_steps(c.model, c.kv, steps, toks, ones, [1, 2], 0.5, conf, acc)
+    def plan():
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0], 64)
+        B.cs_plan_set(c.plan, steps, ones, given=True)
+    def prefill():
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0], 64)
+        B.cs_prefill(c.model, c.kv, [0], prompt, [100000])
+    for call in (fill, verify, plan, prefill):
+        call()                                       # buffers are made
+        call()
+        torch.cuda.synchronize()
+        now = resource.getrlimit(resource.RLIMIT_AS)
+        got = None
+        resource.setrlimit(resource.RLIMIT_AS, (int(open("/proc/self/statm").read().split()[0]) * 4096 + 16384, now[1]))
+        try:
+            call()
+        except B.ConfSpecError as e:
+            got = e.status
+        finally:
+            resource.setrlimit(resource.RLIMIT_AS, now)
+        torch.cuda.synchronize()
+        print(call.__name__, got, flush=True)
+        assert got == B.CS_ENOMEM
+        call()
+    torch.cuda.synchronize()
+print("done")
+"""
+
+
+def test_host_memory_that_runs_out_is_an_error_status():
+    """The lists of work are made in host memory: where it is not to be had the call returns CS_ENOMEM, and works again later. A process
+    of its own, under a limit on its address space."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([here, os.path.dirname(here), os.environ.get("PYTHONPATH", "")]))
+    r = subprocess.run([sys.executable, "-c", _SHORT_OF_MEMORY], capture_output=True, text=True, timeout=300, env=env)
+    assert r.returncode == 0 and r.stdout.strip().endswith("done"), (r.returncode, r.stdout[-500:], r.stderr[-1500:])
