@@ -243,7 +243,8 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  *                      for given = 0, where they are read from the cache. Non-finite values count as cs_kv_append stores them
  *                      (no token's row can spoil the tokens in front of it).
  *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
- *   scale              0: 1 / sqrt(head_dim); else > 0 and finite.
+ *   scale              0: 1 / sqrt(head_dim); else > 0 and at most 2^60. Steps of more than 96 query rows per kv head: scores
+ *                      (scale q . k) beyond 2^25 in magnitude may come out as NaN.
  * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; a row with a
  * larger query comes out as NaN), sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number of new tokens:
  * up to 96 query rows per kv head read the 4-bit pages directly; a batch with a longer step has its rows and contexts put together

@@ -1625,7 +1625,8 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   if ((rc = plan_ready(p, layer, dtype))) return rc;
   cs_kv* kv = p->kv;
   const cs_model_desc& d = kv->model->d;
-  if (kv->format != CS_KV_FMT_INT4 || !(scale >= 0.f) || scale > 3.0e38f) return CS_EINVAL;
+  // Scores of up to 128 x 65524^2 = 2^39 times log2(e) scale stay below 2^100, from where on a score counts as none (kNoMax).
+  if (kv->format != CS_KV_FMT_INT4 || !(scale >= 0.f) || scale > 0x1p60f) return CS_EINVAL;
   if (!plan_stands(p, false)) return CS_ESTATE;
   if (p->T == 0) return CS_OK;                  // no tokens, and rows of no tokens may have no address
   if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;

@@ -385,7 +385,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
           const float sc = e ? scale[nt].y : scale[nt].x;
           float mx = kNoMax;
 #pragma unroll
-          for (int pp = 0; pp < NP; ++pp) mx = fmaxf(mx, fmaxf(s[pp][nt][e], s[pp][nt][e + 2]) * sc);
+          for (int pp = 0; pp < NP; ++pp) mx = fmaxf(mx, __fmul_rn(fmaxf(s[pp][nt][e], s[pp][nt][e + 2]), sc));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
           mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
@@ -401,8 +401,9 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
           }
 #pragma unroll
           for (int pp = 0; pp < NP; ++pp) {
-            x[pp][nt][e] = fmaf(s[pp][nt][e], sc, -m_new);
-            x[pp][nt][e + 2] = fmaf(s[pp][nt][e + 2], sc, -m_new);
+            // rounded as the maximum was: of scores above 2^24 the fused form would leave the products' roundings as exponents
+            x[pp][nt][e] = __fsub_rn(__fmul_rn(s[pp][nt][e], sc), m_new);
+            x[pp][nt][e + 2] = __fsub_rn(__fmul_rn(s[pp][nt][e + 2], sc), m_new);
           }
         }
     }

@@ -454,3 +454,38 @@ def test_host_memory_that_runs_out_is_an_error_status():
     env = dict(os.environ, PYTHONPATH=os.pathsep.join([here, os.path.dirname(here), os.environ.get("PYTHONPATH", "")]))
     r = subprocess.run([sys.executable, "-c", _SHORT_OF_MEMORY], capture_output=True, text=True, timeout=300, env=env)
     assert r.returncode == 0 and r.stdout.strip().endswith("done"), (r.returncode, r.stdout[-500:], r.stderr[-1500:])
+
+
+@pytest.mark.parametrize("n", [2, 60])                                  # 4 and 120 query rows
+def test_the_largest_scale_and_the_refusal_of_larger_ones(n):
+    """The best key takes all the weight, where every score is far below zero too: its value, off by the roundings of p s (2^-11 of
+    8 s), of the output (2^-11) and, expanded, of the value (2^-11). A scale of 2^60 over the 4-bit pages; scores of 2^24 for long steps."""
+    import torch
+    rng = np.random.default_rng(51)
+    k, v = np.abs(rng.standard_normal((40, 1, 128))) * 100.0, rng.standard_normal((40, 1, 128))
+    q = _dev(-np.abs(rng.standard_normal((n, 2, 128))) * 10.0, "float16")
+    k, v = _dev(k, "float16"), _dev(v, "float16")
+    new = _dev(np.full((n, 1, 128), 400.0), "float16")                   # worse than every cached key
+    with K.Cache(2, 1, 128, n_seqs=1) as c:
+        c.B.cs_plan_set(c.plan, [0], [40])
+        c.B.cs_kv_append(c.plan, 0, k, v, rotate=False)
+        c.B.cs_kv_commit(c.plan)
+        c.B.cs_plan_set(c.plan, [0], [n], given=True)
+        out = torch.full_like(q, float("nan"))
+        kq, vq = _quantise(_np(k)), _quantise(_np(v))
+        xk, xv = K.values(*kq)[:, 0], K.values(*vq)[:, 0]
+        scores = np.einsum("thd,kd->thk", _np(q), xk)
+        c.B.cs_attention_4bit(c.plan, 0, q, out, new, new, scale=2.0 ** 60 if n == 2 else float(2.0 ** 24 / np.abs(scores).max()))
+        torch.cuda.synchronize()
+        two = np.sort(scores, -1)[..., -2:]
+        clear = two[..., 1] - two[..., 0] > 2.0 ** -12 * np.abs(two[..., 0])
+        assert clear.mean() > 0.9
+        want = xv[scores.argmax(-1)]
+        err = np.abs(_np(out) - want)[clear]
+        assert np.all(err <= 2.0 ** -11 * (8 * vq[1].max() + 2 * np.abs(want[clear])) + 2.0 ** -24)
+        c.B.cs_take_launch_count()
+        for scale in (2.0 ** 61, 1e25, 3e38, float("inf"), float("nan"), -1.0):
+            with pytest.raises(c.B.ConfSpecError) as e:
+                c.B.cs_attention_4bit(c.plan, 0, q, out, new, new, scale=scale)
+            assert e.value.status == c.B.CS_EINVAL
+        assert c.B.cs_take_launch_count() == 0
