@@ -224,7 +224,7 @@ int cs_kv_commit(cs_plan* plan);
  *   rotate != 0        pairs (j, j + head_dim/2) of every K head turn by the token's position, in fp32; the result is stored
  *                      without an intermediate rounding. rotate == 0: K is stored as it is (already rotated).
  *   q, q_out           device rows [T, n_q_heads, head_dim] or both NULL: the queries, turned and rounded to `dtype`. Only with
- *                      rotate != 0. q_out may be q itself.
+ *                      rotate != 0. q_out may be q itself, with the same stride (CS_EINVAL otherwise).
  * Stored: 16-bit: the nearest bf16 value in the fp16 encoding; 8-bit: the nearest value of the format, ties to even; 4-bit: as at
  * cs_kv_alloc_4bit. NaN is stored as 0 and magnitudes saturate at the format's largest (65504, 448, 57344), so that no row can
  * spoil another sequence that meets it behind its own end. Slots of other tokens keep their bytes.
@@ -242,7 +242,7 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  *   k_new, v_new       device rows [T, n_kv_heads, head_dim] of the new tokens (keys turned), for a plan with given = 1; NULL
  *                      for given = 0, where they are read from the cache. Non-finite values count as cs_kv_append stores them
  *                      (no token's row can spoil the tokens in front of it).
- *   out                device rows [T, n_q_heads, head_dim]; may be q itself with the same stride.
+ *   out                device rows [T, n_q_heads, head_dim]; may be q itself, with the same stride (CS_EINVAL otherwise).
  *   scale              0: 1 / sqrt(head_dim); else > 0 and at most 2^60. Steps of more than 96 query rows per kv head: scores
  *                      (scale q . k) beyond 2^25 in magnitude may come out as NaN.
  * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; a row with a

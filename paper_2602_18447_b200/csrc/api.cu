@@ -1542,6 +1542,7 @@ int cs_kv_append(cs_plan* p, int layer, const uint16_t* k, int64_t k_stride, con
   const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
   if (!rows_ok(k, k_stride, kv_row) || !rows_ok(v, v_stride, kv_row)) return CS_EINVAL;
   if (q && (!rows_ok(q, q_stride, q_row) || !rows_ok(q_out, q_out_stride, q_row))) return CS_EINVAL;
+  if (q && q == q_out && q_stride != q_out_stride && p->T > 1) return CS_EINVAL;      // rows would be written over others' inputs
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((rc = table_ready(p->kv, s))) return rc;
   KvAppendParams a = {};
@@ -1632,6 +1633,7 @@ int cs_attention_4bit(cs_plan* p, int layer, const uint16_t* q, int64_t q_stride
   if (p->given ? (!k_new || !v_new) : (k_new || v_new)) return CS_EINVAL;
   const int64_t kv_row = static_cast<int64_t>(d.n_kv_heads) * d.head_dim, q_row = static_cast<int64_t>(d.n_q_heads) * d.head_dim;
   if (!rows_ok(q, q_stride, q_row) || !rows_ok(out, out_stride, q_row)) return CS_EINVAL;
+  if (q == out && q_stride != out_stride && p->T > 1) return CS_EINVAL;               // rows would be written over others' inputs
   if (p->given && (!rows_ok(k_new, kv_stride, kv_row) || !rows_ok(v_new, kv_stride, kv_row))) return CS_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((rc = table_ready(kv, s))) return rc;

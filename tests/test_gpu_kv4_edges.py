@@ -489,3 +489,27 @@ def test_the_largest_scale_and_the_refusal_of_larger_ones(n):
                 c.B.cs_attention_4bit(c.plan, 0, q, out, new, new, scale=scale)
             assert e.value.status == c.B.CS_EINVAL
         assert c.B.cs_take_launch_count() == 0
+
+
+def test_in_place_needs_one_stride():
+    """Rows written from where they are read, but further apart or closer, would land on rows that are still to be read."""
+    import torch
+    buf = torch.zeros(8, 1024, dtype=torch.float16, device="cuda")
+    near, far, k = buf.view(16, 512)[:4], buf[:4, :512], torch.zeros(4, 256, dtype=torch.float16, device="cuda")
+    with K.Cache(4, 2, 128, n_seqs=1) as c:
+        B = c.B
+        B.cs_plan_set(c.plan, [0], [4])
+        torch.cuda.synchronize()
+        B.cs_take_launch_count()
+        for q, out in ((near, far), (far, near)):
+            for call in (lambda: B.cs_attention_4bit(c.plan, 0, q, out), lambda: B.cs_kv_append(c.plan, 0, k, k, q=q, q_out=out)):
+                with pytest.raises(B.ConfSpecError) as e:
+                    call()
+                assert e.value.status == B.CS_EINVAL
+        assert B.cs_take_launch_count() == 0
+        for q in (near, far):
+            B.cs_kv_append(c.plan, 0, k, k, q=q, q_out=q)
+            B.cs_attention_4bit(c.plan, 0, q, q)
+        B.cs_plan_set(c.plan, [0], [1])
+        B.cs_attention_4bit(c.plan, 0, near[:1], far[:1])
+        torch.cuda.synchronize()
