@@ -73,6 +73,8 @@ struct DevBuf {
     if (zero && (e = cudaMemset(p, 0, want)) != cudaSuccess) return cuda_fail(e, "cudaMemset(workspace)");
     if ((e = cudaMemset(static_cast<uint8_t*>(p) + want, kCanaryByte, kCanaryBytes)) != cudaSuccess)
       return cuda_fail(e, "cudaMemset(workspace canary)");
+    // the fills run on the legacy stream, which streams made with cudaStreamNonBlocking do not wait for
+    if ((e = cudaStreamSynchronize(nullptr)) != cudaSuccess) return cuda_fail(e, "workspace fill");
     cap = want;
     return CS_OK;
   }
@@ -1204,6 +1206,7 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&kv->table_dev), tbytes);
   if (e == cudaSuccess) e = cudaMemset(kv->table_dev, 0, tbytes);
   if (e == cudaSuccess) e = cudaEventCreateWithFlags(&kv->upload_ev, cudaEventDisableTiming);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);      // the zeros are in place before any stream writes rows
   if (e != cudaSuccess) { rc = cuda_fail(e, "kv page table"); cs_kv_free(kv); return rc; }
   std::memset(kv->table_host, 0, tbytes);
   if (format == 0 && !make_kv_group_map(&kv->tm_pool, kv->pool, rows, m->d.head_dim, kPageSize / 8)) {

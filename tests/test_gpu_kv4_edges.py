@@ -513,3 +513,33 @@ def test_in_place_needs_one_stride():
         B.cs_plan_set(c.plan, [0], [1])
         B.cs_attention_4bit(c.plan, 0, near[:1], far[:1])
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["int4", "16bit"])
+def test_a_new_cache_is_zero_before_any_stream_writes_to_it(fmt):
+    """The last pages of a large pool, written on a stream of its own right behind the allocation: the zero fill has ended."""
+    import torch
+    rng = np.random.default_rng(61)
+    k = _dev(rng.standard_normal((20, 8, 128)), "float16")
+    with K.Cache(8, 8, 128, n_seqs=1) as c:
+        B, pages = c.B, 1 << (20 if fmt == "int4" else 18)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        alloc = B.cs_kv_alloc_4bit if fmt == "int4" else B.cs_kv_alloc
+        for _ in range(2):
+            kv = alloc(c.model, pages, 16, 1, 2)
+            B.cs_kv_set_seq(kv, 0, [pages - 1, pages - 2], 0)
+            with torch.cuda.stream(side):
+                plan = B.cs_plan_create(kv)
+                B.cs_plan_set(plan, [0], [20])
+                B.cs_kv_append(plan, 0, k, -k, rotate=False)
+            torch.cuda.synchronize()
+            out_k, out_v = torch.zeros_like(k), torch.zeros_like(k)
+            B.cs_kv_read(kv, 0, torch.zeros(20, dtype=torch.int32, device="cuda"), torch.arange(20, dtype=torch.int32, device="cuda"),
+                         out_k, out_v)
+            torch.cuda.synchronize()
+            B.cs_plan_free(plan)
+            B.cs_kv_free(kv)
+            want = K.values(*_quantise(_np(k))) if fmt == "int4" else _np(k.bfloat16())
+            assert np.array_equal(_np(out_k), want.astype(np.float16).astype(np.float64))
+            assert bool((out_v != 0).any())
