@@ -255,9 +255,9 @@ int cs_attention_4bit(cs_plan* plan, int layer, const uint16_t* q, int64_t q_str
                       void* stream);
 /*
  * cs_kv_read - rows of one layer of a cache, any format, as the values that they stand for.
- *   tok_seq, tok_pos   DEVICE int32[T]: sequence and position of each row. A place outside the page table gives a row of
- *                      zeros, and the next cs_last_status of the model returns CS_ERANGE. Positions that were never written
- *                      hold zeros or what the page's last user left.
+ *   tok_seq, tok_pos   DEVICE int32[T]: sequence and position of each row. A place outside the sequence's pages gives a row of
+ *                      zeros, and the next cs_last_status of the model returns CS_ERANGE. Positions of its pages that were never
+ *                      written hold zeros or what the page's last user left.
  *   out_k, out_v       device [T, n_kv_heads, head_dim] in `dtype`, contiguous (rounded once from fp32; fp16 at most 65504).
  */
 int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_pos, int T, uint16_t* out_k,

@@ -157,7 +157,7 @@ struct cs_kv {
   int format = 0;
   size_t plane_elems;  // elements of one (layer, K or V) plane
   CUtensorMap tm_pool;
-  int32_t* table_host = nullptr;  // pinned [max_seqs, max_pages_per_seq]
+  int32_t* table_host = nullptr;  // pinned [max_seqs, max_pages_per_seq], then the sequences' page counts [max_seqs]
   int32_t* table_dev = nullptr;
   std::vector<int32_t> ctx_len, n_pages;  // per sequence; ctx_len < 0 = not set
   std::vector<uint64_t> set_count;        // how often cs_kv_set_seq has set the sequence
@@ -167,6 +167,8 @@ struct cs_kv {
   bool upload_pending = false;
   bool upload_unseen = false;      // the last upload has not been seen to have ended: other streams have to wait for it
   DevBuf fill_tmp;
+  size_t table_entries() const { return static_cast<size_t>(max_seqs) * max_pages_per_seq; }
+  size_t table_bytes() const { return sizeof(int32_t) * (table_entries() + max_seqs); }
   size_t layer4_bytes() const {
     return static_cast<size_t>(num_pages) * model->d.n_kv_heads * kv4_block_bytes(model->d.head_dim);
   }
@@ -209,9 +211,7 @@ int upload_table(cs_kv* kv, cudaStream_t s) {
     CS_CUDA(cudaStreamWaitEvent(s, kv->upload_ev, 0));
     return CS_OK;
   }
-  CS_CUDA(cudaMemcpyAsync(kv->table_dev, kv->table_host,
-                          sizeof(int32_t) * static_cast<size_t>(kv->max_seqs) * kv->max_pages_per_seq,
-                          cudaMemcpyHostToDevice, s));
+  CS_CUDA(cudaMemcpyAsync(kv->table_dev, kv->table_host, kv->table_bytes(), cudaMemcpyHostToDevice, s));
   CS_CUDA(cudaEventRecord(kv->upload_ev, s));
   kv->upload_pending = true;
   kv->upload_unseen = true;
@@ -1201,7 +1201,7 @@ static int kv_alloc_impl(const cs_model* m, int num_pages, int page_size, int ma
     e = cudaMemset(p, 0, bytes);
     if (e != cudaSuccess) { rc = cuda_fail(e, "cudaMemset(kv pool)"); cs_kv_free(kv); return rc; }
   }
-  const size_t tbytes = sizeof(int32_t) * static_cast<size_t>(max_seqs) * max_pages_per_seq;
+  const size_t tbytes = kv->table_bytes();
   e = cudaMallocHost(reinterpret_cast<void**>(&kv->table_host), tbytes);
   if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&kv->table_dev), tbytes);
   if (e == cudaSuccess) e = cudaMemset(kv->table_dev, 0, tbytes);
@@ -1262,6 +1262,7 @@ int cs_kv_set_seq(cs_kv* kv, int seq, const int32_t* page_ids, int n_pages, int 
   for (int i = 0; i < n_pages; ++i) row[i] = page_ids[i];
   kv->ctx_len[seq] = ctx_len;
   kv->n_pages[seq] = n_pages;
+  kv->table_host[kv->table_entries() + seq] = n_pages;
   ++kv->set_count[seq];
   ++kv->changes;
   kv->dirty = true;
@@ -1688,6 +1689,7 @@ int cs_kv_read(cs_kv* kv, int layer, const int32_t* tok_seq, const int32_t* tok_
   r.pool_k = kv->format == CS_KV_FMT_INT4 ? pool + layer * kv->layer4_bytes() : pool + 2 * layer * plane;
   r.pool_v = kv->format == CS_KV_FMT_INT4 ? nullptr : pool + (2 * layer + 1) * plane;
   r.table = kv->table_dev;
+  r.n_pages = kv->table_dev + kv->table_entries();
   r.tok_seq = tok_seq;
   r.tok_pos = tok_pos;
   r.out_k = out_k;

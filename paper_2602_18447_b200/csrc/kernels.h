@@ -126,7 +126,8 @@ struct KvAppendParams {
 cudaError_t launch_kv_append(KvAppendParams p, int format, int hd, int n_blocks, cudaStream_t s);
 struct KvReadParams {
   const uint8_t *pool_k, *pool_v;
-  const int32_t *table, *tok_seq, *tok_pos;
+  const int32_t *table, *n_pages;  // page table [max_seqs, max_pages_per_seq], pages of each sequence [max_seqs]
+  const int32_t *tok_seq, *tok_pos;
   uint16_t *out_k, *out_v;         // [T, n_kv_heads, head_dim], fp16 or bf16 (dst_bf16)
   int32_t T, max_seqs, max_pages_per_seq, num_pages, n_kv_heads, dst_bf16;
   uint32_t* status;

@@ -457,17 +457,18 @@ __device__ __forceinline__ void block_rows(const uint8_t* b, int lane, uint16_t*
   }
 }
 
-// Page id of a listed place, or -1 outside the page table.
+// Page id of a listed place, or -1 outside the sequence's pages.
 __device__ __forceinline__ int listed_page(const KvReadParams& p, int row, int& pos) {
   const int seq = p.tok_seq[row];
   pos = p.tok_pos[row];
   if (seq < 0 || seq >= p.max_seqs || pos < 0 || pos / kPage >= p.max_pages_per_seq) return -1;
+  const int n = __ldg(p.n_pages + seq);      // beside the next load, not behind it
   const int page = __ldg(p.table + static_cast<size_t>(seq) * p.max_pages_per_seq + pos / kPage);
-  return page < p.num_pages ? page : -1;
+  return (page < p.num_pages) & (pos / kPage < n) ? page : -1;
 }
 
-// Rows listed by (sequence, position) out of a 16-bit or 8-bit cache: one thread per row and 8 channels. A place outside the page
-// table gives a row of zeros and raises the range bit of the status word.
+// Rows listed by (sequence, position) out of a 16-bit or 8-bit cache: one thread per row and 8 channels. A place outside the sequence's
+// pages gives a row of zeros and raises the range bit of the status word.
 template <int HD, int FMT, bool BF16>
 __global__ void __launch_bounds__(2 * HD) kv_read_kernel(const KvReadParams p) {
   constexpr int CH = HD / 8;

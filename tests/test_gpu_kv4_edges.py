@@ -543,3 +543,25 @@ def test_a_new_cache_is_zero_before_any_stream_writes_to_it(fmt):
             want = K.values(*_quantise(_np(k))) if fmt == "int4" else _np(k.bfloat16())
             assert np.array_equal(_np(out_k), want.astype(np.float16).astype(np.float64))
             assert bool((out_v != 0).any())
+
+
+@pytest.mark.parametrize("fmt", ["int4", "16bit", "e4m3"])
+def test_reading_ends_with_a_sequences_own_pages(fmt):
+    """A sequence that has given pages up, and one that was never set, have no rows there: zeros and a status, not what the table's
+    entries last named."""
+    rng = np.random.default_rng(71)
+    k = _dev(np.abs(rng.standard_normal((48, 2, 64))) + 1.0, "float16")
+    with K.Cache(2, 2, 64, n_seqs=2, pages_each=3, fmt=fmt) as c:
+        B = c.B
+        B.cs_plan_set(c.plan, [0], [48])
+        B.cs_kv_append(c.plan, 0, k, k, rotate=False)
+        B.cs_kv_set_seq(c.kv, 0, c.pages[0][:1], 10)
+        B.cs_kv_set_seq(c.kv, 1, [], 0)
+        got = c.read([0, 0, 0, 0, 1], [0, 15, 16, 47, 0])[0]
+        assert got[:2].all() and not got[2:].any()
+        with pytest.raises(B.ConfSpecError) as e:
+            B.cs_last_status(c.model)
+        assert e.value.status == B.CS_ERANGE
+        B.cs_kv_set_seq(c.kv, 1, c.pages[0][1:], 0)                      # its new owner reads them
+        assert c.read([1, 1], [0, 31])[0].all()
+        B.cs_last_status(c.model)

@@ -146,5 +146,5 @@ def test_rows_that_a_kernel_may_have_written_are_read_by_ordinary_loads():
     from paper_2602_18447_b200 import build
     text = open(os.path.join(build.CSRC, "kv_rows.cu")).read()
     code = re.sub(r"//.*", "", text)
-    assert all(re.match(r"(p\.)?(table|pages)\b|static_cast", arg) for arg in re.findall(r"__ldg\(([^,;]*)", code)), re.findall(r"__ldg\(([^,;]*)", code)
+    assert all(re.match(r"(p\.)?(table|pages|n_pages)\b|static_cast", arg) for arg in re.findall(r"__ldg\(([^,;]*)", code)), re.findall(r"__ldg\(([^,;]*)", code)
     assert not re.findall(r"const uint8_t\s*\*\s*__restrict__|const uint16_t\s*\*\s*__restrict__|const float2\s*\*\s*__restrict__", code)
