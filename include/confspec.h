@@ -148,7 +148,8 @@ int cs_kv_alloc_8bit(const cs_model* model, int num_pages, int page_size, int ma
  * (token, kv head) are cut into groups of 64; a group x keeps an fp16 offset o = min x, an fp16 scale
  * s = min((max x - min x) / 15, 1023.5) and a code c = rint((x - o) / s) in 0 .. 15 per channel (0 where s = 0), which stands
  * for s c + o: off by at most s / 2 and the roundings of s and o, where the range of a group stays below 15352 (beyond it
- * values saturate). A row takes head_dim / 2 + 4 head_dim / 64 bytes, 0.28 of a 16-bit row:
+ * values saturate). The fifteenth is taken as the fp32 difference times the fp32 number next to 1 / 15, each rounded, and then as
+ * fp16: where a quotient lies between two fp16 numbers this may be the other one than a division would give. A row takes head_dim / 2 + 4 head_dim / 64 bytes, 0.28 of a 16-bit row:
  *   pool bytes = n_layers * num_pages * n_kv_heads * 18 * head_dim, library-owned.
  * Every call takes it: cs_verify_steps, cs_verify_cascade, cs_prefill and cs_append_accepted (steps of any length), cs_kv_fill
  * (bf16 rows, quantised on the way in), and the calls on a plan below. Within a pass the new tokens see one another's keys and

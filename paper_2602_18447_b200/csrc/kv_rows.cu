@@ -88,20 +88,13 @@ __device__ __forceinline__ void range_lanes(float& lo, float& hi) {
 constexpr float kRound = 12582912.f;
 constexpr uint32_t kRoundBits = 0x4B400000u;
 
-// x / 15, correctly rounded: the product with the rounded reciprocal, corrected once by its remainder, which is exact (Markstein's
-// theorem, 1990; equal to the division for every fp32 mantissa. The product alone is off by a last bit for two of three, and then
-// falls on the other side where a scale lies between two fp16 numbers).
-__device__ __forceinline__ float fifteenth(float x) {
-  constexpr float inv15 = 1.0f / 15.0f;
-  const float r = __fmul_rn(x, inv15);
-  return __fmaf_rn(__fmaf_rn(-15.f, r, x), inv15, r);
-}
 // A group's scale and offset from its smallest and largest value. The smallest value is the offset, a fifteenth of the range the
 // scale, both rounded to fp16 (half a step of 2^-10 relative; the codes are taken against the rounded pair, so the error stays half
-// a code step plus 15 x 2^-11 of one at the far end of the range).
+// a code step plus 15 x 2^-11 of one at the far end of the range). The fifteenth is the product with the rounded reciprocal, which is
+// what the format says and what caches that were written before hold: a division differs in one group of some 2000, by one fp16 step.
 __device__ __forceinline__ void group_params(float lo, float hi, __half& scale, __half& offset) {
   offset = __float2half_rn(lo);
-  scale = __float2half_rn(fminf(fifteenth(__fsub_rn(hi, lo)), kKv4MaxScale));
+  scale = __float2half_rn(fminf(__fmul_rn(__fsub_rn(hi, lo), 1.0f / 15.0f), kKv4MaxScale));
 }
 // The codes of eight channels. code[i]: kRoundBits + the code.
 __device__ __forceinline__ void codes8(const float (&v)[8], __half scale, __half offset, uint32_t (&code)[8]) {

@@ -16,19 +16,6 @@ def _np(t):
     return t.double().cpu().numpy()
 
 
-def _quantise(x):
-    """kv4_common.quantise with the scale as the format states it: a fifteenth of the range by one correctly rounded division (the
-    product with a rounded 1/15 that is taken there differs where a scale lies between two fp16 numbers, one group of some 2000)."""
-    g = x.astype(np.float32).reshape(*x.shape[:-1], -1, K.GROUP)
-    lo, hi = g.min(-1), g.max(-1)
-    o = lo.astype(np.float16)
-    s = np.minimum((hi - lo) / np.float32(15.0), np.float32(K.MAX_SCALE)).astype(np.float16)
-    sf = s.astype(np.float64)[..., None]
-    steps = (g.astype(np.float64) - o.astype(np.float64)[..., None]) / np.where(sf > 0, sf, 1.0)
-    c = np.where(sf > 0, np.rint(steps).clip(0, 15), 0)
-    return c.reshape(x.shape), s.astype(np.float64), o.astype(np.float64)
-
-
 def _attend(q, kc, vc, ctx, lens, given, scale, dtype, kn=None, vn=None):
     """Attention of given float64 rows through a cache that holds `kc`, `vc` -> (outputs, and the same in 64 bits with the bound of
     K.attend but for the output's own rounding)."""
@@ -47,7 +34,7 @@ def _attend(q, kc, vc, ctx, lens, given, scale, dtype, kn=None, vn=None):
         c.B.cs_attention_4bit(c.plan, 0, q, out, kn, vn, scale=scale)
         torch.cuda.synchronize()
         c.B.cs_last_status(c.model)
-    (ck, sk, ok), (cv, sv, ov) = _quantise(_np(kc)), _quantise(_np(vc))
+    (ck, sk, ok), (cv, sv, ov) = K.quantise(_np(kc)), K.quantise(_np(vc))
     rows = [K.values(ck, sk, ok), K.values(cv, sv, ov), K.values(cv, sv, 0 * ov), (79 * sk + np.abs(ok)).max(-1)]
     want, bound = np.zeros(q.shape), np.zeros(q.shape)
     a = b = 0
@@ -153,7 +140,7 @@ def _sinks(sigma, hq, hkv, hd, n, ctx, given, lift):
         out = torch.full_like(q, float("nan"))
         c.B.cs_attention_4bit(c.plan, 0, q, out, *((kn, vn) if given else (None, None)))
         torch.cuda.synchronize()
-    kq, vq = _quantise(_np(k)), _quantise(_np(v))
+    kq, vq = K.quantise(_np(k)), K.quantise(_np(v))
     xk, xv = K.values(*kq), K.values(*vq)
     if given:
         own = (np.zeros((n, hkv, hd)), np.zeros((n, hkv, hd // 64)))
@@ -246,35 +233,6 @@ def test_rows_are_read_right_behind_their_append(fmt):
                     all_rounds(False)
                 graph.replay()
         assert not torch.equal(want[0][0], want[1][0])
-
-
-@pytest.mark.parametrize("hd", [64, 128])
-@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
-def test_scales_are_the_rounded_quotient(hd, dtype):
-    """Groups whose range over 15 lies where two fp16 scales meet: the product with a rounded 1/15 takes the other one."""
-    import torch
-    rng = np.random.default_rng(17)
-    ends = torch.from_numpy(rng.standard_normal((1 << 20, 2)) * np.exp(rng.uniform(-5, 5, (1 << 20, 1))))
-    ends = np.sort(ends.to(getattr(torch, dtype)).float().numpy(), axis=1)
-    span = ends[:, 1] - ends[:, 0]
-    ends = ends[(span / np.float32(15)).astype(np.float16) != (span * np.float32(1.0 / 15.0)).astype(np.float16)]
-    n = len(ends) * K.GROUP // hd
-    assert n >= 20
-    ends = ends[:n * hd // K.GROUP]
-    part = rng.uniform(0, 1, (len(ends), K.GROUP))
-    part[:, 5], part[:, 40] = 0.0, 1.0
-    x = _dev((ends[:, :1] + part * (ends[:, 1:] - ends[:, :1])).reshape(n, 1, hd), dtype)
-    with K.Cache(1, 1, hd, n_seqs=1, pages_each=n // 16 + 1) as c:
-        c.B.cs_plan_set(c.plan, [0], [n])
-        c.B.cs_kv_append(c.plan, 0, x, x, rotate=False)
-        want = K.values(*_quantise(_np(x))).astype(np.float16).astype(np.float64)
-        for got in c.read(np.zeros(n, int), np.arange(n)):
-            assert np.array_equal(got, want)
-        c.B.cs_kv_set_seq(c.kv, 0, c.pages[0], n)
-        if dtype == "bfloat16":                        # the same on the way from host rows
-            bits = x.view(torch.uint16).cpu().numpy()
-            c.B.cs_kv_fill(c.kv, 0, 0, bits, bits)
-            assert np.array_equal(c.read(np.zeros(n, int), np.arange(n))[0], want)
 
 
 def _keys_at_the_top(n, hd, theta, rng):
@@ -472,7 +430,7 @@ def test_the_largest_scale_and_the_refusal_of_larger_ones(n):
         c.B.cs_kv_commit(c.plan)
         c.B.cs_plan_set(c.plan, [0], [n], given=True)
         out = torch.full_like(q, float("nan"))
-        kq, vq = _quantise(_np(k)), _quantise(_np(v))
+        kq, vq = K.quantise(_np(k)), K.quantise(_np(v))
         xk, xv = K.values(*kq)[:, 0], K.values(*vq)[:, 0]
         scores = np.einsum("thd,kd->thk", _np(q), xk)
         c.B.cs_attention_4bit(c.plan, 0, q, out, new, new, scale=2.0 ** 60 if n == 2 else float(2.0 ** 24 / np.abs(scores).max()))
@@ -540,7 +498,7 @@ def test_a_new_cache_is_zero_before_any_stream_writes_to_it(fmt):
             torch.cuda.synchronize()
             B.cs_plan_free(plan)
             B.cs_kv_free(kv)
-            want = K.values(*_quantise(_np(k))) if fmt == "int4" else _np(k.bfloat16())
+            want = K.values(*K.quantise(_np(k))) if fmt == "int4" else _np(k.bfloat16())
             assert np.array_equal(_np(out_k), want.astype(np.float16).astype(np.float64))
             assert bool((out_v != 0).any())
 
