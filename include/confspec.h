@@ -110,7 +110,9 @@ int cs_model_set_lm_head_rows(cs_model* model, const int32_t* row_ids, int n_row
 /*
  * cs_reserve — size the per-model activation workspace for batches of up to max_steps steps and
  * max_tokens new tokens in total. Optional: cs_verify_steps / cs_prefill grow the workspace on demand, but
- * growing synchronises the device, so latency-sensitive callers reserve once up front.
+ * growing synchronises the device, so latency-sensitive callers reserve once up front. What depends on the contexts is not
+ * part of it and grows on demand: the work lists, and over a 4-bit cache the expanded contexts of a batch with long steps
+ * (see cs_kv_alloc_4bit).
  */
 int cs_reserve(cs_model* model, int max_steps, int max_tokens);
 

@@ -14,17 +14,18 @@
 //
 // Bound. Reading the cache: HD / 2 + 4 HD / 64 bytes per row of K or V. Every warp streams whole (page, kv head) blocks with
 // asynchronous copies, two pages at a time and two such rounds ahead; nothing waits on another CTA but the CTAs of a cluster at
-// their end. At the copy bandwidth an SM has ~100 cycles per block, some 400 issue slots over its four schedulers, against 224
-// instructions per block at 8 query rows (293 at 16), HD = 128: what follows counts instructions. Codes become fp16 operands without
+// their end. At the copy bandwidth an SM has ~100 cycles per block, some 400 issue slots over its four schedulers, against 251
+// instructions per block at 8 query rows (334 at 16), HD = 128: what follows counts instructions. Codes become fp16 operands without
 // a conversion instruction: a nibble in the mantissa of a power of two, 64 + c or 1024 + c. The 64 of half of a key's channels is
 // taken back by the product that adds the offsets,
 //     q . k = sum_groups s (sum_d q_d h_d) + o (sum_d q_d) - 64 s (sum over those channels of q_d),
 // whose operands are the offsets and scales as they are stored; one packed addition makes c (keys) or c - 8 (values) of the
 // others. The product that sums the values' offsets has rows of ones besides, which sum the probabilities.
-// Measured on 64 contexts of 2 K to 8 K keys x 8 heads of 128 (0.37 GB): one token each (2 query rows per kv head) 66.4 us, 5.6 TB/s,
-// 0.85 of the copy bandwidth; 5 to 8 tokens (16 rows) 104 us, 0.55, where the accumulators leave 12 warps on an SM and the products'
-// latencies show (tensor pipe 43 % busy, 1.85 instructions a cycle). Two warps that share pages and split the channels (16 warps)
-// were slower, 126 us: 395 instructions a block with the exchange of the probabilities.
+// Measured on 64 contexts of 2 K to 8 K keys x 8 heads of 128 (0.37 GB): one token each (2 query rows per kv head) 68.6 us, 5.4 TB/s,
+// 0.83 of the copy bandwidth; 5 to 8 tokens (16 rows) 109 us, 0.53, where the accumulators leave 12 warps on an SM and the products'
+// latencies show (tensor pipe 40 % busy, 1.87 instructions a cycle); 17 to 96 rows some 90 us for every 16 rows begun, which read and
+// unpack the pages anew. Two warps that share pages and split the channels (16 warps) were slower, 126 us where this form took 109:
+// a third more instructions a block with the exchange of the probabilities.
 //
 // Pieces of a context are joined in their order. Where a few per context fill the machine, they are the CTAs of one cluster, which
 // read one another's (max, sum, O) through shared memory: one launch. Else a piece leaves them in global memory and a second kernel,
