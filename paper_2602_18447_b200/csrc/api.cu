@@ -197,10 +197,13 @@ struct cs_plan {
 namespace {
 
 // The page table on the device, as far as work that is issued to `s` from now on is concerned: uploaded there if it has changed, and
-// behind an upload that another stream may still be at. Not inside a stream capture.
+// behind an upload that another stream may still be at. A capture takes no part in the latter: whoever replays orders the replay.
 int upload_table(cs_kv* kv, cudaStream_t s) {
   if (!kv->dirty) {
     if (!kv->upload_unseen) return CS_OK;
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    CS_CUDA(cudaStreamIsCapturing(s, &st));
+    if (st != cudaStreamCaptureStatusNone) return CS_OK;
     const cudaError_t done = cudaEventQuery(kv->upload_ev);
     if (done == cudaSuccess) {
       kv->upload_unseen = false;
@@ -1329,13 +1332,13 @@ int cs_kv_fill(cs_kv* kv, int seq, int layer, const uint16_t* host_k, const uint
   return guarded([&] { return kv_fill(kv, seq, layer, host_k, host_v, stream); });
 }
 
-// Nothing may be uploaded from inside a stream capture: the page table has to be on the device already (a replay is ordered behind
-// an upload that is still on its way by whoever replays).
+// Nothing may be uploaded from inside a stream capture: the page table has to be on the device already.
 static int table_ready(cs_kv* kv, cudaStream_t s) {
-  if (!kv->dirty && !kv->upload_unseen) return CS_OK;
-  cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
-  CS_CUDA(cudaStreamIsCapturing(s, &st));
-  if (st != cudaStreamCaptureStatusNone) return kv->dirty ? CS_ESTATE : CS_OK;
+  if (kv->dirty) {
+    cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+    CS_CUDA(cudaStreamIsCapturing(s, &st));
+    if (st != cudaStreamCaptureStatusNone) return CS_ESTATE;
+  }
   return upload_table(kv, s);
 }
 

@@ -523,3 +523,67 @@ def test_reading_ends_with_a_sequences_own_pages(fmt):
         B.cs_kv_set_seq(c.kv, 1, c.pages[0][1:], 0)                      # its new owner reads them
         assert c.read([1, 1], [0, 31])[0].all()
         B.cs_last_status(c.model)
+
+
+def test_pages_far_into_a_large_pool():
+    """Attention in both forms over pages 19 GB into a pool gives the bits that it gives over the same rows in a small one."""
+    import torch
+    rng = np.random.default_rng(81)
+    hq, hkv, pages, ctx = 16, 8, 1 << 20, 75
+    k, v = _dev(rng.standard_normal((ctx, hkv, 128)), "float16"), _dev(rng.standard_normal((ctx, hkv, 128)), "float16")
+    with K.Cache(hq, hkv, 128, n_seqs=1) as c:
+        B = c.B
+        far = B.cs_kv_alloc_4bit(c.model, pages, 16, 1, 8)
+        plan = B.cs_plan_create(far)
+        B.cs_kv_set_seq(far, 0, pages - 1 - np.arange(8), 0)
+        for p in (c.plan, plan):
+            B.cs_plan_set(p, [0], [ctx])
+            B.cs_kv_append(p, 0, k, v)
+            B.cs_kv_commit(p)
+        for n in (1, 5, 50):                                             # 2, 10 and 100 query rows
+            q = _dev(rng.standard_normal((n, hq, 128)), "float16")
+            new = _dev(rng.standard_normal((n, hkv, 128)), "float16")
+            outs = []
+            for p in (c.plan, plan):
+                B.cs_plan_set(p, [0], [n], given=True)
+                outs.append(torch.full_like(q, float("nan")))
+                B.cs_attention_4bit(p, 0, q, outs[-1], new, new)
+            torch.cuda.synchronize()
+            assert bool(torch.isfinite(outs[0]).all()) and torch.equal(*outs)
+        B.cs_plan_free(plan)
+        B.cs_kv_free(far)
+
+
+def test_a_capture_while_the_page_table_is_on_its_way():
+    """A capture records nothing of the wait for an upload that another stream is still at, and is not spoiled by it."""
+    import torch
+    rng = np.random.default_rng(91)
+    k = _dev(rng.standard_normal((20, 2, 128)), "float16")
+    with K.Cache(4, 2, 128, n_seqs=2) as c:
+        B = c.B
+        other = B.cs_plan_create(c.kv, 8)
+        B.cs_plan_set(c.plan, [0], [20])
+        B.cs_kv_append(c.plan, 0, k, -k, rotate=False)
+        B.cs_kv_commit(c.plan)
+        place = (torch.zeros(20, dtype=torch.int32, device="cuda"), torch.arange(20, dtype=torch.int32, device="cuda"))
+        want, unused = torch.empty_like(k), torch.empty_like(k)
+        B.cs_kv_read(c.kv, 0, *place, want, unused)
+        got, q = torch.zeros_like(k), torch.ones(1, 4, 128, dtype=torch.float16, device="cuda")
+        out, again = torch.zeros_like(q), torch.zeros_like(q)
+        B.cs_plan_set(c.plan, [0], [1], given=True)
+        B.cs_attention_4bit(c.plan, 0, q, out, k[:1], k[:1])
+        torch.cuda.synchronize()
+        B.cs_kv_set_seq(c.kv, 1, c.pages[1], 0)
+        one = torch.cuda.Stream()
+        with torch.cuda.stream(one):
+            torch.cuda._sleep(50_000_000)
+            B.cs_plan_set(other, [1], [3])                               # uploads the table
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            B.cs_kv_read(c.kv, 0, *place, got, unused)
+            B.cs_attention_4bit(c.plan, 0, q, again, k[:1], k[:1])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(out, again) and bool(want.any()) and bool(out.any())
+        B.cs_plan_free(other)
