@@ -500,6 +500,17 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nt][mt][e] *= f;
   };
+  // Slots of a warp's pages behind the last key that any row of the tile sees hold what the pages' last user left: their value
+  // scales become zero, so that they have no say in k. (Their probabilities are zero.)
+  const int last_seen = see_base + see_step * ((row0 + R - 1) / G);
+  auto hide = [&](uint8_t* b, int pg) {
+    if (pg * kPage + (lane & 15) + half * kPage > last_seen) {
+      __half* at = reinterpret_cast<__half*>(b + half * L::kBlock + L::v_scale(lane & 15, 0));
+      at[0] = __half(0.f);
+      if (NG == 2) at[4] = __half(0.f);
+    }
+    __syncwarp();
+  };
   auto fit_scales = [&](auto np, const uint8_t* b) {
     uint32_t top = v_most;
 #pragma unroll
@@ -627,7 +638,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
     fetch(pg + (kStages - 1) * kStep, id_ahead, ahead_off);
     cp_async_commit();
     id_ahead = page_id(pg + kStages * kStep);
-    const uint8_t* b = my + stage_off;
+    uint8_t* b = my + stage_off;
     if (pg + 1 < end_cached) {
       float s[2][NT][4];
       uint32_t pb[2][NT][2];
@@ -636,6 +647,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       if (pg * kPage + 2 * kPage - 1 > all_see) {
         mask(s[0], pg * kPage, see_base, see_step);
         mask(s[1], pg * kPage + kPage, see_base, see_step);
+        hide(b, pg);
       }
       softmax(std::integral_constant<int, 2>{}, s, pb);
       fit_scales(std::integral_constant<int, 2>{}, b);
@@ -646,6 +658,7 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
       uint32_t pb[1][NT][2];
       cached_scores(b, s[0]);
       mask(s[0], pg * kPage, see_base, see_step);
+      hide(b, pg);
       softmax(std::integral_constant<int, 1>{}, s, pb);
       fit_scales(std::integral_constant<int, 1>{}, b);
       cached_values(b, pb[0]);

@@ -587,3 +587,35 @@ def test_a_capture_while_the_page_table_is_on_its_way():
         torch.cuda.synchronize()
         assert torch.equal(got, want) and torch.equal(out, again) and bool(want.any()) and bool(out.any())
         B.cs_plan_free(other)
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("hd,n", [(128, 1), (128, 5), (64, 1), (64, 5)])
+def test_small_values_do_not_meet_what_lies_behind_a_sequence(hd, n, given):
+    """The last page's other slots held rows of the largest scale: the outputs are the bits over clean pages, for values of size 1e-6
+    as for others, beside a key that draws 2^11 times the weight."""
+    import torch
+    outs = []
+    for dirty in (False, True):
+        rng = np.random.default_rng(101)
+        ctx = 37
+        k, v = np.zeros((ctx + n, 2, hd)), rng.standard_normal((ctx + n, 2, hd)) * 1e-6
+        k[32], v[32] = 11 * np.log(2.0) / np.sqrt(hd), 0.0
+        q, k, v = (_dev(x, "bfloat16") for x in (np.ones((n, 6, hd)), k, v))
+        with K.Cache(6, 2, hd, n_seqs=1) as c:
+            if dirty:
+                bad = _dev(np.where(np.arange(64)[:, None, None] % 2, 1, -1) * rng.uniform(2e4, 6e4, (64, 2, hd)) * np.where(
+                    np.arange(hd) % 2, 1, -1), "bfloat16")
+                c.B.cs_plan_set(c.plan, [0], [64])
+                c.B.cs_kv_append(c.plan, 0, bad, bad, rotate=False)
+            m = ctx if given else ctx + n
+            c.B.cs_plan_set(c.plan, [0], [m])
+            c.B.cs_kv_append(c.plan, 0, k[:m], v[:m], rotate=False)
+            c.set([ctx])
+            c.B.cs_plan_set(c.plan, [0], [n], given=given)
+            out = torch.full_like(q, float("nan"))
+            c.B.cs_attention_4bit(c.plan, 0, q, out, *((k[ctx:], v[ctx:]) if given else (None, None)))
+            torch.cuda.synchronize()
+            outs.append(out)
+    assert bool(torch.isfinite(outs[0]).all()) and bool(outs[0].any())
+    assert torch.equal(*outs)
