@@ -292,7 +292,7 @@ constexpr double kAttn4Join = 8;
 constexpr double kAttn4ClusterJoin = 5;
 // Steps of up to this many query rows per kv head (new tokens x heads in the group) read the 4-bit pages themselves, once per 16
 // rows; a batch with a longer one has its contexts expanded to fp16 for the tensor-core kernel. Measured, 64 contexts of 2 K to
-// 8 K keys x 8 heads: 64 rows 381 us against 540, 96 rows 551 against 549, 128 rows 731 against 540; 8 contexts of 1 K to 4 K keys
+// 8 K keys x 8 heads: 64 rows 387 us against 540, 96 rows 560 against 549, 128 rows 731 against 540; 8 contexts of 1 K to 4 K keys
 // x 4 heads: 84 rows 28 against 39, up to 672 rows 105 against 65. Batches of unequal steps were not measured: the longest decides.
 constexpr int kAttn4MaxRows = 96;
 

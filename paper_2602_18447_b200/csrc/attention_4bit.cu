@@ -14,15 +14,15 @@
 //
 // Bound. Reading the cache: HD / 2 + 4 HD / 64 bytes per row of K or V. Every warp streams whole (page, kv head) blocks with
 // asynchronous copies, two pages at a time and two such rounds ahead; nothing waits on another CTA but the CTAs of a cluster at
-// their end. At the copy bandwidth an SM has ~100 cycles per block, some 400 issue slots over its four schedulers, against 251
-// instructions per block at 8 query rows (334 at 16), HD = 128: what follows counts instructions. Codes become fp16 operands without
+// their end. At the copy bandwidth an SM has ~100 cycles per block, some 400 issue slots over its four schedulers, against 255
+// instructions per block at 8 query rows (336 at 16), HD = 128: what follows counts instructions. Codes become fp16 operands without
 // a conversion instruction: a nibble in the mantissa of a power of two, 64 + c or 1024 + c. The 64 of half of a key's channels is
 // taken back by the product that adds the offsets,
 //     q . k = sum_groups s (sum_d q_d h_d) + o (sum_d q_d) - 64 s (sum over those channels of q_d),
 // whose operands are the offsets and scales as they are stored; one packed addition makes c (keys) or c - 8 (values) of the
 // others. The product that sums the values' offsets has rows of ones besides, which sum the probabilities.
-// Measured on 64 contexts of 2 K to 8 K keys x 8 heads of 128 (0.37 GB): one token each (2 query rows per kv head) 68.6 us, 5.4 TB/s,
-// 0.83 of the copy bandwidth; 5 to 8 tokens (16 rows) 109 us, 0.53, where the accumulators leave 12 warps on an SM and the products'
+// Measured on 64 contexts of 2 K to 8 K keys x 8 heads of 128 (0.37 GB): one token each (2 query rows per kv head) 69.2 us, 5.4 TB/s,
+// 0.82 of the copy bandwidth; 5 to 8 tokens (16 rows) 110 us, 0.52, where the accumulators leave 12 warps on an SM and the products'
 // latencies show (tensor pipe 40 % busy, 1.87 instructions a cycle); 17 to 96 rows some 90 us for every 16 rows begun, which read and
 // unpack the pages anew. Two warps that share pages and split the channels (16 warps) were slower, 126 us where this form took 109:
 // a third more instructions a block with the exchange of the probabilities.
@@ -485,8 +485,8 @@ attention_4bit_kernel(const Attn4Params p, const AttnItem* __restrict__ items) {
   };
 
   // Value scales enter the products times 2^k, which the accumulators hold until the end: p s 2^k stays in fp16's normal range for
-  // small values too. k is as large as the largest scale so far allows. (Costs 2 % at 8 query rows, 3 % at 16; a look at a share
-  // of the scales by each lane instead of all of them was no faster.)
+  // small values too. k is as large as the largest scale so far allows. (Costs 2 % at 8 query rows, 3 % at 16, and 1 % more for the
+  // slots hidden below; a look at a share of the scales by each lane instead of all of them was no faster.)
   uint32_t v_up = k2Max, v_most = kMostAt2Max;             // 2^k; kKv4MaxScale 2^-k
   auto value_scales = [&](const uint8_t* b, uint32_t (&vs)[2 * NG]) {      // of keys 2 q, 2 q + 1 and 2 q + 8, 2 q + 9, by group
     if (NG == 2) *reinterpret_cast<uint4*>(vs) = *reinterpret_cast<const uint4*>(b + L::kVParams + q * 32 + 16);
