@@ -151,7 +151,8 @@ int cs_kv_alloc_8bit(const cs_model* model, int num_pages, int page_size, int ma
  * s = min((max x - min x) / 15, 1023.5) and a code c = rint((x - o) / s) in 0 .. 15 per channel (0 where s = 0), which stands
  * for s c + o: off by at most s / 2 and the roundings of s and o, where the range of a group stays below 15352 (beyond it
  * values saturate). The fifteenth is taken as the fp32 difference times the fp32 number next to 1 / 15, each rounded, and then as
- * fp16: where a quotient lies between two fp16 numbers this may be the other one than a division would give. A row takes head_dim / 2 + 4 head_dim / 64 bytes, 0.28 of a 16-bit row:
+ * fp16: where a quotient lies between two fp16 numbers this may be the other one than a division would give. A row takes
+ * head_dim / 2 + 4 head_dim / 64 bytes, 0.28 of a 16-bit row:
  *   pool bytes = n_layers * num_pages * n_kv_heads * 18 * head_dim, library-owned.
  * Every call takes it: cs_verify_steps, cs_verify_cascade, cs_prefill and cs_append_accepted (steps of any length), cs_kv_fill
  * (bf16 rows, quantised on the way in), and the calls on a plan below. Within a pass the new tokens see one another's keys and
@@ -248,10 +249,10 @@ int cs_kv_append(cs_plan* plan, int layer, const uint16_t* k, int64_t k_stride, 
  *   out                device rows [T, n_q_heads, head_dim]; may be q itself, with the same stride (CS_EINVAL otherwise).
  *   scale              0: 1 / sqrt(head_dim); else > 0 and at most 2^60. Steps of more than 96 query rows per kv head: scores
  *                      (scale q . k) beyond 2^25 in magnitude may come out as NaN.
- * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; a row with a
- * larger query comes out as NaN), sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number of new tokens:
- * up to 96 query rows per kv head read the 4-bit pages directly; a batch with a longer step has its rows and contexts put together
- * as fp16 in the plan (values rounded to fp16 once) for the pass's tensor-core attention. Deterministic.
+ * Products take fp16 operands (bf16 rows are re-encoded, exact for magnitudes in [2^-14, 65504]; a row with a larger query comes
+ * out as NaN), sums and the softmax are fp32; probabilities, and their products with the scales, are rounded to fp16. Any number
+ * of new tokens: up to 96 query rows per kv head read the 4-bit pages directly; a batch with a longer step has its rows and
+ * contexts put together as fp16 in the plan (values rounded to fp16 once) for the pass's tensor-core attention. Deterministic.
  */
 int cs_attention_4bit(cs_plan* plan, int layer, const uint16_t* q, int64_t q_stride, const uint16_t* k_new,
                       const uint16_t* v_new, int64_t kv_stride, uint16_t* out, int64_t out_stride, int dtype, float scale,
