@@ -511,6 +511,50 @@ int cs_lm_head_gate_static(const uint16_t* w_lm, const uint16_t* h, int B, int d
                            int32_t* out_verdict, float* out_lse, void* stream);
 /* out fp16 [rows, d] = RMSNorm(x fp32 [rows, d]; gain fp32 [d], eps). */
 int cs_rmsnorm(const float* x, const float* gain, uint16_t* out, int rows, int d, float eps, void* stream);
+
+/*
+ * Projections in 8-bit integers: for a program that runs its own layers with half the weights' bytes and the integer rate of the
+ * tensor cores. A matrix is held as one signed 8-bit code per value and one fp32 scale per row (output channel of a weight,
+ * token of an activation); a code stands for code * scale.
+ *
+ * cs_quantize_i8 - rows to codes. With A = max |x_i| of a row: scale = A / 127 (fp32), code_i = rint(127 x_i / A), ties to even, of
+ * the quotient as a real number: -127 .. 127, off by at most half a scale. A row of zeros has the scale 0. A row that holds a NaN
+ * or an infinity gets codes of 0 and the scale NaN, and so do the values and products made of it.
+ *   x                  device rows of d values, CS_F16, CS_BF16 or CS_F32 (dtype), x_stride elements apart.
+ *   codes, scales      device int8 [rows, d], contiguous, and float [rows].
+ * cs_dequantize_i8 - codes back to values, fp32(scale * code) rounded once to dtype, rows out_stride elements apart.
+ * cs_rmsnorm_i8 - the RMS norm of cs_rmsnorm with the residual's addition in front and codes as its result:
+ *     x' = x + delta (rounded to the type of x, stored in x_out),  y = x' g / sqrt(mean x'^2 + eps),  codes and scale of y.
+ *   The codes are those of fp32(x' g), exactly (the root is common to the row); the scale carries the root. Sums in fp32.
+ *   x, x_out           device rows of dtype; x_out may be x. delta, x_out: both NULL to norm x as it is.
+ *   delta              device rows of delta_dtype: any type for x in CS_F32, else the type of x.
+ *   gain               device float [d]; eps >= 0. A row with a NaN or infinity in x' or x' g, or whose squares overflow fp32, is
+ *                      left as cs_quantize_i8 leaves one.
+ * For these three, d is a multiple of 16, rows and gains are 16-byte aligned and strides whole 16-byte pieces; rows may be 0.
+ *
+ * cs_gemm_i8 - with acc[t, n] = sum_k a[t, k] w[n, k] in 32-bit integers (exact) and y = a_scales[t] w_scales[n] acc:
+ *     out = y                          w2, add NULL; dtype CS_F16, CS_BF16 or CS_F32
+ *     out = add + y                    add fp32 rows [M, N]; dtype CS_F32; out may be add, with the same stride
+ *     out = silu(y) * y2               w2, w2_scales a second matrix (the gate is w); CS_F16 or CS_BF16
+ *   The scales are applied in fp32, the result rounded once; beyond the type's range it is an infinity.
+ *   a                  device codes, M rows of K, a_stride bytes apart (a multiple of 16).
+ *   w, w2              device codes [N, K], contiguous. All codes 16-byte aligned, K a multiple of 16 and at most 131056.
+ *   out, add           strides in elements, any that hold a row; aligned to their type.
+ *   Any M from 0 and N from 1. Deterministic. No workspace: calls on several streams, and graphs that hold them, may overlap.
+ * All are asynchronous on `stream` and may be captured. Pointers belong to the current device.
+ * cs_i8_status       synchronises `stream`: CS_ETIMEOUT if a cs_gemm_i8 of the current device has given up on a bounded wait since
+ *                    the last query (its output is not to be used), else CS_OK.
+ */
+#define CS_F32 2
+int cs_quantize_i8(const void* x, int64_t x_stride, int dtype, int8_t* codes, float* scales, int rows, int d, void* stream);
+int cs_dequantize_i8(const int8_t* codes, const float* scales, int rows, int d, void* out, int64_t out_stride, int dtype,
+                     void* stream);
+int cs_rmsnorm_i8(const void* x, int64_t x_stride, int dtype, const void* delta, int64_t delta_stride, int delta_dtype, void* x_out,
+                  int64_t x_out_stride, const float* gain, int8_t* codes, float* scales, int rows, int d, float eps, void* stream);
+int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w, const float* w_scales, const int8_t* w2,
+               const float* w2_scales, const float* add, int64_t add_stride, void* out, int64_t out_stride, int M, int N, int K,
+               int dtype, void* stream);
+int cs_i8_status(void* stream);
 /*
  * Per-kernel-class timing of the pass. cs_profile(model, 1) makes cs_verify_steps / cs_prefill record a pair
  * of CUDA events around each kernel launch (on the call's stream); cs_profile_read waits for the recorded

@@ -19,7 +19,8 @@ EXPORTED = [
     "cs_kv_alloc", "cs_kv_alloc_8bit", "cs_kv_alloc_4bit", "cs_plan_create", "cs_plan_set", "cs_plan_free", "cs_kv_commit",
     "cs_kv_append", "cs_attention_4bit", "cs_kv_read", "cs_kv_free", "cs_kv_pool_bytes", "cs_kv_set_seq", "cs_kv_fill", "cs_prefill",
     "cs_verify_steps", "cs_verify_cascade", "cs_append_accepted", "cs_escalate_mask", "cs_cascade_select", "cs_set_keep_logits", "cs_set_deterministic", "cs_get_last_logits", "cs_get_last_lse",
-    "cs_last_status", "cs_selftest_wait_timeout", "cs_debug_build", "cs_selftest_range_check", "cs_check_workspace", "cs_gemm_f16", "cs_rmsnorm", "cs_lm_head_gate", "cs_lm_head_gate_static", "cs_take_launch_count", "cs_last_h2d_bytes", "cs_profile", "cs_profile_read",
+    "cs_last_status", "cs_selftest_wait_timeout", "cs_debug_build", "cs_selftest_range_check", "cs_check_workspace", "cs_gemm_f16", "cs_rmsnorm", "cs_lm_head_gate", "cs_lm_head_gate_static",
+    "cs_quantize_i8", "cs_dequantize_i8", "cs_rmsnorm_i8", "cs_gemm_i8", "cs_i8_status", "cs_take_launch_count", "cs_last_h2d_bytes", "cs_profile", "cs_profile_read",
 ]
 
 PROF_CLASSES = ["embed", "rmsnorm", "gemm_qkv", "rope", "attention", "gemm_o", "gemm_gateup", "gemm_down",
@@ -103,6 +104,11 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "cs_rmsnorm": (C.c_int, [vp, vp, vp, i32, i32, f32, vp]),
         "cs_lm_head_gate": (C.c_int, [vp, vp, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp, vp]),
         "cs_lm_head_gate_static": (C.c_int, [vp, vp, i32, i32, i32, vp, i32, f32, vp, vp, vp, vp, vp]),
+        "cs_quantize_i8": (C.c_int, [vp, i64, i32, vp, vp, i32, i32, vp]),
+        "cs_dequantize_i8": (C.c_int, [vp, vp, i32, i32, vp, i64, i32, vp]),
+        "cs_rmsnorm_i8": (C.c_int, [vp, i64, i32, vp, i64, i32, vp, i64, vp, vp, vp, i32, i32, f32, vp]),
+        "cs_gemm_i8": (C.c_int, [vp, i64, vp, vp, vp, vp, vp, vp, i64, vp, i64, i32, i32, i32, i32, vp]),
+        "cs_i8_status": (C.c_int, [vp]),
         "cs_take_launch_count": (C.c_int64, []),
         "cs_last_h2d_bytes": (C.c_int64, [vp]),
         "cs_profile": (C.c_int, [vp, i32]),
@@ -547,6 +553,126 @@ def cs_lm_head_gate_static(w_lm, h, verdict_ids: Sequence[int], tau: float, out_
 def cs_rmsnorm(x, gain, out, rows: int, d: int, eps: float, stream=None) -> None:
     _check(load_library().cs_rmsnorm(_dev_ptr(x), _dev_ptr(gain), _dev_ptr(out), rows, d, float(eps),
                                      _stream_ptr(stream)), "cs_rmsnorm")
+
+
+CS_F32 = 2
+
+_i8_types: dict = {}
+
+
+def _matrix(t, name, kinds, shape, contiguous=False):
+    """(device address, elements between rows, type code) of a CUDA matrix of one of the types `kinds`, on the current device,
+    whose rows are contiguous. `shape`: what it has to have."""
+    torch = _torch or _t()
+    if not _i8_types:
+        _i8_types.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16, torch.float32: CS_F32, torch.int8: -1})
+    code = _i8_types.get(t.dtype)
+    if code is None or code not in kinds:
+        raise ValueError(f"{name}: type {t.dtype}")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} has to be on the current device")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple(shape)} is expected")
+    if contiguous or len(shape) == 1:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} has to be contiguous")
+        return t.data_ptr(), shape[-1], code
+    rows, cols = shape
+    if not rows:
+        return None, cols, code
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row have to be contiguous")
+    if rows == 1:
+        return t.data_ptr(), -1, code        # the stride of one row says nothing
+    if t.stride(0) < cols:
+        raise ValueError(f"{name}: its rows overlap")
+    return t.data_ptr(), t.stride(0), code
+
+
+_ROWS = (CS_F16, CS_BF16, CS_F32)
+
+
+def _one_row(stride: int, cols: int, step: int) -> int:
+    """A stride that a single row of `cols` values may have."""
+    return (cols + step - 1) // step * step if stride < 0 else stride
+
+
+def _rows_2d(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} is a matrix of rows")
+    return t.shape
+
+
+def cs_quantize_i8(x, codes, scales, stream=None) -> None:
+    """x: CUDA rows [M, d] (float16, bfloat16 or float32; the rows may lie apart); codes: contiguous int8 [M, d]; scales:
+    float32 [M]."""
+    shape = _rows_2d(x, "x")
+    xp, xs, kind = _matrix(x, "x", _ROWS, shape)
+    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
+    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
+    _check(load_library().cs_quantize_i8(xp, _one_row(xs, shape[1], 8), kind, cp, sp, shape[0], shape[1], _stream_ptr(stream)),
+           "cs_quantize_i8")
+
+
+def cs_dequantize_i8(codes, scales, out, stream=None) -> None:
+    """codes: contiguous CUDA int8 [M, d]; scales: float32 [M]; out: rows [M, d] (float16, bfloat16 or float32)."""
+    shape = _rows_2d(codes, "codes")
+    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
+    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
+    op, os_, kind = _matrix(out, "out", _ROWS, shape)
+    _check(load_library().cs_dequantize_i8(cp, sp, shape[0], shape[1], op, _one_row(os_, shape[1], 8), kind, _stream_ptr(stream)),
+           "cs_dequantize_i8")
+
+
+def cs_rmsnorm_i8(x, gain, codes, scales, eps: float, delta=None, x_out=None, stream=None) -> None:
+    """x: CUDA rows [M, d] (float16, bfloat16 or float32); gain: float32 [d]; codes: contiguous int8 [M, d]; scales: float32 [M].
+    delta: rows added to x first (of the type of x, or of any of the three for float32 x), x_out: rows of the type of x that
+    receive the sum (x itself where it is not given)."""
+    shape = _rows_2d(x, "x")
+    xp, xs, kind = _matrix(x, "x", _ROWS, shape)
+    gp, _, _ = _matrix(gain, "gain", (CS_F32,), shape[1:])
+    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
+    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
+    dp, ds, dkind, op, os_ = None, 0, kind, None, 0
+    if delta is not None:
+        dp, ds, dkind = _matrix(delta, "delta", _ROWS if kind == CS_F32 else (kind,), shape)
+        op, os_, _ = _matrix(x if x_out is None else x_out, "x_out", (kind,), shape)
+    elif x_out is not None:
+        raise ValueError("x_out comes with delta")
+    step = 8
+    _check(load_library().cs_rmsnorm_i8(xp, _one_row(xs, shape[1], step), kind, dp, _one_row(ds, shape[1], step), dkind, op,
+                                        _one_row(os_, shape[1], step), gp, cp, sp, shape[0], shape[1], float(eps),
+                                        _stream_ptr(stream)), "cs_rmsnorm_i8")
+
+
+def cs_gemm_i8(a, a_scales, w, w_scales, out, w2=None, w2_scales=None, add=None, stream=None) -> None:
+    """a: CUDA int8 codes [M, K] (rows may lie apart by a multiple of 16); w, w2: contiguous int8 codes [N, K]; scales: float32 [M],
+    [N], [N]; out: rows [M, N]. out = y (any of the three row types), add + y (add, out: float32 rows; out may be add) or
+    silu(y) * y2 (float16 or bfloat16)."""
+    (m, k), n = _rows_2d(a, "a"), _rows_2d(w, "w")[0]
+    ap, as_, _ = _matrix(a, "a", (-1,), (m, k))
+    wp, _, _ = _matrix(w, "w", (-1,), (n, k), True)
+    asp, _, _ = _matrix(a_scales, "a_scales", (CS_F32,), (m,))
+    wsp, _, _ = _matrix(w_scales, "w_scales", (CS_F32,), (n,))
+    w2p = w2sp = dp = None
+    ds = 0
+    if w2 is not None:
+        w2p, _, _ = _matrix(w2, "w2", (-1,), (n, k), True)
+        w2sp, _, _ = _matrix(w2_scales, "w2_scales", (CS_F32,), (n,))
+        if add is not None:
+            raise ValueError("add goes with a single matrix")
+    elif w2_scales is not None:
+        raise ValueError("w2_scales come with w2")
+    if add is not None:
+        dp, ds, _ = _matrix(add, "add", (CS_F32,), (m, n))
+    kinds = (CS_F32,) if add is not None else _ROWS[:2] if w2 is not None else _ROWS
+    op, os_, kind = _matrix(out, "out", kinds, (m, n))
+    _check(load_library().cs_gemm_i8(ap, _one_row(as_, k, 16), asp, wp, wsp, w2p, w2sp, dp, _one_row(ds, n, 1), op,
+                                     _one_row(os_, n, 1), m, n, k, kind, _stream_ptr(stream)), "cs_gemm_i8")
+
+
+def cs_i8_status(stream=None) -> None:
+    _check(load_library().cs_i8_status(_stream_ptr(stream)), "cs_i8_status")
 
 
 def cs_profile(model: int, enable: bool) -> None:

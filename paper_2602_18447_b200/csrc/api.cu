@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "gemm.h"
+#include "i8.h"
 #include "kernels.h"
 #include "kv4.cuh"
 
@@ -2149,6 +2150,112 @@ int cs_lm_head_gate(const uint16_t* w_lm, const uint16_t* h, int B, int d_model,
                         out_verdict ? out_verdict + b0 : nullptr, out_lse ? out_lse + b0 : nullptr, s));
   }
   return CS_OK;
+}
+
+static int type_bytes(int dtype) { return dtype == CS_F32 ? 4 : dtype == CS_F16 || dtype == CS_BF16 ? 2 : 0; }
+// Rows of 16-byte pieces.
+static bool typed_rows_ok(const void* p, int64_t stride, int64_t row, int dtype) {
+  const int bytes = type_bytes(dtype);
+  return bytes && p && (reinterpret_cast<uintptr_t>(p) & 15) == 0 && stride >= row && stride * bytes % 16 == 0;
+}
+static bool codes_ok(const int8_t* codes, const float* scales, int rows, int d) {
+  return rows >= 0 && d >= 16 && d % 16 == 0 && codes && scales && (reinterpret_cast<uintptr_t>(codes) & 15) == 0 &&
+         (reinterpret_cast<uintptr_t>(scales) & 3) == 0;
+}
+
+int cs_quantize_i8(const void* x, int64_t x_stride, int dtype, int8_t* codes, float* scales, int rows, int d, void* stream) {
+  if (rows == 0 && d >= 16 && d % 16 == 0 && type_bytes(dtype)) return CS_OK;      // rows of none may have no address
+  if (!codes_ok(codes, scales, rows, d) || !typed_rows_ok(x, x_stride, d, dtype)) return CS_EINVAL;
+  QuantRows q = {};
+  q.x = x;
+  q.x_stride = x_stride;
+  q.type = dtype;
+  q.codes = codes;
+  q.scales = scales;
+  q.rows = rows;
+  q.d = d;
+  CS_CUDA(launch_quantize_i8(q, static_cast<cudaStream_t>(stream)));
+  return CS_OK;
+}
+
+int cs_dequantize_i8(const int8_t* codes, const float* scales, int rows, int d, void* out, int64_t out_stride, int dtype,
+                     void* stream) {
+  if (rows == 0 && d >= 16 && d % 16 == 0 && type_bytes(dtype)) return CS_OK;
+  if (!codes_ok(codes, scales, rows, d) || !typed_rows_ok(out, out_stride, d, dtype)) return CS_EINVAL;
+  CS_CUDA(launch_dequantize_i8(codes, scales, out, out_stride, rows, d, dtype, static_cast<cudaStream_t>(stream)));
+  return CS_OK;
+}
+
+int cs_rmsnorm_i8(const void* x, int64_t x_stride, int dtype, const void* delta, int64_t delta_stride, int delta_dtype, void* x_out,
+                  int64_t x_out_stride, const float* gain, int8_t* codes, float* scales, int rows, int d, float eps, void* stream) {
+  if (!(eps >= 0.f) || eps > 3.0e38f) return CS_EINVAL;
+  if (rows == 0 && d >= 16 && d % 16 == 0 && type_bytes(dtype)) return CS_OK;
+  if (!codes_ok(codes, scales, rows, d) || !typed_rows_ok(x, x_stride, d, dtype)) return CS_EINVAL;
+  if (!gain || (reinterpret_cast<uintptr_t>(gain) & 15) || (delta == nullptr) != (x_out == nullptr)) return CS_EINVAL;
+  if (delta) {
+    if (dtype != CS_F32 && delta_dtype != dtype) return CS_EINVAL;
+    if (!typed_rows_ok(delta, delta_stride, d, delta_dtype) || !typed_rows_ok(x_out, x_out_stride, d, dtype)) return CS_EINVAL;
+    // rows would be written over others' inputs
+    if (rows > 1 && ((x_out == x && x_out_stride != x_stride) ||
+                     (x_out == delta && (x_out_stride != delta_stride || delta_dtype != dtype))))
+      return CS_EINVAL;
+  }
+  QuantRows q = {};
+  q.x = x;
+  q.x_stride = x_stride;
+  q.type = dtype;
+  q.delta = delta;
+  q.delta_stride = delta_stride;
+  q.delta_type = delta_dtype;
+  q.x_out = x_out;
+  q.x_out_stride = x_out_stride;
+  q.gain = gain;
+  q.codes = codes;
+  q.scales = scales;
+  q.rows = rows;
+  q.d = d;
+  q.eps = eps;
+  CS_CUDA(launch_quantize_i8(q, static_cast<cudaStream_t>(stream)));
+  return CS_OK;
+}
+
+int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w, const float* w_scales, const int8_t* w2,
+               const float* w2_scales, const float* add, int64_t add_stride, void* out, int64_t out_stride, int M, int N, int K,
+               int dtype, void* stream) {
+  if (M < 0 || N < 1 || K < 16 || K % 16 || K > kMaxI8K || !type_bytes(dtype)) return CS_EINVAL;
+  if ((w2 == nullptr) != (w2_scales == nullptr) || (w2 && (add || dtype == CS_F32)) || (add && dtype != CS_F32)) return CS_EINVAL;
+  if (M == 0) return CS_OK;
+  const auto aligned = [](const void* p, uintptr_t to) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; };
+  if (!aligned(a, 16) || !aligned(w, 16) || (w2 && !aligned(w2, 16)) || a_stride < K || a_stride % 16) return CS_EINVAL;
+  if (!aligned(a_scales, 4) || !aligned(w_scales, 4) || (w2 && !aligned(w2_scales, 4))) return CS_EINVAL;
+  if (!aligned(out, type_bytes(dtype)) || out_stride < N) return CS_EINVAL;
+  if (add && (!aligned(add, 4) || add_stride < N || (add == out && add_stride != out_stride && M > 1))) return CS_EINVAL;
+  CUtensorMap ta, tw, tw2;
+  if (!make_i8_map(&ta, a, M, K, a_stride, gemm_i8_box(M, w2 != nullptr)) || !make_i8_map(&tw, w, N, K, K, 128) ||
+      (w2 && !make_i8_map(&tw2, w2, N, K, K, 128))) {
+    g_cuda_error = "cuTensorMapEncodeTiled failed";
+    return CS_ECUDA;
+  }
+  GemmI8 g = {};
+  g.a_scales = a_scales;
+  g.w_scales = w_scales;
+  g.w2_scales = w2_scales;
+  g.add = add;
+  g.add_stride = add_stride;
+  g.out = out;
+  g.out_stride = out_stride;
+  g.M = M;
+  g.N = N;
+  g.K = K;
+  g.type = dtype;
+  CS_CUDA(gemm_i8(ta, tw, w2 ? &tw2 : nullptr, g, static_cast<cudaStream_t>(stream)));
+  return CS_OK;
+}
+
+int cs_i8_status(void* stream) {
+  uint32_t bits = 0;
+  CS_CUDA(i8_status(&bits, static_cast<cudaStream_t>(stream)));
+  return (bits & 1u) ? CS_ETIMEOUT : CS_OK;
 }
 
 int cs_rmsnorm(const float* x, const float* gain, uint16_t* out, int rows, int d, float eps, void* stream) {

@@ -1,0 +1,333 @@
+// Products of 8-bit codes: out[t, n] = a_scale[t] w_scale[n] sum_k a[t, k] w[n, k], the sum in 32-bit integers on the tensor cores
+// (tcgen05, kind::i8) and exact, whatever its order.
+//
+// Narrow form: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few columns.
+// A CTA owns 128 output channels, up to 256 tokens and a piece of the k range; the pieces of a tile are the CTAs of a cluster, each
+// of which collects the others' sums for its share of the tokens through distributed shared memory. Nothing is kept between calls.
+#include "i8.h"
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "gemm.h"
+#include "kernels.h"
+
+namespace cs {
+
+namespace {
+
+constexpr int kBK = 128;                    // codes (= bytes) of a k block: one 128-byte swizzled row
+constexpr int kTileBytes = 128 * kBK;       // 128 rows of it
+constexpr int kThreads = 192;               // warp 0: copies, warp 1: products, warps 2-5: results
+constexpr int kMaxSplit = 8;
+
+// Time-outs of launches that are given no status word.
+static __device__ uint32_t g_status;
+
+// Instruction descriptor: signed 8-bit x signed 8-bit -> 32-bit integers, both operands K-major, tile M x N.
+__host__ __device__ constexpr uint32_t idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
+}
+// D (+)= A B^T over one k block: four steps of 32 codes, the descriptors advancing by 32 bytes.
+__device__ __forceinline__ void umma_i8_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred P;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+      "setp.ne.b32 P, %4, 0;\n\t"
+      "add.u64 a1, %1, 2;\n\tadd.u64 b1, %2, 2;\n\t"
+      "add.u64 a2, %1, 4;\n\tadd.u64 b2, %2, 4;\n\t"
+      "add.u64 a3, %1, 6;\n\tadd.u64 b3, %2, 6;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, P;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], a1, b1, %3, 1;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], a2, b2, %3, 1;\n\t"
+      "tcgen05.mma.cta_group::1.kind::i8 [%0], a3, b3, %3, 1;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld_16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void cluster_arrive_wait() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t cta) {
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+  return r;
+}
+__device__ __forceinline__ void st_peer_v2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
+
+// y / (1 + e^-y); the fast division leaves 0 for a divisor beyond 2^126, which is what the quotient tends to.
+__device__ __forceinline__ float silu(float y) { return __fdividef(y, 1.0f + __expf(-y)); }
+
+__device__ __forceinline__ void store_one(void* out, int64_t at, float v, int type) {
+  if (type == kF16) static_cast<__half*>(out)[at] = __float2half_rn(v);
+  else if (type == kBF16) static_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(v);
+  else static_cast<float*>(out)[at] = v;
+}
+
+template <int BN, bool GATED>
+struct Narrow {
+  static constexpr int kWTiles = GATED ? 2 : 1;
+  static constexpr int kStageBytes = kWTiles * kTileBytes + BN * kBK;
+  // Two CTAs to an SM where the columns are few, else one that takes it all.
+  static constexpr int kStages = (BN * kWTiles <= 64 ? 112 * 1024 : 216 * 1024) / kStageBytes;
+  static constexpr uint32_t kCols = kWTiles * BN < 32 ? 32 : kWTiles * BN;
+  static constexpr int kBarOff = kStages * kStageBytes;
+  static constexpr int kTotal = kBarOff + 256 + 1024;       // + slack for the tiles' alignment
+  // CTAs that share an SM must find their columns whenever they fit its shared memory: one that waited for columns while the rest of
+  // its cluster waited for it could wait for a CTA that waits likewise.
+  static_assert(kTotal * 512ll >= kCols * 227ll * 1024 || kTotal > 190 * 1024, "tensor memory before shared memory");
+  static_assert(kStages >= 3 && kTotal <= 227 * 1024, "stages");
+};
+
+template <int BN, bool GATED>
+__global__ void __launch_bounds__(kThreads)
+gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
+                      const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int n_tiles, int split) {
+  using L = Narrow<BN, GATED>;
+  constexpr uint32_t kIdesc = idesc_i8(128, BN);
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* full_bar = bars;
+  uint64_t* empty_bar = bars + L::kStages;
+  uint64_t* acc_bar = bars + 2 * L::kStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 1);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* status = p.status ? p.status : &g_status;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int piece = blockIdx.x % split, tile = blockIdx.x / split;
+  const int n0 = (tile % n_tiles) * 128, t0 = (tile / n_tiles) * BN;
+  const int kblocks = (p.K + kBK - 1) / kBK;
+  const int kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * piece / split);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (piece + 1) / split);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(&full_bar[s], 1);
+      mbar_init(&empty_bar[s], 1);
+    }
+    mbar_init(acc_bar, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tm_a);
+    tma_prefetch_desc(&tm_w);
+    if (GATED) tma_prefetch_desc(&tm_w2);
+  }
+  if (warp == 1) {
+    tmem_alloc(tmem_slot, L::kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_launch_dependents();
+  // Weights that nothing in front of this launch writes are sent for at once, the tokens' rows after the wait.
+  int ahead = 0;
+  if (threadIdx.x == 0 && p.weights_settled) {
+    for (; ahead < L::kStages && kb0 + ahead < kb1; ++ahead) {
+      uint8_t* sw = smem + ahead * L::kStageBytes;
+      mbar_arrive_expect_tx(&full_bar[ahead], L::kStageBytes);
+      tma_load_2d(sw, &tm_w, &full_bar[ahead], (kb0 + ahead) * kBK, n0);
+      if (GATED) tma_load_2d(sw + kTileBytes, &tm_w2, &full_bar[ahead], (kb0 + ahead) * kBK, n0);
+    }
+  }
+  pdl_wait();
+
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      for (int kb = kb0; kb < kb1; ++kb) {
+        uint8_t* sw = smem + stage * L::kStageBytes;
+        if (kb - kb0 >= ahead) {
+          if (!mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, status)) { ok = false; break; }
+          mbar_arrive_expect_tx(&full_bar[stage], L::kStageBytes);
+          tma_load_2d(sw, &tm_w, &full_bar[stage], kb * kBK, n0);
+          if (GATED) tma_load_2d(sw + kTileBytes, &tm_w2, &full_bar[stage], kb * kBK, n0);
+        }
+        tma_load_2d(sw + L::kWTiles * kTileBytes, &tm_a, &full_bar[stage], kb * kBK, t0);
+        if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+      }
+      // after a time-out: let the copies in flight land before the CTA goes away
+      if (!ok)
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      const uint64_t wdesc0 = umma_desc_k128(smem_u32(smem));
+      for (int kb = kb0; kb < kb1; ++kb) {
+        if (!mbar_wait(&full_bar[stage], phase, abort_flag, status)) { ok = false; break; }
+        tc_fence_after();
+        const uint64_t wd = wdesc0 + static_cast<uint64_t>(stage * (L::kStageBytes >> 4));
+        const uint64_t ad = wd + (L::kWTiles * kTileBytes >> 4);
+        umma_i8_block(tmem_base, wd, ad, kIdesc, kb != kb0);
+        if (GATED) umma_i8_block(tmem_base + BN, wd + (kTileBytes >> 4), ad, kIdesc, kb != kb0);
+        umma_commit(&empty_bar[stage]);
+        if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) umma_commit(acc_bar);
+    }
+  }
+  __syncwarp();
+
+  // ------------------------------------------------------------------ results: a thread per output channel
+  const int quad = warp & 3;      // the lanes of tensor memory that this warp may read
+  const bool results = warp >= 2;
+  const int row = quad * 32 + lane;
+  const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
+  const int own = BN / split;     // tokens that this CTA writes: own * piece ..
+  const int n = n0 + row;
+  const bool n_ok = n < p.N;
+  float ws = 0.f, ws2 = 0.f;
+  if (results && n_ok) {
+    ws = p.w_scales[n];
+    if (GATED) ws2 = p.w2_scales[n];
+  }
+  if (results) {
+    ok = mbar_wait(acc_bar, 0, abort_flag, status);
+    tc_fence_after();
+  }
+  if (split > 1) {
+    // Everybody's products are done with the stages: they become [piece][pair of tokens][weight matrix][128 channels][2].
+    cluster_arrive_wait();
+    if (results) {
+      const uint32_t mine = smem_u32(smem) + static_cast<uint32_t>(piece * own * L::kWTiles * 512);
+#pragma unroll 1
+      for (int c = 0; c < BN; c += 16) {
+#pragma unroll
+        for (int w = 0; w < L::kWTiles; ++w) {
+          uint32_t r[16];
+          tmem_ld_16(t_row + w * BN + c, r);
+          tmem_ld_wait();
+#pragma unroll
+          for (int j = 0; j < 16; j += 2) {
+            const int to = (c + j) / own;
+            const int pair = (c + j - to * own) >> 1;
+            if (to != piece)
+              st_peer_v2(peer_addr(mine + static_cast<uint32_t>(((pair * L::kWTiles + w) * 128 + row) * 8), to), r[j], r[j + 1]);
+          }
+        }
+      }
+    }
+    cluster_arrive_wait();
+  }
+  if (results && ok) {
+#pragma unroll 1
+    for (int c = own * piece & ~15; c < own * (piece + 1); c += 16) {
+      if (t0 + c >= p.M) break;
+      uint32_t r[16], r2[16];
+      tmem_ld_16(t_row + c, r);
+      if (GATED) tmem_ld_16(t_row + BN + c, r2);
+      tmem_ld_wait();
+#pragma unroll
+      for (int j = 0; j < 16; j += 2) {
+        const int col = c + j - own * piece;
+        if (col < 0 || col >= own) continue;
+        int s[2] = {static_cast<int>(r[j]), static_cast<int>(r[j + 1])};
+        int s2[2] = {0, 0};
+        if (GATED) { s2[0] = static_cast<int>(r2[j]); s2[1] = static_cast<int>(r2[j + 1]); }
+        for (int q = 0; q < split; ++q) {
+          if (q == piece) continue;
+          const int2* from = reinterpret_cast<const int2*>(smem) + (q * own / 2 + (col >> 1)) * L::kWTiles * 128 + row;
+          const int2 v = from[0];
+          s[0] += v.x;
+          s[1] += v.y;
+          if (GATED) {
+            const int2 v2 = from[128];
+            s2[0] += v2.x;
+            s2[1] += v2.y;
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int t = t0 + c + j + e;
+          if (t >= p.M || !n_ok) continue;
+          const float as = p.a_scales[t];
+          float v = static_cast<float>(s[e]) * as * ws;
+          if (GATED) v = silu(v) * (static_cast<float>(s2[e]) * as * ws2);
+          if (p.add) v += p.add[t * p.add_stride + n];
+          store_one(p.out, t * p.out_stride + n, v, p.type);
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, L::kCols);
+  }
+}
+
+template <int BN, bool GATED>
+cudaError_t launch_narrow(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
+  using L = Narrow<BN, GATED>;
+  static std::atomic<uint64_t> opted{0};
+  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_narrow_kernel<BN, GATED>, L::kTotal, opted); e != cudaSuccess) return e;
+  const int n_tiles = (p.N + 127) / 128, t_tiles = (p.M + BN - 1) / BN, kblocks = (p.K + kBK - 1) / kBK;
+  const int64_t tiles = static_cast<int64_t>(n_tiles) * t_tiles;
+  int split = 1;
+  // every piece has a k block, every CTA of the cluster a pair of tokens, and the sums fit where the stages were
+  while (split < kMaxSplit && tiles * split * 2 <= 2 * kNumSMs && kblocks >= 2 * split && BN / (2 * split) >= 2 &&
+         BN * L::kWTiles * 512 <= L::kBarOff)
+    split *= 2;
+  if (tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
+  const dim3 grid(static_cast<unsigned>(tiles * split));
+  const cudaError_t e = split > 1 ? launch_pdl_cluster(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kThreads), L::kTotal, s, split, ta,
+                                                       tw, tw2, p, n_tiles, split)
+                                  : launch_pdl(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kThreads), L::kTotal, s, ta, tw, tw2, p,
+                                               n_tiles, split);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <bool GATED>
+cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
+  switch (gemm_i8_box(p.M, GATED)) {
+    case 16: return launch_narrow<16, GATED>(ta, tw, tw2, p, s);
+    case 32: return launch_narrow<32, GATED>(ta, tw, tw2, p, s);
+    case 64: return launch_narrow<64, GATED>(ta, tw, tw2, p, s);
+    case 128: return launch_narrow<128, GATED>(ta, tw, tw2, p, s);
+    default: return launch_narrow<256, GATED>(ta, tw, tw2, p, s);
+  }
+}
+
+}  // namespace
+
+int gemm_i8_box(int M, bool) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256; }
+
+bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows) {
+  return make_tensor_map_8b(tm, base, static_cast<uint64_t>(rows), static_cast<uint64_t>(k), static_cast<uint64_t>(stride),
+                            static_cast<uint32_t>(box_rows), kBK);
+}
+
+cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap* tw2, const GemmI8& p, cudaStream_t s) {
+  if (p.M <= 0) return cudaSuccess;
+  return tw2 ? launch_by_tokens<true>(ta, tw, *tw2, p, s) : launch_by_tokens<false>(ta, tw, tw, p, s);
+}
+
+cudaError_t i8_status(uint32_t* bits, cudaStream_t s) {
+  cudaError_t e = cudaMemcpyFromSymbolAsync(bits, g_status, sizeof(uint32_t), 0, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e != cudaSuccess || *bits == 0) return e;
+  const uint32_t zero = 0;
+  e = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof(uint32_t), 0, cudaMemcpyHostToDevice, s);
+  return e == cudaSuccess ? cudaStreamSynchronize(s) : e;
+}
+
+}  // namespace cs
