@@ -1,7 +1,7 @@
 // Products of 8-bit codes: out[t, n] = a_scale[t] w_scale[n] sum_k a[t, k] w[n, k], the sum in 32-bit integers on the tensor cores
 // (tcgen05, kind::i8) and exact, whatever its order.
 //
-// Narrow form: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few columns.
+// Many tokens: see the wide form below. Narrow form, few tokens: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few columns.
 // A CTA owns 128 output channels, up to 256 tokens and a piece of the k range; the pieces of a tile are the CTAs of a cluster, each
 // of which collects the others' sums for its share of the tokens through distributed shared memory. Nothing is kept between calls.
 #include "i8.h"
@@ -64,8 +64,13 @@ __device__ __forceinline__ void st_peer_v2(uint32_t addr, uint32_t a, uint32_t b
   asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
 }
 
-// y / (1 + e^-y); the fast division leaves 0 for a divisor beyond 2^126, which is what the quotient tends to.
-__device__ __forceinline__ float silu(float y) { return __fdividef(y, 1.0f + __expf(-y)); }
+// A sum with its scales, and what becomes of it. Every operation is rounded by itself, so that no form of the product fuses two of
+// them and a token has the same bits in every batch.
+__device__ __forceinline__ float scaled(uint32_t acc, float as, float ws) {
+  return __fmul_rn(__fmul_rn(static_cast<float>(static_cast<int>(acc)), as), ws);
+}
+// silu(y) y2, silu(y) = y / (1 + e^-y); the fast division leaves 0 for a divisor beyond 2^126, which is what the quotient tends to.
+__device__ __forceinline__ float gate(float y, float y2) { return __fmul_rn(__fdividef(y, __fadd_rn(1.0f, __expf(-y))), y2); }
 
 __device__ __forceinline__ void store_one(void* out, int64_t at, float v, int type) {
   if (type == kF16) static_cast<__half*>(out)[at] = __float2half_rn(v);
@@ -198,7 +203,7 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     if (GATED) ws2 = p.w2_scales[n];
   }
   if (results) {
-    ok = mbar_wait(acc_bar, 0, abort_flag, status);
+    ok = __all_sync(0xffffffffu, mbar_wait(acc_bar, 0, abort_flag, status));
     tc_fence_after();
   }
   if (split > 1) {
@@ -237,17 +242,15 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       for (int j = 0; j < 16; j += 2) {
         const int col = c + j - own * piece;
         if (col < 0 || col >= own) continue;
-        int s[2] = {static_cast<int>(r[j]), static_cast<int>(r[j + 1])};
-        int s2[2] = {0, 0};
-        if (GATED) { s2[0] = static_cast<int>(r2[j]); s2[1] = static_cast<int>(r2[j + 1]); }
+        uint32_t s[2] = {r[j], r[j + 1]}, s2[2] = {r2[j], r2[j + 1]};
         for (int q = 0; q < split; ++q) {
           if (q == piece) continue;
-          const int2* from = reinterpret_cast<const int2*>(smem) + (q * own / 2 + (col >> 1)) * L::kWTiles * 128 + row;
-          const int2 v = from[0];
+          const uint2* from = reinterpret_cast<const uint2*>(smem) + (q * own / 2 + (col >> 1)) * L::kWTiles * 128 + row;
+          const uint2 v = from[0];
           s[0] += v.x;
           s[1] += v.y;
           if (GATED) {
-            const int2 v2 = from[128];
+            const uint2 v2 = from[128];
             s2[0] += v2.x;
             s2[1] += v2.y;
           }
@@ -257,9 +260,9 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           const int t = t0 + c + j + e;
           if (t >= p.M || !n_ok) continue;
           const float as = p.a_scales[t];
-          float v = static_cast<float>(s[e]) * as * ws;
-          if (GATED) v = silu(v) * (static_cast<float>(s2[e]) * as * ws2);
-          if (p.add) v += p.add[t * p.add_stride + n];
+          float v = scaled(s[e], as, ws);
+          if (GATED) v = gate(v, scaled(s2[e], as, ws2));
+          if (p.add) v = __fadd_rn(p.add[t * p.add_stride + n], v);
           store_one(p.out, t * p.out_stride + n, v, p.type);
         }
       }
@@ -298,7 +301,7 @@ cudaError_t launch_narrow(const CUtensorMap& ta, const CUtensorMap& tw, const CU
 
 template <bool GATED>
 cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
-  switch (gemm_i8_box(p.M, GATED)) {
+  switch (gemm_i8_box(p.M, GATED)) {     // at most kNarrowTokens
     case 16: return launch_narrow<16, GATED>(ta, tw, tw2, p, s);
     case 32: return launch_narrow<32, GATED>(ta, tw, tw2, p, s);
     case 64: return launch_narrow<64, GATED>(ta, tw, tw2, p, s);
@@ -307,9 +310,345 @@ cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const
   }
 }
 
+// ---------------------------------------------------------------------------------------------------------- wide form
+// Two CTAs (a pair) share a tile of 256 tokens x 256 rows of weights (gated: 128 of each matrix): each holds 128 rows of either
+// operand, the leader issues products that read both CTAs' shared memory (cta_group::2), and each keeps the sums of its own 128
+// tokens in its tensor memory, in one of two accumulators. Per SM and k block 32 KB are fetched for 512 cycles of products, half of
+// what two separate 128 x 256 tiles would fetch.
+constexpr int kWideThreads = 320;                      // warp 0: copies, warp 1: products, warps 2-9: results
+struct Wide {
+  static constexpr int kStageBytes = 2 * kTileBytes;
+  static constexpr int kStages = 6;
+  static constexpr int kScaleOff = kStages * kStageBytes;              // [2 accumulators][256] scales of the tile's weights
+  static constexpr int kBarOff = kScaleOff + 2 * 256 * 4;
+  static constexpr int kTotal = kBarOff + 256 + 1024;
+};
+
+// The same as umma_i8_block over the pair. A test of `peek_bar` is issued before the products and its answer read after them: a wait
+// on a barrier, even a complete one, would leave the tensor cores without work for its round trip.
+__device__ __forceinline__ bool umma_i8_pair_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
+                                                   uint64_t* commit_bar, uint32_t ctas, uint64_t* peek_bar, uint32_t peek_parity) {
+  uint32_t ready;
+  asm volatile(
+      "{\n\t.reg .pred P, Q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 m;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\t"
+      "setp.ne.b32 Q, %7, 0;\n\t"
+      "add.u64 a1, %4, 2;\n\tadd.u64 b1, %5, 2;\n\t"
+      "add.u64 a2, %4, 4;\n\tadd.u64 b2, %5, 4;\n\t"
+      "add.u64 a3, %4, 6;\n\tadd.u64 b3, %5, 6;\n\t"
+      "cvt.u16.u32 m, %9;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%3], %4, %5, %6, Q;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%3], a1, b1, %6, 1;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%3], a2, b2, %6, 1;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%3], a3, b3, %6, 1;\n\t"
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%8], m;\n\t"
+      "selp.u32 %0, 1, 0, P;\n\t}"
+      : "=r"(ready)
+      : "r"(smem_u32(peek_bar)), "r"(peek_parity), "r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate),
+        "r"(smem_u32(commit_bar)), "r"(ctas)
+      : "memory");
+  return ready != 0;
+}
+// Arrives at this barrier of every CTA of the mask once the products issued so far are done.
+__device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint32_t ctas) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(smem_u32(bar)), "h"(static_cast<uint16_t>(ctas))
+               : "memory");
+}
+// A copy into this CTA's shared memory that counts at a barrier of the pair's leader.
+__device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, uint32_t leader_bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leader_bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n\t"
+               "tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
+}
+__device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// 32 consecutive results of one token.
+template <bool GATED>
+__device__ __forceinline__ void finish_row(const GemmI8& p, const uint32_t (&r)[32], const uint32_t (&r2)[32], float as, const float* ws,
+                                           const float* ws2, int64_t t, int n, bool pieces) {
+  float v[32];
+#pragma unroll
+  for (int j = 0; j < 32; ++j) {
+    v[j] = scaled(r[j], as, ws[j]);
+    if (GATED) v[j] = gate(v[j], scaled(r2[j], as, ws2[j]));
+  }
+  if (!pieces || n + 32 > p.N) {                       // rows that are not whole 16-byte pieces, and the last columns
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+      if (n + j < p.N) store_one(p.out, t * p.out_stride + n + j, p.add ? __fadd_rn(p.add[t * p.add_stride + n + j], v[j]) : v[j], p.type);
+    return;
+  }
+  if (p.type == kF32) {
+    float4* o = reinterpret_cast<float4*>(static_cast<float*>(p.out) + t * p.out_stride + n);
+    const float4* a = reinterpret_cast<const float4*>(p.add + t * p.add_stride + n);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float4 x = p.add ? a[j] : make_float4(0.f, 0.f, 0.f, 0.f);
+      o[j] = p.add ? make_float4(__fadd_rn(x.x, v[4 * j]), __fadd_rn(x.y, v[4 * j + 1]), __fadd_rn(x.z, v[4 * j + 2]), __fadd_rn(x.w, v[4 * j + 3]))
+                   : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    }
+    return;
+  }
+  uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + t * p.out_stride + n);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float lo = v[8 * j + 2 * e], hi = v[8 * j + 2 * e + 1];
+      w[e] = p.type == kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+    }
+    o[j] = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+template <bool GATED>
+__global__ void __launch_bounds__(kWideThreads, 1)
+gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
+                    const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int t_tiles, int tiles, int split, int pieces_ok) {
+  using L = Wide;
+  constexpr uint32_t kIdesc = idesc_i8(256, 256);
+  constexpr int kOut = GATED ? 128 : 256;              // output columns of a tile
+  constexpr int kUnits = kOut / 32;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* scales = reinterpret_cast<float*>(smem + L::kScaleOff);
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* full_bar = bars;                           // the leader's: both CTAs' copies of a stage
+  uint64_t* empty_bar = bars + L::kStages;             // each CTA's own
+  uint64_t* acc_full = bars + 2 * L::kStages;          // [2], each CTA's own
+  uint64_t* acc_empty = bars + 2 * L::kStages + 2;     // [2], the leader's: both CTAs' eight warps
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 4);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* status = p.status ? p.status : &g_status;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t rank;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  const uint32_t half = rank & 1, leader = rank & ~1u, pair_mask = 3u << leader;
+  const int piece = rank >> 1;
+  const int kblocks = (p.K + kBK - 1) / kBK;
+  const int kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * piece / split);
+  const int kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (piece + 1) / split);
+  const int first = blockIdx.x / (2 * split), step = gridDim.x / (2 * split);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < L::kStages; ++s) {
+      mbar_init(&full_bar[s], 1);
+      mbar_init(&empty_bar[s], 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(&acc_full[a], 1);
+      mbar_init(&acc_empty[a], 16);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+    tma_prefetch_desc(&tm_a);
+    tma_prefetch_desc(GATED && half ? &tm_w2 : &tm_w);
+  }
+  if (warp == 1) tmem_alloc_pair(tmem_slot, 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive_wait();                               // the pair's barriers are ready
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  pdl_launch_dependents();
+
+  // Token tiles run fastest: tiles that are in work together share their weights, and every weight is read from DRAM about once.
+  const auto token0 = [&](int tile) { return (tile % t_tiles) * 256 + static_cast<int>(half) * 128; };
+  const auto column0 = [&](int tile) { return tile / t_tiles * kOut; };
+  const auto load_w = [&](int stage, uint32_t bar, int kb, int tile) {
+    uint8_t* dst = smem + stage * L::kStageBytes + kTileBytes;
+    if (GATED) tma_load_2d_pair(dst, half ? &tm_w2 : &tm_w, bar, kb * kBK, column0(tile));
+    else tma_load_2d_pair(dst, &tm_w, bar, kb * kBK, column0(tile) + static_cast<int>(half) * 128);
+  };
+  int ahead = 0;
+  if (threadIdx.x == 0 && p.weights_settled && first < tiles) {
+    for (; ahead < L::kStages && kb0 + ahead < kb1; ++ahead) {
+      if (!half) mbar_arrive_expect_tx(&full_bar[ahead], 2 * L::kStageBytes);
+      load_w(ahead, peer_addr(smem_u32(&full_bar[ahead]), leader), kb0 + ahead, first);
+    }
+  }
+  pdl_wait();
+
+  bool ok = true;
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0, issued = 0;
+      uint32_t phase = 0;
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        for (int kb = kb0; kb < kb1; ++kb, ++issued) {
+          const uint32_t bar = peer_addr(smem_u32(&full_bar[stage]), leader);
+          if (issued >= ahead) {
+            if (!mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, status)) { ok = false; break; }
+            if (!half) mbar_arrive_expect_tx(&full_bar[stage], 2 * L::kStageBytes);
+            load_w(stage, bar, kb, tile);
+          }
+          tma_load_2d_pair(smem + stage * L::kStageBytes, &tm_a, bar, kb * kBK, token0(tile));
+          if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+        }
+      }
+      // after a time-out: let the copies in flight land before the CTA goes away
+      if (!ok)
+        for (int i = 0; i < 64; ++i) __nanosleep(10000);
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && !half) {
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      bool ready = false;
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem)), bdesc0 = umma_desc_k128(smem_u32(smem) + kTileBytes);
+      for (int tile = first; tile < tiles && ok; tile += step) {
+        if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, status)) { ok = false; break; }
+        tc_fence_after();
+        for (int kb = kb0; kb < kb1; ++kb) {
+          if (!ready && !mbar_wait(&full_bar[stage], phase, abort_flag, status)) { ok = false; break; }
+          tc_fence_after();
+          const int next = stage + 1 == L::kStages ? 0 : stage + 1;
+          const uint32_t next_phase = next == 0 ? phase ^ 1u : phase;
+          const uint64_t off = static_cast<uint64_t>(stage * (L::kStageBytes >> 4));
+          ready = umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kb != kb0, &empty_bar[stage], pair_mask,
+                                     &full_bar[next], next_phase);
+          stage = next;
+          phase = next_phase;
+        }
+        if (!ok) break;
+        umma_commit_pair(&acc_full[acc], pair_mask);
+        acc ^= 1;
+        if (acc == 0) acc_phase ^= 1u;
+      }
+    }
+  }
+  __syncwarp();
+
+  // ------------------------------------------------------------------ results: a thread per token, two warps per 32 tokens
+  if (warp >= 2 || split > 1) {
+    const bool results = warp >= 2;
+    const int quad = warp & 3, side = (warp - 2) >> 2;
+    const int row = quad * 32 + lane;
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    for (int tile = first; tile < tiles; tile += step) {
+      const int t = token0(tile) + row, n0 = column0(tile);
+      const bool t_ok = t < p.M;
+      float* ws = scales + acc * 256;
+      float as = 0.f;
+      if (results) {
+        // column c of the tile is row c of w, or of w2 behind the first 128 of a gated tile
+        const int c = threadIdx.x - 64;
+        const int n = n0 + (GATED ? c & 127 : c);
+        ws[c] = n < p.N ? (GATED && c >= 128 ? p.w2_scales[n] : p.w_scales[n]) : 0.f;
+        if (t_ok) as = p.a_scales[t];
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, status));
+        tc_fence_after();
+      }
+      const uint32_t t_row = tmem_base + acc * 256 + (static_cast<uint32_t>(quad * 32) << 16);
+      const int own = kUnits / split;                  // 32-column units that this pair writes: own * piece ..
+      if (split > 1) {
+        // Everybody's products are done with the stages: they become [piece][own unit][matrix][4-column group][128 tokens][4].
+        cluster_arrive_wait();
+        if (results) {
+          constexpr int kUnitBytes = (GATED ? 2 : 1) * 128 * 128;
+          for (int u = side; u < kUnits; u += 2) {
+            const int to = u / own;
+            if (to == piece) continue;
+            const uint32_t at = peer_addr(smem_u32(smem) + static_cast<uint32_t>((piece * own + u - to * own) * kUnitBytes + row * 16),
+                                          static_cast<uint32_t>(2 * to) + half);
+#pragma unroll
+            for (int w = 0; w < (GATED ? 2 : 1); ++w) {
+              uint32_t r[32];
+              tmem_ld_32x32(t_row + w * 128 + u * 32, r);
+              tmem_ld_wait();
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                st_peer_v4(at + w * 16384 + j * 2048, r[4 * j], r[4 * j + 1], r[4 * j + 2], r[4 * j + 3]);
+            }
+          }
+        }
+        cluster_arrive_wait();
+      }
+      if (results) {
+        for (int u = own * piece + side; u < own * (piece + 1); u += 2) {
+          if (!ok || n0 + u * 32 >= p.N) break;
+          uint32_t r[32], r2[32];
+          tmem_ld_32x32(t_row + u * 32, r);
+          if (GATED) tmem_ld_32x32(t_row + 128 + u * 32, r2);
+          tmem_ld_wait();
+          for (int q = 0; q < split; ++q) {
+            if (q == piece) continue;
+            const uint8_t* from = smem + (q * own + u - own * piece) * (GATED ? 2 : 1) * 16384 + row * 16;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              const uint4 v = *reinterpret_cast<const uint4*>(from + j * 2048);
+              r[4 * j] += v.x; r[4 * j + 1] += v.y; r[4 * j + 2] += v.z; r[4 * j + 3] += v.w;
+              if (GATED) {
+                const uint4 v2 = *reinterpret_cast<const uint4*>(from + 16384 + j * 2048);
+                r2[4 * j] += v2.x; r2[4 * j + 1] += v2.y; r2[4 * j + 2] += v2.z; r2[4 * j + 3] += v2.w;
+              }
+            }
+          }
+          if (t_ok) finish_row<GATED>(p, r, r2, as, ws + u * 32, ws + 128 + u * 32, t, n0 + u * 32, pieces_ok);
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_at(peer_addr(smem_u32(&acc_empty[acc]), leader));
+      }
+      acc ^= 1;
+      if (acc == 0) acc_phase ^= 1u;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  cluster_arrive_wait();                               // nobody leaves while the pair may still use its memory
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem_base, 512);
+  }
+}
+
+template <bool GATED>
+cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
+  static std::atomic<uint64_t> opted{0};
+  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_wide_kernel<GATED>, Wide::kTotal, opted); e != cudaSuccess) return e;
+  constexpr int kPairs = kNumSMs / 2;
+  const int64_t t_tiles = (p.M + 255) / 256, n_tiles = (p.N + (GATED ? 127 : 255)) / (GATED ? 128 : 256), tiles = t_tiles * n_tiles;
+  if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
+  const int kblocks = (p.K + kBK - 1) / kBK;
+  int split = 1;
+  while (split < 4 && tiles * split * 2 <= kPairs && kblocks >= 8 * split) split *= 2;
+  const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
+  const int bytes = p.type == kF32 ? 4 : 2;
+  const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
+                      (!p.add || (reinterpret_cast<uintptr_t>(p.add) % 16 == 0 && p.add_stride % 4 == 0));
+  const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide::kTotal, s,
+                                           2 * split, ta, tw, tw2, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
+                                           pieces ? 1 : 0);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// Up to this many tokens are the columns of the narrow form.
+constexpr int kNarrowTokens = 256;
+
 }  // namespace
 
-int gemm_i8_box(int M, bool) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256; }
+int gemm_i8_box(int M, bool) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : M <= kNarrowTokens ? 256 : 128; }
 
 bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows) {
   return make_tensor_map_8b(tm, base, static_cast<uint64_t>(rows), static_cast<uint64_t>(k), static_cast<uint64_t>(stride),
@@ -318,6 +657,7 @@ bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t s
 
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap* tw2, const GemmI8& p, cudaStream_t s) {
   if (p.M <= 0) return cudaSuccess;
+  if (p.M > kNarrowTokens) return tw2 ? launch_wide<true>(ta, tw, *tw2, p, s) : launch_wide<false>(ta, tw, tw, p, s);
   return tw2 ? launch_by_tokens<true>(ta, tw, *tw2, p, s) : launch_by_tokens<false>(ta, tw, tw, p, s);
 }
 

@@ -182,6 +182,7 @@ SHAPES = [  # M, N, K
     (64, 1000, 2048), (65, 63, 640), (100, 1536, 1536), (128, 256, 8960), (129, 7, 1024), (200, 777, 256), (255, 512, 48),
     (256, 130, 2064), (257, 2048, 384), (300, 264, 1552), (421, 2048, 2048), (513, 1030, 896), (1163, 1536, 8960), (1, 5, 131056),
     (300, 640, 32768), (3001, 96, 64), (2050, 2500, 160),
+    (260, 100, 4096), (512, 520, 2048), (5377, 1536, 1536), (270, 20001, 80),
 ]
 
 
@@ -218,6 +219,26 @@ def test_product(B, M, N, K, how):
     big = np.abs(y) > 65000 if kind == "f16" else np.zeros(y.shape, bool)
     I.check(_np(out)[~big], y[~big], I.rounded(y, b, kind)[~big])
     B.cs_i8_status()
+
+
+@pytest.mark.parametrize("N,K", [(264, 1552), (2048, 1536), (520, 8960)])
+@pytest.mark.parametrize("how", ["f16", "add", "gated"])
+def test_a_token_has_the_same_bits_in_every_batch(B, N, K, how):
+    """Every form of the product applies the scales in one order to an exact sum."""
+    import torch
+    g = np.random.default_rng(N)
+    a, sa = (_dev(v) for v in I.codes_of(g, 1200, K))
+    w, sw = (_dev(v) for v in I.codes_of(g, N, K))
+    sw /= 10.0
+    more = dict(w2=w.flip(0).contiguous(), w2_scales=sw) if how == "gated" else {}
+    x = torch.randn(1200, N, device="cuda") if how == "add" else None
+    kind = torch.float32 if how == "add" else torch.float16
+    whole = torch.empty(1200, N, dtype=kind, device="cuda")
+    B.cs_gemm_i8(a, sa, w, sw, whole, add=x, **more)
+    for m in (1, 16, 29, 60, 128, 250, 300, 512, 700):
+        out = torch.empty(m, N, dtype=kind, device="cuda")
+        B.cs_gemm_i8(a[7:7 + m], sa[7:7 + m], w, sw, out, add=None if x is None else x[7:7 + m], **more)
+        assert torch.equal(out, whole[7:7 + m]), m
 
 
 @pytest.mark.parametrize("M,N", [(1, 130), (40, 130), (130, 130), (300, 300), (600, 520)])
