@@ -55,6 +55,10 @@ __device__ __forceinline__ void tmem_ld_16(uint32_t taddr, uint32_t (&r)[16]) {
 __device__ __forceinline__ void cluster_arrive_wait() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// Where only the order of the CTAs' progress matters: a releasing arrival would wait for this thread's stores to global memory.
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t cta) {
   uint32_t r;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
@@ -208,7 +212,7 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
   if (split > 1) {
     // Everybody's products are done with the stages: they become [piece][pair of tokens][weight matrix][128 channels][2].
-    cluster_arrive_wait();
+    cluster_meet();
     if (results) {
       const uint32_t mine = smem_u32(smem) + static_cast<uint32_t>(piece * own * L::kWTiles * 512);
 #pragma unroll 1
@@ -319,35 +323,43 @@ constexpr int kWideThreads = 320;                      // warp 0: copies, warp 1
 struct Wide {
   static constexpr int kStageBytes = 2 * kTileBytes;
   static constexpr int kStages = 6;
-  static constexpr int kScaleOff = kStages * kStageBytes;              // [2 accumulators][256] scales of the tile's weights
-  static constexpr int kBarOff = kScaleOff + 2 * 256 * 4;
+  static constexpr int kBoxOff = kStages * kStageBytes;               // [8 warps] 32 rows of 32 results on their way out
+  static constexpr int kBoxBytes = 4096;
+  static constexpr int kScaleOff = kBoxOff + 8 * kBoxBytes;           // [256] scales of the tile's weights
+  static constexpr int kBarOff = kScaleOff + 256 * 4;
   static constexpr int kTotal = kBarOff + 256 + 1024;
+  static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
-// The same as umma_i8_block over the pair. A test of `peek_bar` is issued before the products and its answer read after them: a wait
-// on a barrier, even a complete one, would leave the tensor cores without work for its round trip.
-__device__ __forceinline__ bool umma_i8_pair_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
-                                                   uint64_t* commit_bar, uint32_t ctas, uint64_t* peek_bar, uint32_t peek_parity) {
-  uint32_t ready;
+// The same as umma_i8_block over the pair, and an arrival at `commit_bar` of both CTAs once the products are done.
+__device__ __forceinline__ void umma_i8_pair_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
+                                                   uint64_t* commit_bar, uint32_t ctas) {
   asm volatile(
-      "{\n\t.reg .pred P, Q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 m;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\t"
-      "setp.ne.b32 Q, %7, 0;\n\t"
-      "add.u64 a1, %4, 2;\n\tadd.u64 b1, %5, 2;\n\t"
-      "add.u64 a2, %4, 4;\n\tadd.u64 b2, %5, 4;\n\t"
-      "add.u64 a3, %4, 6;\n\tadd.u64 b3, %5, 6;\n\t"
-      "cvt.u16.u32 m, %9;\n\t"
-      "tcgen05.mma.cta_group::2.kind::i8 [%3], %4, %5, %6, Q;\n\t"
-      "tcgen05.mma.cta_group::2.kind::i8 [%3], a1, b1, %6, 1;\n\t"
-      "tcgen05.mma.cta_group::2.kind::i8 [%3], a2, b2, %6, 1;\n\t"
-      "tcgen05.mma.cta_group::2.kind::i8 [%3], a3, b3, %6, 1;\n\t"
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%8], m;\n\t"
-      "selp.u32 %0, 1, 0, P;\n\t}"
-      : "=r"(ready)
-      : "r"(smem_u32(peek_bar)), "r"(peek_parity), "r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate),
-        "r"(smem_u32(commit_bar)), "r"(ctas)
+      "{\n\t.reg .pred Q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 m;\n\t"
+      "setp.ne.b32 Q, %4, 0;\n\t"
+      "add.u64 a1, %1, 2;\n\tadd.u64 b1, %2, 2;\n\t"
+      "add.u64 a2, %1, 4;\n\tadd.u64 b2, %2, 4;\n\t"
+      "add.u64 a3, %1, 6;\n\tadd.u64 b3, %2, 6;\n\t"
+      "cvt.u16.u32 m, %6;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, Q;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], a1, b1, %3, 1;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], a2, b2, %3, 1;\n\t"
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], a3, b3, %3, 1;\n\t"
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], m;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(smem_u32(commit_bar)), "r"(ctas)
       : "memory");
-  return ready != 0;
+}
+// Whether the phase is complete, without waiting.
+__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred P;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 P, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, P;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_u32(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
 }
 // Arrives at this barrier of every CTA of the mask once the products issued so far are done.
 __device__ __forceinline__ void umma_commit_pair(uint64_t* bar, uint32_t ctas) {
@@ -376,50 +388,105 @@ __device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b
   asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// 32 consecutive results of one token.
+// 32 consecutive results of one token per lane.
 template <bool GATED>
-__device__ __forceinline__ void finish_row(const GemmI8& p, const uint32_t (&r)[32], const uint32_t (&r2)[32], float as, const float* ws,
-                                           const float* ws2, int64_t t, int n, bool pieces) {
-  float v[32];
+__device__ __forceinline__ void results_of(const uint32_t (&r)[32], const uint32_t (&r2)[32], float as, const float* ws, const float* ws2,
+                                           float (&v)[32]) {
 #pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    v[j] = scaled(r[j], as, ws[j]);
-    if (GATED) v[j] = gate(v[j], scaled(r2[j], as, ws2[j]));
+  for (int j = 0; j < 8; ++j) {
+    const float4 w = reinterpret_cast<const float4*>(ws)[j];
+    const float wj[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[4 * j + e] = scaled(r[4 * j + e], as, wj[e]);
+    if (GATED) {
+      const float4 w2 = reinterpret_cast<const float4*>(ws2)[j];
+      const float w2j[4] = {w2.x, w2.y, w2.z, w2.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = gate(v[4 * j + e], scaled(r2[4 * j + e], as, w2j[e]));
+    }
   }
-  if (!pieces || n + 32 > p.N) {                       // rows that are not whole 16-byte pieces, and the last columns
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* m, const void* src, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];\n\t"
+               "cp.async.bulk.commit_group;" ::"l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(src)), "r"(x), "r"(y)
+               : "memory");
+}
+// Until at most N of this thread's stores still read their shared memory.
+template <int N>
+__device__ __forceinline__ void tma_store_wait() {
+  asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory");
+}
+constexpr int kOutBoxes = 0, kOutPieces = 1, kOutValues = 2;
+// A warp's 32 rows x 32 columns through its box in shared memory, so that rows are written in whole 64- or 128-byte pieces (from the
+// lanes' registers every store would touch 32 rows). Stores are boxes of a tensor map, or, where the residual is added, 16-byte pieces,
+// or single values where rows of the output are not made of 16-byte pieces. Boxes of 16-bit results alternate between two places.
+__device__ __forceinline__ void write_box(const GemmI8& p, const CUtensorMap* tm_out, uint8_t* box, int& turn, const float (&v)[32], int t0,
+                                          int n0, int lane, int out_way) {
+  if (p.type != kF32) {
+    box += turn * 2048;
+    if (out_way == kOutBoxes) {
+      if (lane == 0) tma_store_wait<1>();
+      turn ^= 1;
+    }
+    __syncwarp();
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (n + j < p.N) store_one(p.out, t * p.out_stride + n + j, p.add ? __fadd_rn(p.add[t * p.add_stride + n + j], v[j]) : v[j], p.type);
+    for (int j = 0; j < 4; ++j) {
+      uint32_t w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float lo = v[8 * j + 2 * e], hi = v[8 * j + 2 * e + 1];
+        w[e] = p.type == kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+      }
+      *reinterpret_cast<uint4*>(box + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  } else {
+    if (out_way == kOutBoxes && lane == 0) tma_store_wait<0>();
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      *reinterpret_cast<float4*>(box + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+  }
+  if (out_way == kOutBoxes) {
+    fence_proxy_async();
+    __syncwarp();
+    if (lane == 0 && t0 < p.M) tma_store_2d(tm_out, box, n0, t0);
     return;
   }
-  if (p.type == kF32) {
-    float4* o = reinterpret_cast<float4*>(static_cast<float*>(p.out) + t * p.out_stride + n);
-    const float4* a = reinterpret_cast<const float4*>(p.add + t * p.add_stride + n);
+  __syncwarp();
+  if (out_way == kOutPieces && n0 + 32 <= p.N) {           // fp32, with or without the residual
+    const int c = lane & 7;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float4 x = p.add ? a[j] : make_float4(0.f, 0.f, 0.f, 0.f);
-      o[j] = p.add ? make_float4(__fadd_rn(x.x, v[4 * j]), __fadd_rn(x.y, v[4 * j + 1]), __fadd_rn(x.z, v[4 * j + 2]), __fadd_rn(x.w, v[4 * j + 3]))
-                   : make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    for (int i = 0; i < 8; ++i) {
+      const int row = 4 * i + (lane >> 3);
+      const int64_t t = t0 + row;
+      if (t >= p.M) break;
+      float4 y = *reinterpret_cast<const float4*>(box + row * 128 + ((c ^ (row & 7)) << 4));
+      if (p.add) {
+        const float4 x = *reinterpret_cast<const float4*>(p.add + t * p.add_stride + n0 + 4 * c);
+        y = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
+      }
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + t * p.out_stride + n0 + 4 * c) = y;
     }
-    return;
-  }
-  uint4* o = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + t * p.out_stride + n);
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float lo = v[8 * j + 2 * e], hi = v[8 * j + 2 * e + 1];
-      w[e] = p.type == kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+  } else if (n0 + lane < p.N) {
+    for (int row = 0; row < 32 && t0 + row < p.M; ++row) {
+      const int64_t t = t0 + row;
+      if (p.type == kF32) {
+        float y = *reinterpret_cast<const float*>(box + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4);
+        if (p.add) y = __fadd_rn(p.add[t * p.add_stride + n0 + lane], y);
+        static_cast<float*>(p.out)[t * p.out_stride + n0 + lane] = y;
+      } else {
+        static_cast<uint16_t*>(p.out)[t * p.out_stride + n0 + lane] =
+            *reinterpret_cast<const uint16_t*>(box + row * 64 + (((lane >> 3) ^ (row >> 1 & 3)) << 4) + (lane & 7) * 2);
+      }
     }
-    o[j] = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
 template <bool GATED>
 __global__ void __launch_bounds__(kWideThreads, 1)
 gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
-                    const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int t_tiles, int tiles, int split, int pieces_ok) {
+                    const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_out, const GemmI8 p, int t_tiles,
+                    int tiles, int split, int out_way) {
   using L = Wide;
   constexpr uint32_t kIdesc = idesc_i8(256, 256);
   constexpr int kOut = GATED ? 128 : 256;              // output columns of a tile
@@ -436,7 +503,7 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* status = p.status ? p.status : &g_status;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   uint32_t rank;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t half = rank & 1, leader = rank & ~1u, pair_mask = 3u << leader;
@@ -507,7 +574,8 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
         for (int i = 0; i < 64; ++i) __nanosleep(10000);
     }
   } else if (warp == 1) {
-    if (lane == 0 && !half) {
+    // the whole warp keeps step, one elected thread issues: what it hands to the tensor cores is then known to be uniform
+    if (!half) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ready = false;
@@ -521,13 +589,15 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
           const int next = stage + 1 == L::kStages ? 0 : stage + 1;
           const uint32_t next_phase = next == 0 ? phase ^ 1u : phase;
           const uint64_t off = static_cast<uint64_t>(stage * (L::kStageBytes >> 4));
-          ready = umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kb != kb0, &empty_bar[stage], pair_mask,
-                                     &full_bar[next], next_phase);
+          ready = mbar_test(&full_bar[next], next_phase);
+          if (elect_one()) umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kb != kb0, &empty_bar[stage], pair_mask);
+          __syncwarp();
           stage = next;
           phase = next_phase;
         }
         if (!ok) break;
-        umma_commit_pair(&acc_full[acc], pair_mask);
+        if (elect_one()) umma_commit_pair(&acc_full[acc], pair_mask);
+        __syncwarp();
         acc ^= 1;
         if (acc == 0) acc_phase ^= 1u;
       }
@@ -540,19 +610,19 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     const bool results = warp >= 2;
     const int quad = warp & 3, side = (warp - 2) >> 2;
     const int row = quad * 32 + lane;
-    int acc = 0;
+    uint8_t* box = smem + L::kBoxOff + (results ? warp - 2 : 0) * L::kBoxBytes;
+    int acc = 0, turn = 0;
     uint32_t acc_phase = 0;
     for (int tile = first; tile < tiles; tile += step) {
       const int t = token0(tile) + row, n0 = column0(tile);
-      const bool t_ok = t < p.M;
-      float* ws = scales + acc * 256;
       float as = 0.f;
       if (results) {
+        asm volatile("bar.sync 1, 256;" ::: "memory");        // the last tile's scales have been read
         // column c of the tile is row c of w, or of w2 behind the first 128 of a gated tile
         const int c = threadIdx.x - 64;
         const int n = n0 + (GATED ? c & 127 : c);
-        ws[c] = n < p.N ? (GATED && c >= 128 ? p.w2_scales[n] : p.w_scales[n]) : 0.f;
-        if (t_ok) as = p.a_scales[t];
+        scales[c] = n < p.N ? (GATED && c >= 128 ? p.w2_scales[n] : p.w_scales[n]) : 0.f;
+        if (t < p.M) as = p.a_scales[t];
         asm volatile("bar.sync 1, 256;" ::: "memory");
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&acc_full[acc], acc_phase, abort_flag, status));
         tc_fence_after();
@@ -561,10 +631,11 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       const int own = kUnits / split;                  // 32-column units that this pair writes: own * piece ..
       if (split > 1) {
         // Everybody's products are done with the stages: they become [piece][own unit][matrix][4-column group][128 tokens][4].
-        cluster_arrive_wait();
+        cluster_meet();
         if (results) {
           constexpr int kUnitBytes = (GATED ? 2 : 1) * 128 * 128;
-          for (int u = side; u < kUnits; u += 2) {
+          for (int i = side; i < kUnits; i += 2) {
+            const int u = (i + own * (piece + 1)) % kUnits;      // everybody begins with another receiver
             const int to = u / own;
             if (to == piece) continue;
             const uint32_t at = peer_addr(smem_u32(smem) + static_cast<uint32_t>((piece * own + u - to * own) * kUnitBytes + row * 16),
@@ -583,7 +654,8 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
         cluster_arrive_wait();
       }
       if (results) {
-        for (int u = own * piece + side; u < own * (piece + 1); u += 2) {
+        const int u0 = own * piece + side * (own / 2);
+        for (int u = u0; u < u0 + own / 2; ++u) {
           if (!ok || n0 + u * 32 >= p.N) break;
           uint32_t r[32], r2[32];
           tmem_ld_32x32(t_row + u * 32, r);
@@ -602,7 +674,9 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
               }
             }
           }
-          if (t_ok) finish_row<GATED>(p, r, r2, as, ws + u * 32, ws + 128 + u * 32, t, n0 + u * 32, pieces_ok);
+          float v[32];
+          results_of<GATED>(r, r2, as, scales + u * 32, scales + 128 + u * 32, v);
+          write_box(p, &tm_out, box, turn, v, token0(tile) + quad * 32, n0 + u * 32, lane, out_way);
         }
         tc_fence_before();
         __syncwarp();
@@ -613,9 +687,10 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     }
   }
 
+  if (warp >= 2 && lane == 0) tma_store_wait<0>();
   tc_fence_before();
   __syncthreads();
-  cluster_arrive_wait();                               // nobody leaves while the pair may still use its memory
+  cluster_meet();                                      // nobody leaves while the pair may still use its memory
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc_pair(tmem_base, 512);
@@ -631,14 +706,17 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
   const int kblocks = (p.K + kBK - 1) / kBK;
   int split = 1;
-  while (split < 4 && tiles * split * 2 <= kPairs && kblocks >= 8 * split) split *= 2;
+  while (split < (GATED ? 2 : 4) && tiles * split * 2 <= kPairs && kblocks >= 8 * split) split *= 2;
   const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
   const int bytes = p.type == kF32 ? 4 : 2;
   const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
                       (!p.add || (reinterpret_cast<uintptr_t>(p.add) % 16 == 0 && p.add_stride % 4 == 0));
+  const int out_way = !pieces ? kOutValues : p.add ? kOutPieces : kOutBoxes;
+  CUtensorMap tm_out = ta;
+  if (out_way == kOutBoxes && !make_tensor_map_rows(&tm_out, p.out, p.M, p.N, p.out_stride, bytes, 32, 32)) return cudaErrorInvalidValue;
   const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide::kTotal, s,
-                                           2 * split, ta, tw, tw2, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
-                                           pieces ? 1 : 0);
+                                           2 * split, ta, tw, tw2, tm_out, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
+                                           out_way);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
