@@ -2231,12 +2231,17 @@ int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const i
   if (!aligned(out, type_bytes(dtype)) || out_stride < N) return CS_EINVAL;
   if (add && (!aligned(add, 4) || add_stride < N || (add == out && add_stride != out_stride && M > 1))) return CS_EINVAL;
   CUtensorMap ta, tw, tw2;
-  if (!make_i8_map(&ta, a, M, K, a_stride, gemm_i8_box(M, w2 != nullptr)) || !make_i8_map(&tw, w, N, K, K, 128) ||
-      (w2 && !make_i8_map(&tw2, w2, N, K, K, 128))) {
+  const int box = gemm_i8_box(M, N, K, w2 != nullptr);
+  if (box && (!make_i8_map(&ta, a, M, K, a_stride, box) || !make_i8_map(&tw, w, N, K, K, 128) ||
+              (w2 && !make_i8_map(&tw2, w2, N, K, K, 128)))) {
     g_cuda_error = "cuTensorMapEncodeTiled failed";
     return CS_ECUDA;
   }
   GemmI8 g = {};
+  g.a = a;
+  g.a_stride = a_stride;
+  g.w = w;
+  g.w2 = w2;
   g.a_scales = a_scales;
   g.w_scales = w_scales;
   g.w2_scales = w2_scales;
@@ -2248,7 +2253,7 @@ int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const i
   g.N = N;
   g.K = K;
   g.type = dtype;
-  CS_CUDA(gemm_i8(ta, tw, w2 ? &tw2 : nullptr, g, static_cast<cudaStream_t>(stream)));
+  CS_CUDA(gemm_i8(ta, tw, tw2, g, static_cast<cudaStream_t>(stream)));
   return CS_OK;
 }
 

@@ -1,9 +1,14 @@
 // Products of 8-bit codes: out[t, n] = a_scale[t] w_scale[n] sum_k a[t, k] w[n, k], the sum in 32-bit integers on the tensor cores
 // (tcgen05, kind::i8) and exact, whatever its order.
 //
-// Many tokens: see the wide form below. Narrow form, few tokens: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few columns.
-// A CTA owns 128 output channels, up to 256 tokens and a piece of the k range; the pieces of a tile are the CTAs of a cluster, each
-// of which collects the others' sums for its share of the tokens through distributed shared memory. Nothing is kept between calls.
+// Three forms by the number of tokens; a token has the same bits in all of them.
+//   up to 8     vector: integer dot products of the ordinary cores, weights straight from global memory into registers
+//   up to 128   narrow: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few
+//               columns; a CTA owns 128 output channels, all tokens and a piece of the k range, and the pieces of a tile are the
+//               CTAs of a cluster, each of which collects the others' sums for its share of the tokens through distributed shared
+//               memory
+//   more        wide: pairs of CTAs over 256 tokens x 256 rows of weights (below)
+// Nothing is kept between calls and no global memory is used in between.
 #include "i8.h"
 
 #include <algorithm>
@@ -18,7 +23,6 @@ namespace {
 
 constexpr int kBK = 128;                    // codes (= bytes) of a k block: one 128-byte swizzled row
 constexpr int kTileBytes = 128 * kBK;       // 128 rows of it
-constexpr int kThreads = 192;               // warp 0: copies, warp 1: products, warps 2-5: results
 constexpr int kMaxSplit = 8;
 
 // Time-outs of launches that are given no status word.
@@ -64,8 +68,8 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t addr, uint32_t cta) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
   return r;
 }
-__device__ __forceinline__ void st_peer_v2(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+__device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
 // A sum with its scales, and what becomes of it. Every operation is rounded by itself, so that no form of the product fuses two of
@@ -82,6 +86,102 @@ __device__ __forceinline__ void store_one(void* out, int64_t at, float v, int ty
   else static_cast<float*>(out)[at] = v;
 }
 
+// Clusters of 2 c CTAs that run at once, [one or two such CTAs to an SM][c]: what cudaOccupancyMaxActiveClusters says on a B200, whose
+// 148 SMs are not evenly spread over the groups that a cluster has to fit in.
+constexpr int kClusters[2][5] = {{0, 74, 33, 0, 15}, {0, 148, 71, 0, 33}};
+
+// -------------------------------------------------------------------------------------------------------- vector form
+constexpr int kVectorTokens = 8;            // at most
+constexpr int kVectorRows = 8;
+
+__device__ __forceinline__ uint4 load_once(const int8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int dot16(uint4 a, uint4 b, int s) {
+  s = __dp4a(static_cast<int>(a.x), static_cast<int>(b.x), s);
+  s = __dp4a(static_cast<int>(a.y), static_cast<int>(b.y), s);
+  s = __dp4a(static_cast<int>(a.z), static_cast<int>(b.z), s);
+  return __dp4a(static_cast<int>(a.w), static_cast<int>(b.w), s);
+}
+
+// A CTA holds eight rows of weights (gated: four of each matrix), its warps and lanes 16 codes of k at a time. Bound by reading the
+// weights.
+template <int TOKENS, bool GATED, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS)
+gemm_i8_vector_kernel(const int8_t* a, int64_t a_stride, const int8_t* w, const int8_t* w2, const GemmI8 p) {
+  constexpr int kChannels = GATED ? kVectorRows / 2 : kVectorRows;
+  __shared__ int sums[WARPS][kVectorRows * TOKENS];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n0 = blockIdx.x * kChannels;
+  pdl_launch_dependents();
+  if (!p.weights_settled) pdl_wait();
+  const int8_t* row[kVectorRows];
+#pragma unroll
+  for (int r = 0; r < kVectorRows; ++r)      // rows past the last are the last once more
+    row[r] = (GATED && r >= kChannels ? w2 : w) + static_cast<int64_t>(min(n0 + (GATED ? r % kChannels : r), p.N - 1)) * p.K;
+  int s[kVectorRows][TOKENS] = {};
+  bool waited = !p.weights_settled;
+#pragma unroll 1
+  for (int k = threadIdx.x * 16; k < p.K; k += WARPS * 512) {
+    uint4 x[kVectorRows];
+#pragma unroll
+    for (int r = 0; r < kVectorRows; ++r) x[r] = load_once(row[r] + k);
+    if (!waited) {
+      pdl_wait();
+      waited = true;
+    }
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+      const uint4 y = *reinterpret_cast<const uint4*>(a + min(t, p.M - 1) * a_stride + k);
+#pragma unroll
+      for (int r = 0; r < kVectorRows; ++r) s[r][t] = dot16(x[r], y, s[r][t]);
+    }
+  }
+  if (!waited) pdl_wait();
+#pragma unroll
+  for (int r = 0; r < kVectorRows; ++r)
+#pragma unroll
+    for (int t = 0; t < TOKENS; ++t) {
+      const int sum = __reduce_add_sync(0xffffffffu, s[r][t]);
+      if (lane == (r * TOKENS + t) % 32) sums[warp][r * TOKENS + t] = sum;
+    }
+  __syncthreads();
+  const int c = threadIdx.x % kChannels, t = threadIdx.x / kChannels, n = n0 + c;
+  if (t >= min(TOKENS, p.M) || n >= p.N) return;
+  int sum = 0, sum2 = 0;
+#pragma unroll
+  for (int q = 0; q < WARPS; ++q) {
+    sum += sums[q][c * TOKENS + t];
+    if (GATED) sum2 += sums[q][(c + kChannels) * TOKENS + t];
+  }
+  const float as = p.a_scales[t];
+  float v = scaled(static_cast<uint32_t>(sum), as, p.w_scales[n]);
+  if (GATED) v = gate(v, scaled(static_cast<uint32_t>(sum2), as, p.w2_scales[n]));
+  if (p.add) v = __fadd_rn(p.add[t * p.add_stride + n], v);
+  store_one(p.out, t * p.out_stride + n, v, p.type);
+}
+
+template <bool GATED, int WARPS>
+cudaError_t launch_vector(const GemmI8& p, int blocks, cudaStream_t s) {
+  const auto kernel = p.M == 1   ? gemm_i8_vector_kernel<1, GATED, WARPS>
+                      : p.M == 2 ? gemm_i8_vector_kernel<2, GATED, WARPS>
+                      : p.M <= 4 ? gemm_i8_vector_kernel<4, GATED, WARPS>
+                                 : gemm_i8_vector_kernel<8, GATED, 4>;
+  const cudaError_t e = launch_pdl(kernel, dim3(blocks), dim3(32 * WARPS), 0, s, p.a, p.a_stride, p.w, p.w2, p);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+template <bool GATED>
+cudaError_t launch_vector(const GemmI8& p, cudaStream_t s) {
+  const int channels = GATED ? kVectorRows / 2 : kVectorRows, blocks = (p.N + channels - 1) / channels;
+  return blocks <= 2 * kNumSMs && p.M <= 4 ? launch_vector<GATED, 8>(p, blocks, s) : launch_vector<GATED, 4>(p, blocks, s);
+}
+
+// -------------------------------------------------------------------------------------------------------- narrow form
+constexpr int kNarrowTokens = 128;
+constexpr int kNarrowThreads = 320;         // warp 0: copies, warp 1: products, warps 2-9: results
+
 template <int BN, bool GATED>
 struct Narrow {
   static constexpr int kWTiles = GATED ? 2 : 1;
@@ -89,22 +189,24 @@ struct Narrow {
   // Two CTAs to an SM where the columns are few, else one that takes it all.
   static constexpr int kStages = (BN * kWTiles <= 64 ? 112 * 1024 : 216 * 1024) / kStageBytes;
   static constexpr uint32_t kCols = kWTiles * BN < 32 ? 32 : kWTiles * BN;
-  static constexpr int kBarOff = kStages * kStageBytes;
+  static constexpr int kScaleOff = kStages * kStageBytes;   // [BN] scales of the tokens
+  static constexpr int kBarOff = kScaleOff + BN * 4;
   static constexpr int kTotal = kBarOff + 256 + 1024;       // + slack for the tiles' alignment
   // CTAs that share an SM must find their columns whenever they fit its shared memory: one that waited for columns while the rest of
   // its cluster waited for it could wait for a CTA that waits likewise.
-  static_assert(kTotal * 512ll >= kCols * 227ll * 1024 || kTotal > 190 * 1024, "tensor memory before shared memory");
-  static_assert(kStages >= 3 && kTotal <= 227 * 1024, "stages");
+  static_assert(kTotal * 512ll >= kCols * 227ll * 1024, "tensor memory before shared memory");
+  static_assert(kStages >= 3 && kTotal <= 227 * 1024 && std::max(BN, 4 * kMaxSplit) * kWTiles * 512 <= kStages * kStageBytes, "stages");
 };
 
 template <int BN, bool GATED>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kNarrowThreads)
 gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
-                      const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int n_tiles, int split) {
+                      const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int split, int log_own) {
   using L = Narrow<BN, GATED>;
   constexpr uint32_t kIdesc = idesc_i8(128, BN);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  float* a_scales = reinterpret_cast<float*>(smem + L::kScaleOff);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
   uint64_t* full_bar = bars;
   uint64_t* empty_bar = bars + L::kStages;
@@ -113,9 +215,8 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* status = p.status ? p.status : &g_status;
 
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int piece = blockIdx.x % split, tile = blockIdx.x / split;
-  const int n0 = (tile % n_tiles) * 128, t0 = (tile / n_tiles) * BN;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+  const int piece = blockIdx.x % split, n0 = blockIdx.x / split * 128;
   const int kblocks = (p.K + kBK - 1) / kBK;
   const int kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * piece / split);
   const int kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (piece + 1) / split);
@@ -166,7 +267,7 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           tma_load_2d(sw, &tm_w, &full_bar[stage], kb * kBK, n0);
           if (GATED) tma_load_2d(sw + kTileBytes, &tm_w2, &full_bar[stage], kb * kBK, n0);
         }
-        tma_load_2d(sw + L::kWTiles * kTileBytes, &tm_a, &full_bar[stage], kb * kBK, t0);
+        tma_load_2d(sw + L::kWTiles * kTileBytes, &tm_a, &full_bar[stage], kb * kBK, 0);
         if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
       }
       // after a time-out: let the copies in flight land before the CTA goes away
@@ -193,41 +294,43 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   }
   __syncwarp();
 
-  // ------------------------------------------------------------------ results: a thread per output channel
-  const int quad = warp & 3;      // the lanes of tensor memory that this warp may read
+  // ------------------------------------------------------------------ results: a thread per output channel, two warps per 32 channels
+  const int quad = warp & 3, side = (warp - 2) >> 2;      // the lanes of tensor memory that this warp may read; which chunks it takes
   const bool results = warp >= 2;
   const int row = quad * 32 + lane;
   const uint32_t t_row = tmem_base + (static_cast<uint32_t>(quad * 32) << 16);
-  const int own = BN / split;     // tokens that this CTA writes: own * piece ..
+  const int own0 = piece << log_own;                      // the 2^log_own tokens that this CTA writes
   const int n = n0 + row;
-  const bool n_ok = n < p.N;
   float ws = 0.f, ws2 = 0.f;
-  if (results && n_ok) {
-    ws = p.w_scales[n];
-    if (GATED) ws2 = p.w2_scales[n];
-  }
   if (results) {
+    const int t = threadIdx.x - 64;
+    if (t < BN) a_scales[t] = t < p.M ? p.a_scales[t] : 0.f;
+    if (n < p.N) {
+      ws = p.w_scales[n];
+      if (GATED) ws2 = p.w2_scales[n];
+    }
+    asm volatile("bar.sync 1, 256;" ::: "memory");
     ok = __all_sync(0xffffffffu, mbar_wait(acc_bar, 0, abort_flag, status));
     tc_fence_after();
   }
   if (split > 1) {
-    // Everybody's products are done with the stages: they become [piece][pair of tokens][weight matrix][128 channels][2].
+    // Everybody's products are done with the stages: they become [piece][four tokens][weight matrix][128 channels][4].
     cluster_meet();
     if (results) {
-      const uint32_t mine = smem_u32(smem) + static_cast<uint32_t>(piece * own * L::kWTiles * 512);
+      const uint32_t mine = smem_u32(smem) + static_cast<uint32_t>((piece << log_own) * L::kWTiles * 512 + row * 16);
 #pragma unroll 1
-      for (int c = 0; c < BN; c += 16) {
+      for (int c = side * 16; c < BN && c < p.M; c += 32) {
 #pragma unroll
         for (int w = 0; w < L::kWTiles; ++w) {
           uint32_t r[16];
           tmem_ld_16(t_row + w * BN + c, r);
           tmem_ld_wait();
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) {
-            const int to = (c + j) / own;
-            const int pair = (c + j - to * own) >> 1;
-            if (to != piece)
-              st_peer_v2(peer_addr(mine + static_cast<uint32_t>(((pair * L::kWTiles + w) * 128 + row) * 8), to), r[j], r[j + 1]);
+          for (int j = 0; j < 16; j += 4) {
+            const int to = (c + j) >> log_own;
+            if (to == piece || c + j >= p.M) continue;
+            const uint32_t at = peer_addr(mine, to) + static_cast<uint32_t>(((c + j - (to << log_own)) * L::kWTiles + 4 * w) * 512);
+            st_peer_v4(at, r[j], r[j + 1], r[j + 2], r[j + 3]);
           }
         }
       }
@@ -235,37 +338,36 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     cluster_arrive_wait();
   }
   if (results && ok) {
+    const int own1 = min(own0 + (1 << log_own), p.M);
 #pragma unroll 1
-    for (int c = own * piece & ~15; c < own * (piece + 1); c += 16) {
-      if (t0 + c >= p.M) break;
+    for (int c = (own0 & ~15) + side * 16; c < own1; c += 32) {
       uint32_t r[16], r2[16];
       tmem_ld_16(t_row + c, r);
       if (GATED) tmem_ld_16(t_row + BN + c, r2);
       tmem_ld_wait();
 #pragma unroll
-      for (int j = 0; j < 16; j += 2) {
-        const int col = c + j - own * piece;
-        if (col < 0 || col >= own) continue;
-        uint32_t s[2] = {r[j], r[j + 1]}, s2[2] = {r2[j], r2[j + 1]};
-        for (int q = 0; q < split; ++q) {
+      for (int j = 0; j < 16; j += 4) {
+        if (c + j < own0 || c + j >= own1) continue;
+        uint32_t s[4] = {r[j], r[j + 1], r[j + 2], r[j + 3]}, s2[4] = {r2[j], r2[j + 1], r2[j + 2], r2[j + 3]};
+        const uint4* from = reinterpret_cast<const uint4*>(smem) + (c + j - own0) / 4 * L::kWTiles * 128 + row;
+#pragma unroll 1
+        for (int q = 0; q < split; ++q, from += (L::kWTiles * 32) << log_own) {
           if (q == piece) continue;
-          const uint2* from = reinterpret_cast<const uint2*>(smem) + (q * own / 2 + (col >> 1)) * L::kWTiles * 128 + row;
-          const uint2 v = from[0];
-          s[0] += v.x;
-          s[1] += v.y;
+          const uint4 v = from[0];
+          s[0] += v.x; s[1] += v.y; s[2] += v.z; s[3] += v.w;
           if (GATED) {
-            const uint2 v2 = from[128];
-            s2[0] += v2.x;
-            s2[1] += v2.y;
+            const uint4 v2 = from[128];
+            s2[0] += v2.x; s2[1] += v2.y; s2[2] += v2.z; s2[3] += v2.w;
           }
         }
+        const float4 as4 = *reinterpret_cast<const float4*>(a_scales + c + j);
+        const float as[4] = {as4.x, as4.y, as4.z, as4.w};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int t = t0 + c + j + e;
-          if (t >= p.M || !n_ok) continue;
-          const float as = p.a_scales[t];
-          float v = scaled(s[e], as, ws);
-          if (GATED) v = gate(v, scaled(s2[e], as, ws2));
+        for (int e = 0; e < 4; ++e) {
+          const int64_t t = c + j + e;
+          if (t >= own1 || n >= p.N) continue;
+          float v = scaled(s[e], as[e], ws);
+          if (GATED) v = gate(v, scaled(s2[e], as[e], ws2));
           if (p.add) v = __fadd_rn(p.add[t * p.add_stride + n], v);
           store_one(p.out, t * p.out_stride + n, v, p.type);
         }
@@ -286,31 +388,30 @@ cudaError_t launch_narrow(const CUtensorMap& ta, const CUtensorMap& tw, const CU
   using L = Narrow<BN, GATED>;
   static std::atomic<uint64_t> opted{0};
   if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_narrow_kernel<BN, GATED>, L::kTotal, opted); e != cudaSuccess) return e;
-  const int n_tiles = (p.N + 127) / 128, t_tiles = (p.M + BN - 1) / BN, kblocks = (p.K + kBK - 1) / kBK;
-  const int64_t tiles = static_cast<int64_t>(n_tiles) * t_tiles;
-  int split = 1;
-  // every piece has a k block, every CTA of the cluster a pair of tokens, and the sums fit where the stages were
-  while (split < kMaxSplit && tiles * split * 2 <= 2 * kNumSMs && kblocks >= 2 * split && BN / (2 * split) >= 2 &&
-         BN * L::kWTiles * 512 <= L::kBarOff)
+  const int tiles = (p.N + 127) / 128, kblocks = (p.K + kBK - 1) / kBK;
+  int split = 1, log_own = BN == 16 ? 4 : BN == 32 ? 5 : BN == 64 ? 6 : 7;
+  // every piece has a k block, and all clusters run at once; fewer than four tokens are not shared out
+  constexpr int kTogether = L::kTotal > 113 * 1024 ? 1 : 2;
+  while (split < kMaxSplit && tiles <= kClusters[kTogether - 1][split] && kblocks >= 2 * split) {
     split *= 2;
-  if (tiles * split > 0x7fffffff) return cudaErrorInvalidValue;
+    log_own = std::max(2, log_own - 1);
+  }
   const dim3 grid(static_cast<unsigned>(tiles * split));
-  const cudaError_t e = split > 1 ? launch_pdl_cluster(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kThreads), L::kTotal, s, split, ta,
-                                                       tw, tw2, p, n_tiles, split)
-                                  : launch_pdl(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kThreads), L::kTotal, s, ta, tw, tw2, p,
-                                               n_tiles, split);
+  const cudaError_t e = split > 1 ? launch_pdl_cluster(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::kTotal, s, split,
+                                                       ta, tw, tw2, p, split, log_own)
+                                  : launch_pdl(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::kTotal, s, ta, tw, tw2, p,
+                                               split, log_own);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 template <bool GATED>
 cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
-  switch (gemm_i8_box(p.M, GATED)) {     // at most kNarrowTokens
+  switch (gemm_i8_box(p.M, p.N, p.K, GATED)) {
     case 16: return launch_narrow<16, GATED>(ta, tw, tw2, p, s);
     case 32: return launch_narrow<32, GATED>(ta, tw, tw2, p, s);
     case 64: return launch_narrow<64, GATED>(ta, tw, tw2, p, s);
-    case 128: return launch_narrow<128, GATED>(ta, tw, tw2, p, s);
-    default: return launch_narrow<256, GATED>(ta, tw, tw2, p, s);
+    default: return launch_narrow<128, GATED>(ta, tw, tw2, p, s);
   }
 }
 
@@ -384,10 +485,6 @@ __device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols) {
 __device__ __forceinline__ void tmem_dealloc_pair(uint32_t taddr, uint32_t cols) {
   asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(cols) : "memory");
 }
-__device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-  asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
-}
-
 // 32 consecutive results of one token per lane.
 template <bool GATED>
 __device__ __forceinline__ void results_of(const uint32_t (&r)[32], const uint32_t (&r2)[32], float as, const float* ws, const float* ws2,
@@ -706,7 +803,7 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
   const int kblocks = (p.K + kBK - 1) / kBK;
   int split = 1;
-  while (split < (GATED ? 2 : 4) && tiles * split * 2 <= kPairs && kblocks >= 8 * split) split *= 2;
+  while (split < (GATED ? 2 : 4) && tiles <= kClusters[0][2 * split] && kblocks >= 8 * split) split *= 2;
   const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
   const int bytes = p.type == kF32 ? 4 : 2;
   const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
@@ -721,22 +818,40 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 
-// Up to this many tokens are the columns of the narrow form.
-constexpr int kNarrowTokens = 256;
-
 }  // namespace
 
-int gemm_i8_box(int M, bool) { return M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : M <= kNarrowTokens ? 256 : 128; }
+namespace {
+enum class Form { kVector, kNarrow, kWide };
+// Which form. The vector form is bound by its dot products from about 2^26 products on (4 tokens x 1536 x 8960 6.4 us against 8.3
+// narrow, 8 tokens 8.2 and 8.4; gated 4 x 8960 x 1536 9.0 and 8.7, 8 x 18944 x 3584 40.7 and 26.0), except that one and two tokens
+// never are. Between 64 and 128 tokens the wide form wins where its tiles occupy half of the pairs (gated 128 x 8960 x 1536 12.6 us
+// against 14.4; 128 x 2048 x 1536 8.8 and 7.3).
+Form form_of(int M, int N, int K, bool gated) {
+  const int64_t weights = static_cast<int64_t>(N) * K * (gated ? 2 : 1);
+  if (M <= 2 || (M <= kVectorTokens && weights * (M <= 4 ? 4 : 8) <= 1 << 26)) return Form::kVector;
+  const int wide_tiles = N / (gated ? 128 : 256);
+  return M <= (wide_tiles > kNumSMs / 4 ? 64 : kNarrowTokens) ? Form::kNarrow : Form::kWide;
+}
+}  // namespace
+
+int gemm_i8_box(int M, int N, int K, bool gated) {
+  const Form f = form_of(M, N, K, gated);
+  return f == Form::kVector ? 0 : f == Form::kWide ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+}
 
 bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows) {
   return make_tensor_map_8b(tm, base, static_cast<uint64_t>(rows), static_cast<uint64_t>(k), static_cast<uint64_t>(stride),
                             static_cast<uint32_t>(box_rows), kBK);
 }
 
-cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap* tw2, const GemmI8& p, cudaStream_t s) {
+cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
   if (p.M <= 0) return cudaSuccess;
-  if (p.M > kNarrowTokens) return tw2 ? launch_wide<true>(ta, tw, *tw2, p, s) : launch_wide<false>(ta, tw, tw, p, s);
-  return tw2 ? launch_by_tokens<true>(ta, tw, *tw2, p, s) : launch_by_tokens<false>(ta, tw, tw, p, s);
+  const bool gated = p.w2 != nullptr;
+  switch (form_of(p.M, p.N, p.K, gated)) {
+    case Form::kVector: return gated ? launch_vector<true>(p, s) : launch_vector<false>(p, s);
+    case Form::kNarrow: return gated ? launch_by_tokens<true>(ta, tw, tw2, p, s) : launch_by_tokens<false>(ta, tw, tw, p, s);
+    default: return gated ? launch_wide<true>(ta, tw, tw2, p, s) : launch_wide<false>(ta, tw, tw, p, s);
+  }
 }
 
 cudaError_t i8_status(uint32_t* bits, cudaStream_t s) {

@@ -30,6 +30,8 @@ cudaError_t launch_dequantize_i8(const int8_t* codes, const float* scales, void*
                                  cudaStream_t s);
 
 struct GemmI8 {
+  const int8_t *a, *w, *w2;                          // [M, K] rows a_stride apart, [N, K], [N, K] (gated) or null
+  int64_t a_stride;
   const float *a_scales, *w_scales, *w2_scales;      // [M], [N], [N] (gated)
   const float* add;                                  // [M, >= N] or null
   void* out;                                         // [M, >= N] of `type` (kF32 only for ungated products, and with add)
@@ -40,10 +42,11 @@ struct GemmI8 {
 };
 // 2D map over [rows, k] codes, rows `stride` bytes apart: boxes of box_rows x 128 bytes, 128-byte swizzle.
 bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows);
-// Rows of a box of the activations' map for a product of M rows.
-int gemm_i8_box(int M, bool gated);
-// tw2 null: out = codes' product times both scales (+ add); else silu(first) * second. K a multiple of 16, at most kMaxI8K.
-cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap* tw2, const GemmI8& p, cudaStream_t s);
+// Rows of a box of the activations' map for such a product; 0: it takes no maps.
+int gemm_i8_box(int M, int N, int K, bool gated);
+// out = the codes' product times both scales (+ add), or silu(first) * second. K a multiple of 16, at most kMaxI8K. Maps: of a with
+// boxes of gemm_i8_box rows, of the weights with boxes of 128; tw2 is read for gated products only.
+cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s);
 // The time-out bits that launches without a status word of their own have left on this device, and clears them. Synchronises s.
 cudaError_t i8_status(uint32_t* bits, cudaStream_t s);
 

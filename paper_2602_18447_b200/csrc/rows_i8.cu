@@ -66,52 +66,71 @@ __device__ __forceinline__ Piece<TYPE> held(const float (&v)[8]) {
   return p;
 }
 
-// Eight codes. 1.5 * 2^23 added in the same rounding as the product leaves the nearest integer in the low bits of the sum. The
-// product y * inv is off the quotient by at most 127 * 2^-24, the rounding of inv, so a remainder that is not within 2^-16 of a half
-// decides the code. For the others the sign of 127 y - (c + 1/2) most is taken exactly: both products as a rounded part and its error.
-// (One value in thirty thousand, but in 16-bit rows half of the largest magnitude, a tie, is met in every few hundred.)
-__device__ __forceinline__ uint2 codes8(const float (&y)[8], float inv, float most) {
-  constexpr float kMagic = 12582912.0f, kNear = 0.5f - 0x1p-16f;
-  float t[8], rem[8], worst = 0.f;
+// Numbers a little above and below 127 / most.
+struct Inverse {
+  float up, down, most;
+};
+__device__ __forceinline__ Inverse inverse_of(float most) {
+  const uint32_t near = __float_as_uint(__fdividef(127.0f, most));      // off by two steps at most
+  return {__uint_as_float(near + 3), __uint_as_float(near - 3), most};
+}
+// Eight codes. 1.5 * 2^23 added in the same rounding as the product leaves the nearest integer in the low bits of the sum. Where the
+// two inverses give one integer, it is the quotient's. Else the half between the two is compared with the quotient exactly: the sign
+// of 127 y - half * most, both products as a rounded part and its error. (One value in twenty thousand; in 16-bit rows half of the
+// largest magnitude, a tie, is met in every few hundred.)
+__device__ __forceinline__ uint2 codes8(const float (&y)[8], const Inverse& by) {
+  constexpr float kMagic = 12582912.0f;
+  uint32_t b[8], differ = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    t[j] = fmaf(y[j], inv, kMagic);
-    rem[j] = fmaf(y[j], inv, -(t[j] - kMagic));
-    worst = fmaxf(worst, fabsf(rem[j]));
+    b[j] = __float_as_uint(fmaf(y[j], by.up, kMagic));
+    differ |= b[j] ^ __float_as_uint(fmaf(y[j], by.down, kMagic));
   }
-  if (worst > kNear) {
+  if (differ) {
+    uint32_t which = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float half = t[j] - kMagic + copysignf(0.5f, rem[j]);
-      const float p = __fmul_rn(127.0f, y[j]), q = __fmul_rn(half, most);
-      const float d = (p - q) + (fmaf(127.0f, y[j], -p) - fmaf(half, most, -q));
+    for (int j = 0; j < 8; ++j) which |= b[j] != __float_as_uint(fmaf(y[j], by.down, kMagic)) ? 1u << j : 0u;
+#pragma unroll 1
+    for (; which; which &= which - 1) {
+      const int at = __ffs(which) - 1;
+      float v = y[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) v = at == j ? y[j] : v;
+      const float half = 0.5f * ((fmaf(v, by.up, kMagic) - kMagic) + (fmaf(v, by.down, kMagic) - kMagic));
+      const float p = __fmul_rn(127.0f, v), q = __fmul_rn(half, by.most);
+      const float d = (p - q) + (fmaf(127.0f, v, -p) - fmaf(half, by.most, -q));
       const float c = d > 0.f ? half + 0.5f : d < 0.f ? half - 0.5f : rintf(half);
-      if (fabsf(rem[j]) > kNear) t[j] = c + kMagic;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = at == j ? __float_as_uint(c + kMagic) : b[j];
     }
   }
   uint2 r;
-  r.x = __byte_perm(__byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040),
-                    __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040), 0x5410);
-  r.y = __byte_perm(__byte_perm(__float_as_uint(t[4]), __float_as_uint(t[5]), 0x0040),
-                    __byte_perm(__float_as_uint(t[6]), __float_as_uint(t[7]), 0x0040), 0x5410);
+  r.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  r.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  return r;
+}
+// The larger of m and |v|; NaN if either is.
+__device__ __forceinline__ float larger(float m, float v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(v)));
   return r;
 }
 
 struct RowStats {
-  uint32_t most;     // bits of the largest magnitude: ordered as the magnitudes are, infinity and NaN above all numbers
+  float most;        // the largest magnitude, NaN where a value is
   float squares;
 };
 // Over the threads of a row, the same order every time.
 template <bool NORM>
 __device__ __forceinline__ RowStats row_stats(RowStats s, RowStats* shared) {
-  s.most = __reduce_max_sync(0xffffffffu, s.most);
+  s.most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(s.most)));       // ordered as the bits are, NaN above all
   if (NORM) s.squares = warp_sum(s.squares);
   const int warps = blockDim.x >> 5;
   if (warps == 1) return s;
   if ((threadIdx.x & 31) == 0) shared[threadIdx.x >> 5] = s;
   __syncthreads();
-  s = (threadIdx.x & 31) < warps ? shared[threadIdx.x & 31] : RowStats{0u, 0.f};
-  s.most = __reduce_max_sync(0xffffffffu, s.most);
+  s = (threadIdx.x & 31) < warps ? shared[threadIdx.x & 31] : RowStats{0.f, 0.f};
+  s.most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(s.most)));       // ordered as the bits are, NaN above all
   if (NORM) s.squares = warp_sum(s.squares);
   return s;
 }
@@ -120,7 +139,7 @@ __device__ __forceinline__ RowStats row_stats(RowStats s, RowStats* shared) {
 // thread holds NV pieces of eight values, as they came, between the row's statistics and its codes; a longer row is read again.
 // What counts is how many rows an SM has on their way: registers are kept to 32 a thread where the types allow it.
 template <int TYPE, int DELTA, bool NORM, int NV>
-__global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) quantize_i8_kernel(const QuantRows p) {
+__global__ void __launch_bounds__(NV == 4 ? 640 : 1024, NV == 4 && TYPE != kF32 ? 2 : 1) quantize_i8_kernel(const QuantRows p) {
   __shared__ RowStats shared[32];
   pdl_launch_dependents();
   pdl_wait();
@@ -132,7 +151,7 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
   void* x_out = DELTA < 0 ? nullptr : static_cast<uint8_t*>(p.x_out) + row * p.x_out_stride * kBytes;
   const int units = p.d >> 3;
 
-  RowStats s = {0u, 0.f};
+  RowStats s = {0.f, 0.f};
   const auto add = [&](int unit, Piece<TYPE> a, const Piece<(DELTA < 0 ? kF16 : DELTA)>& b) {
     if (DELTA < 0) return a;
     float v[8], w[8];
@@ -151,7 +170,13 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] *= g[j];
   };
+  uint32_t most2 = 0;       // 16-bit rows without gains: the magnitudes' bits, two at a time
   const auto look = [&](int unit, const Piece<TYPE>& a) {
+    if (!NORM && TYPE != kF32) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) most2 = __vmaxu2(most2, a.w[j] & 0x7fff7fffu);
+      return;
+    }
     float v[8];
     values<TYPE>(a, v);
     if (NORM) {
@@ -160,7 +185,7 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
     }
     gained(unit, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s.most = max(s.most, __float_as_uint(v[j]) & 0x7fffffffu);
+    for (int j = 0; j < 8; ++j) s.most = larger(s.most, v[j]);
   };
 
   Piece<TYPE> held_x[NV];
@@ -183,20 +208,25 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
   }
   for (int unit = threadIdx.x + NV * blockDim.x; unit < units; unit += blockDim.x)
     look(unit, add(unit, load_piece<TYPE>(x, unit), DELTA < 0 ? held_d[0] : load_piece<(DELTA < 0 ? kF16 : DELTA)>(delta, unit)));
+  if (!NORM && TYPE != kF32) {
+    const uint32_t m = max(most2 >> 16, most2 & 0xffffu);
+    s.most = TYPE == kF16 ? __half2float(__ushort_as_half(static_cast<uint16_t>(m))) : __uint_as_float(m << 16);
+  }
   s = row_stats<NORM>(s, shared);
 
-  const float most = __uint_as_float(s.most);
-  bool good = s.most < 0x7f800000u;
-  float scale = most / 127.0f;
-  if (NORM) {
-    good = good && s.squares < __uint_as_float(0x7f800000u);
-    scale = most > 0.f ? most / sqrtf(s.squares / static_cast<float>(p.d) + p.eps) / 127.0f : 0.f;
+  const float most = s.most;
+  bool good = most < __uint_as_float(0x7f800000u);
+  const float mean = NORM ? s.squares / static_cast<float>(p.d) + p.eps : 1.f;
+  if (NORM) good = good && mean < __uint_as_float(0x7f800000u) && (mean > 0.f || most == 0.f);
+  if (threadIdx.x == 0) {
+    float scale = most / 127.0f;
+    if (NORM && most > 0.f) scale = most / sqrtf(mean) / 127.0f;
+    p.scales[row] = good ? scale : __uint_as_float(0x7fffffffu);
   }
-  if (threadIdx.x == 0) p.scales[row] = good ? scale : __uint_as_float(0x7fffffffu);
   // Rows far from 1 are brought nearer, by a power of two, so that neither inv nor a product leaves the normal range; values that this
   // makes subnormal have codes of 0 either way.
   const float by = most < 0x1p-60f ? 0x1p90f : most > 0x1p100f ? 0x1p-60f : 1.0f;
-  const float top = most * by, inv = 127.0f / top;
+  const Inverse inverse = inverse_of(most * by);
   const bool any = good && most > 0.f;
   uint2* codes = reinterpret_cast<uint2*>(p.codes + row * p.d);
   const auto put = [&](int unit, const Piece<TYPE>& a) {
@@ -207,7 +237,7 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= by;
     }
-    codes[unit] = any ? codes8(v, inv, top) : make_uint2(0u, 0u);
+    codes[unit] = any ? codes8(v, inverse) : make_uint2(0u, 0u);
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -218,33 +248,46 @@ __global__ void __launch_bounds__(1024, TYPE == kF32 || NORM || NV > 2 ? 1 : 2) 
     put(unit, load_piece<TYPE>(DELTA < 0 ? x : x_out, unit));          // what this thread stored above
 }
 
+// A thread per 16 codes. A byte with its sign turned, put under the exponent of 2^23, is 2^23 + 128 + code.
 template <int TYPE>
-__global__ void dequantize_i8_kernel(const int8_t* __restrict__ codes, const float* __restrict__ scales, void* __restrict__ out,
-                                     int64_t out_stride, int rows, int d) {
+__global__ void __launch_bounds__(256) dequantize_i8_kernel(const int8_t* codes, const float* scales, void* out, int64_t out_stride,
+                                                            int rows, int d) {
   pdl_launch_dependents();
   pdl_wait();
   constexpr int kBytes = TYPE == kF32 ? 4 : 2;
-  const int64_t units = d >> 3, all = units * rows;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
-    const int64_t row = i / units;
-    const int unit = static_cast<int>(i - row * units);
-    const uint2 c = reinterpret_cast<const uint2*>(codes)[i];
-    const float s = scales[row];
-    float v[8];
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y;
+  if (row >= rows) return;
+  const float s = scales[row];
+  const uint4* from = reinterpret_cast<const uint4*>(codes + row * d);
+  void* to = static_cast<uint8_t*>(out) + row * out_stride * kBytes;
+  for (int unit = threadIdx.x + blockIdx.y * blockDim.x; unit < d >> 4; unit += blockDim.x * gridDim.y) {
+    const uint4 c = from[unit];
+    const uint32_t w[4] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u, c.z ^ 0x80808080u, c.w ^ 0x80808080u};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = s * static_cast<float>(static_cast<int8_t>((j < 4 ? c.x : c.y) >> (8 * (j & 3))));
-    store_piece<TYPE>(static_cast<uint8_t*>(out) + row * out_stride * kBytes, unit, held<TYPE>(v));
+    for (int h = 0; h < 2; ++h) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = s * (__uint_as_float(__byte_perm(w[2 * h + (j >> 2)], 0x4b000000u, 0x7540 + (j & 3))) - 8388736.0f);
+      store_piece<TYPE>(to, 2 * unit + h, held<TYPE>(v));
+    }
   }
 }
 
 template <int TYPE, int DELTA, bool NORM>
 cudaError_t launch_rows(const QuantRows& p, cudaStream_t s) {
+  // Pieces a thread. What a thread does once for a row costs as much as ten values, so many rows take four pieces where that leaves
+  // four warps to a row (8191 x 3584 bf16: 36.0 us, two pieces 39.1; 1163 x 1536 fp16: 3.7 and 3.2), fp32 rows two, whose registers
+  // are twice as many (2048 x 3584: 8.1 either way; norm of 5377 x 1536: 18.4 and 17.5). Few rows are bound by latency: two pieces,
+  // the norm, whose loads are three, one (16 x 1536: 2.0 us against 2.3 with two and 2.8 with four).
   const int units = p.d >> 3;
-  const int nv = (p.rows <= kNumSMs && units <= 1024) ? 1 : units <= 2048 ? 2 : 4;
-  const int threads = std::min(1024, (units + 32 * nv - 1) / (32 * nv) * 32), together = threads == 32 ? 8 : 1;
-  const auto kernel = nv == 1   ? quantize_i8_kernel<TYPE, DELTA, NORM, 1>
+  const bool few = p.rows <= kNumSMs;
+  int nv = units > (TYPE == kF32 ? 2048 : 256) && !few ? 4 : 2;
+  if (NORM && few && units <= 1024) nv = 1;
+  if (units > 2048) nv = 4;
+  const int threads = std::min(nv == 4 ? 640 : 1024, (units + 32 * nv - 1) / (32 * nv) * 32), together = threads == 32 ? 8 : 1;
+  const auto kernel = nv == 4   ? quantize_i8_kernel<TYPE, DELTA, NORM, 4>
                       : nv == 2 ? quantize_i8_kernel<TYPE, DELTA, NORM, 2>
-                                : quantize_i8_kernel<TYPE, DELTA, NORM, 4>;
+                                : quantize_i8_kernel<TYPE, DELTA, NORM, NORM ? 1 : 2>;
   const cudaError_t e = launch_pdl(kernel, dim3((p.rows + together - 1) / together), dim3(threads, together), 0, s, p);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
@@ -275,10 +318,11 @@ cudaError_t launch_quantize_i8(const QuantRows& p, cudaStream_t s) {
 cudaError_t launch_dequantize_i8(const int8_t* codes, const float* scales, void* out, int64_t out_stride, int rows, int d, int type,
                                  cudaStream_t s) {
   if (rows <= 0) return cudaSuccess;
-  const int64_t blocks = (static_cast<int64_t>(d >> 3) * rows + 255) / 256;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(blocks, kNumSMs * 8)));
+  const int units = d >> 4, across = std::min(256, (units + 31) / 32 * 32), down = 256 / across;
+  const int64_t blocks = (static_cast<int64_t>(rows) + down - 1) / down;
   const auto kernel = type == kF16 ? dequantize_i8_kernel<kF16> : type == kBF16 ? dequantize_i8_kernel<kBF16> : dequantize_i8_kernel<kF32>;
-  const cudaError_t e = launch_pdl(kernel, grid, dim3(256), 0, s, codes, scales, out, out_stride, rows, d);
+  const cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(blocks), std::min(64, (units + across - 1) / across)), dim3(across, down), 0,
+                                   s, codes, scales, out, out_stride, rows, d);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
