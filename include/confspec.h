@@ -108,6 +108,19 @@ int cs_model_set_lm_head_rows(cs_model* model, const int32_t* row_ids, int n_row
                               void* stream);
 
 /*
+ * cs_model_quantize_i8 - turn the layers' projections (query, key, value, output, gate, up, down) of a loaded model into 8-bit integers
+ * with one scale per output channel (see cs_quantize_i8) and free their fp16 matrices: half the projections' bytes, and passes whose
+ * projections run at the integer rate of the tensor cores. From then on every pass over the model (cs_verify_steps,
+ * cs_verify_cascade, cs_prefill, cs_append_accepted) takes each token's normed, attention and gated rows as 8-bit codes with a scale
+ * per token, multiplies codes exactly, and leaves projections in fp16; the residual stream stays fp32, the LM head, attention and
+ * caches as they are. Passes are deterministic whatever cs_set_deterministic says, and a step's projections do not depend on the rest
+ * of its batch. The rounding of weights and activations to 8 bits moves logits by more than the fp16 passes' 3e-2: choose tau anew.
+ * There is no way back but loading the model again. Synchronises the device. d_model and d_ffn have to be multiples of 16
+ * (CS_EINVAL); CS_ESTATE if it has been done; on CS_ENOMEM (room for the codes is needed next to the matrices) the model is as it was.
+ */
+int cs_model_quantize_i8(cs_model* model, void* stream);
+
+/*
  * cs_reserve — size the per-model activation workspace for batches of up to max_steps steps and
  * max_tokens new tokens in total. Optional: cs_verify_steps / cs_prefill grow the workspace on demand, but
  * growing synchronises the device, so latency-sensitive callers reserve once up front. What depends on the contexts is not
@@ -560,7 +573,7 @@ int cs_i8_status(void* stream);
  * of CUDA events around each kernel launch (on the call's stream); cs_profile_read waits for the recorded
  * events, adds the elapsed milliseconds and the number of timed launches per class into ms_out / calls_out
  * (host arrays of n_classes >= CS_PROF_CLASSES entries) and clears the record. Classes, in order: embedding,
- * RMSNorm, QKV GEMM (rotary turn in its epilogue), rotary (unused: always 0), attention, O GEMM, gate/up GEMM (SwiGLU),
+ * RMSNorm, QKV GEMM (rotary turn in its epilogue), rotary (only after cs_model_quantize_i8: else always 0), attention, O GEMM, gate/up GEMM (SwiGLU),
  * down GEMM, LM head, gate, other. The events keep consecutive kernels from overlapping and cost a little host and
  * device time, so throughput is measured with profiling off.
  */

@@ -15,7 +15,7 @@ CS_OK, CS_EINVAL, CS_ENOMEM, CS_ECUDA, CS_ETIMEOUT, CS_ESTATE, CS_ELIMIT, CS_ERA
 
 EXPORTED = [
     "cs_version", "cs_strerror", "cs_last_cuda_error", "cs_model_load", "cs_model_free", "cs_model_set_lm_head_rows",
-    "cs_reserve",
+    "cs_reserve", "cs_model_quantize_i8",
     "cs_kv_alloc", "cs_kv_alloc_8bit", "cs_kv_alloc_4bit", "cs_plan_create", "cs_plan_set", "cs_plan_free", "cs_kv_commit",
     "cs_kv_append", "cs_attention_4bit", "cs_kv_read", "cs_kv_free", "cs_kv_pool_bytes", "cs_kv_set_seq", "cs_kv_fill", "cs_prefill",
     "cs_verify_steps", "cs_verify_cascade", "cs_append_accepted", "cs_escalate_mask", "cs_cascade_select", "cs_set_keep_logits", "cs_set_deterministic", "cs_get_last_logits", "cs_get_last_lse",
@@ -70,6 +70,7 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
         "cs_model_free": (C.c_int, [vp]),
         "cs_model_set_lm_head_rows": (C.c_int, [vp, vp, i32, vp, vp]),
         "cs_reserve": (C.c_int, [vp, i32, i32]),
+        "cs_model_quantize_i8": (C.c_int, [vp, vp]),
         "cs_kv_alloc": (C.c_int, [vp, i32, i32, i32, i32, vp, C.POINTER(vp)]),
         "cs_kv_alloc_8bit": (C.c_int, [vp, i32, i32, i32, i32, i32, C.POINTER(vp)]),
         "cs_kv_alloc_4bit": (C.c_int, [vp, i32, i32, i32, i32, C.POINTER(vp)]),
@@ -235,6 +236,10 @@ def cs_model_set_lm_head_rows(model: int, row_ids, rows_bf16: np.ndarray, stream
 
 def cs_reserve(model: int, max_steps: int, max_tokens: int) -> None:
     _check(load_library().cs_reserve(model, max_steps, max_tokens), "cs_reserve")
+
+
+def cs_model_quantize_i8(model: int, stream=None) -> None:
+    _check(load_library().cs_model_quantize_i8(model, _stream_ptr(stream)), "cs_model_quantize_i8")
 
 
 def cs_kv_pool_bytes(model: int, num_pages: int, page_size: int = 16) -> int:
@@ -558,117 +563,113 @@ def cs_rmsnorm(x, gain, out, rows: int, d: int, eps: float, stream=None) -> None
 CS_F32 = 2
 
 _i8_types: dict = {}
+_ROWS, _F32, _I8 = (CS_F16, CS_BF16, CS_F32), (CS_F32,), (-1,)
 
 
-def _matrix(t, name, kinds, shape, contiguous=False):
-    """(device address, elements between rows, type code) of a CUDA matrix of one of the types `kinds`, on the current device,
-    whose rows are contiguous. `shape`: what it has to have."""
+def _i8_ready():
+    """The current device; the types' codes are looked up at the first call."""
     torch = _torch or _t()
     if not _i8_types:
         _i8_types.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16, torch.float32: CS_F32, torch.int8: -1})
+    return torch.cuda.current_device()
+
+
+def _whole(t, name, kinds, shape, dev):
+    """The address of a contiguous CUDA tensor of one of the types `kinds` and of this shape on the device `dev`."""
+    if _i8_types.get(t.dtype) not in kinds or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)} on the current device, "
+                         f"got {tuple(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+def _spread(t, name, kinds, shape, dev, step):
+    """(address, elements between rows, type) of such a matrix whose rows are contiguous but may lie apart; what a single row
+    is given as its stride is a row's length, in whole `step`s."""
     code = _i8_types.get(t.dtype)
-    if code is None or code not in kinds:
-        raise ValueError(f"{name}: type {t.dtype}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} has to be on the current device")
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)} where {tuple(shape)} is expected")
-    if contiguous or len(shape) == 1:
-        if not t.is_contiguous():
-            raise ValueError(f"{name} has to be contiguous")
-        return t.data_ptr(), shape[-1], code
+    if code not in kinds or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{name}: expected a matrix of shape {tuple(shape)} on the current device, got {tuple(t.shape)} of {t.dtype}")
     rows, cols = shape
-    if not rows:
-        return None, cols, code
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError(f"{name}: the values of a row have to be contiguous")
-    if rows == 1:
-        return t.data_ptr(), -1, code        # the stride of one row says nothing
-    if t.stride(0) < cols:
-        raise ValueError(f"{name}: its rows overlap")
-    return t.data_ptr(), t.stride(0), code
-
-
-_ROWS = (CS_F16, CS_BF16, CS_F32)
-
-
-def _one_row(stride: int, cols: int, step: int) -> int:
-    """A stride that a single row of `cols` values may have."""
-    return (cols + step - 1) // step * step if stride < 0 else stride
+    if rows <= 1:
+        if rows and cols > 1 and t.stride()[1] != 1:
+            raise ValueError(f"{name}: the values of a row have to be contiguous")
+        return (t.data_ptr() if rows else None), (cols + step - 1) // step * step, code
+    apart, along = t.stride()
+    if apart < cols or (cols > 1 and along != 1):
+        raise ValueError(f"{name}: the values of a row have to be contiguous, and rows must not overlap")
+    return t.data_ptr(), apart, code
 
 
 def _rows_2d(t, name):
-    if t.dim() != 2:
+    shape = tuple(t.shape)
+    if len(shape) != 2:
         raise ValueError(f"{name} is a matrix of rows")
-    return t.shape
+    return shape
+
+
+def _stream_on(dev, stream):
+    """The handle of the stream, the current one of the device where none is given."""
+    return _torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream_ptr(stream)
 
 
 def cs_quantize_i8(x, codes, scales, stream=None) -> None:
     """x: CUDA rows [M, d] (float16, bfloat16 or float32; the rows may lie apart); codes: contiguous int8 [M, d]; scales:
     float32 [M]."""
-    shape = _rows_2d(x, "x")
-    xp, xs, kind = _matrix(x, "x", _ROWS, shape)
-    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
-    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
-    _check(load_library().cs_quantize_i8(xp, _one_row(xs, shape[1], 8), kind, cp, sp, shape[0], shape[1], _stream_ptr(stream)),
+    dev, shape = _i8_ready(), _rows_2d(x, "x")
+    xp, xs, kind = _spread(x, "x", _ROWS, shape, dev, 8)
+    _check((_lib or load_library()).cs_quantize_i8(xp, xs, kind, _whole(codes, "codes", _I8, shape, dev),
+                                         _whole(scales, "scales", _F32, shape[:1], dev), shape[0], shape[1], _stream_on(dev, stream)),
            "cs_quantize_i8")
 
 
 def cs_dequantize_i8(codes, scales, out, stream=None) -> None:
     """codes: contiguous CUDA int8 [M, d]; scales: float32 [M]; out: rows [M, d] (float16, bfloat16 or float32)."""
-    shape = _rows_2d(codes, "codes")
-    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
-    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
-    op, os_, kind = _matrix(out, "out", _ROWS, shape)
-    _check(load_library().cs_dequantize_i8(cp, sp, shape[0], shape[1], op, _one_row(os_, shape[1], 8), kind, _stream_ptr(stream)),
-           "cs_dequantize_i8")
+    dev, shape = _i8_ready(), _rows_2d(codes, "codes")
+    op, os_, kind = _spread(out, "out", _ROWS, shape, dev, 8)
+    _check((_lib or load_library()).cs_dequantize_i8(_whole(codes, "codes", _I8, shape, dev), _whole(scales, "scales", _F32, shape[:1], dev),
+                                           shape[0], shape[1], op, os_, kind, _stream_on(dev, stream)), "cs_dequantize_i8")
 
 
 def cs_rmsnorm_i8(x, gain, codes, scales, eps: float, delta=None, x_out=None, stream=None) -> None:
     """x: CUDA rows [M, d] (float16, bfloat16 or float32); gain: float32 [d]; codes: contiguous int8 [M, d]; scales: float32 [M].
     delta: rows added to x first (of the type of x, or of any of the three for float32 x), x_out: rows of the type of x that
     receive the sum (x itself where it is not given)."""
-    shape = _rows_2d(x, "x")
-    xp, xs, kind = _matrix(x, "x", _ROWS, shape)
-    gp, _, _ = _matrix(gain, "gain", (CS_F32,), shape[1:])
-    cp, _, _ = _matrix(codes, "codes", (-1,), shape, True)
-    sp, _, _ = _matrix(scales, "scales", (CS_F32,), shape[:1])
+    dev, shape = _i8_ready(), _rows_2d(x, "x")
+    xp, xs, kind = _spread(x, "x", _ROWS, shape, dev, 8)
     dp, ds, dkind, op, os_ = None, 0, kind, None, 0
     if delta is not None:
-        dp, ds, dkind = _matrix(delta, "delta", _ROWS if kind == CS_F32 else (kind,), shape)
-        op, os_, _ = _matrix(x if x_out is None else x_out, "x_out", (kind,), shape)
+        dp, ds, dkind = _spread(delta, "delta", _ROWS if kind == CS_F32 else (kind,), shape, dev, 8)
+        op, os_ = (xp, xs) if x_out is None else _spread(x_out, "x_out", (kind,), shape, dev, 8)[:2]
     elif x_out is not None:
         raise ValueError("x_out comes with delta")
-    step = 8
-    _check(load_library().cs_rmsnorm_i8(xp, _one_row(xs, shape[1], step), kind, dp, _one_row(ds, shape[1], step), dkind, op,
-                                        _one_row(os_, shape[1], step), gp, cp, sp, shape[0], shape[1], float(eps),
-                                        _stream_ptr(stream)), "cs_rmsnorm_i8")
+    _check((_lib or load_library()).cs_rmsnorm_i8(xp, xs, kind, dp, ds, dkind, op, os_, _whole(gain, "gain", _F32, shape[1:], dev),
+                                        _whole(codes, "codes", _I8, shape, dev), _whole(scales, "scales", _F32, shape[:1], dev),
+                                        shape[0], shape[1], float(eps), _stream_on(dev, stream)), "cs_rmsnorm_i8")
 
 
 def cs_gemm_i8(a, a_scales, w, w_scales, out, w2=None, w2_scales=None, add=None, stream=None) -> None:
     """a: CUDA int8 codes [M, K] (rows may lie apart by a multiple of 16); w, w2: contiguous int8 codes [N, K]; scales: float32 [M],
     [N], [N]; out: rows [M, N]. out = y (any of the three row types), add + y (add, out: float32 rows; out may be add) or
     silu(y) * y2 (float16 or bfloat16)."""
-    (m, k), n = _rows_2d(a, "a"), _rows_2d(w, "w")[0]
-    ap, as_, _ = _matrix(a, "a", (-1,), (m, k))
-    wp, _, _ = _matrix(w, "w", (-1,), (n, k), True)
-    asp, _, _ = _matrix(a_scales, "a_scales", (CS_F32,), (m,))
-    wsp, _, _ = _matrix(w_scales, "w_scales", (CS_F32,), (n,))
+    dev, (m, k), n = _i8_ready(), _rows_2d(a, "a"), _rows_2d(w, "w")[0]
+    ap, as_, _ = _spread(a, "a", _I8, (m, k), dev, 16)
     w2p = w2sp = dp = None
-    ds = 0
+    ds, kinds = 0, _ROWS
     if w2 is not None:
-        w2p, _, _ = _matrix(w2, "w2", (-1,), (n, k), True)
-        w2sp, _, _ = _matrix(w2_scales, "w2_scales", (CS_F32,), (n,))
         if add is not None:
             raise ValueError("add goes with a single matrix")
+        if w2_scales is None:
+            raise ValueError("w2 comes with w2_scales")
+        kinds = _ROWS[:2]
+        w2p, w2sp = _whole(w2, "w2", _I8, (n, k), dev), _whole(w2_scales, "w2_scales", _F32, (n,), dev)
     elif w2_scales is not None:
         raise ValueError("w2_scales come with w2")
     if add is not None:
-        dp, ds, _ = _matrix(add, "add", (CS_F32,), (m, n))
-    kinds = (CS_F32,) if add is not None else _ROWS[:2] if w2 is not None else _ROWS
-    op, os_, kind = _matrix(out, "out", kinds, (m, n))
-    _check(load_library().cs_gemm_i8(ap, _one_row(as_, k, 16), asp, wp, wsp, w2p, w2sp, dp, _one_row(ds, n, 1), op,
-                                     _one_row(os_, n, 1), m, n, k, kind, _stream_ptr(stream)), "cs_gemm_i8")
+        kinds = _F32
+        dp, ds, _ = _spread(add, "add", _F32, (m, n), dev, 1)
+    op, os_, kind = _spread(out, "out", kinds, (m, n), dev, 1)
+    _check((_lib or load_library()).cs_gemm_i8(ap, as_, _whole(a_scales, "a_scales", _F32, (m,), dev), _whole(w, "w", _I8, (n, k), dev),
+                                     _whole(w_scales, "w_scales", _F32, (n,), dev), w2p, w2sp, dp, ds, op, os_, m, n, k, kind,
+                                     _stream_on(dev, stream)), "cs_gemm_i8")
 
 
 def cs_i8_status(stream=None) -> None:

@@ -50,6 +50,12 @@ struct LayerDev {
   float *norm1, *norm2;
   float* qk_gain = nullptr;   // [2 * head_dim]: query gains then key gains; null when the family has no such norm
   CUtensorMap tm_wqkv, tm_wo, tm_wg, tm_wu, tm_wd;
+  // after cs_model_quantize_i8, in place of the five matrices (which are null then): codes and one scale per output channel
+  struct I8 {
+    int8_t* codes = nullptr;
+    float* scales = nullptr;
+    CUtensorMap tm;
+  } qkv8, o8, g8, u8, d8;
 };
 
 // A workspace buffer. Behind its `cap` usable bytes lie kCanaryBytes of a fixed pattern that nothing may write: a
@@ -126,9 +132,11 @@ struct cs_model {
   double* inv_freq = nullptr;
   std::vector<LayerDev> layers;
   std::vector<void*> owned;
+  bool i8 = false;              // the layers' projections are products of 8-bit codes
   CUtensorMap tm_lm;
   // workspace
   DevBuf x, x_last, a, qkv, attn_o, hmlp, rope, h_last, lm_part, vlogits, logits, lse, attn_part_o, attn_part_ml, attn_counters;
+  DevBuf codes, row_scales;     // 8-bit projections: the rows that the next product reads
   DevBuf expanded;              // a 4-bit cache's pages of one layer in the 16-bit layout, for steps of many query rows
   uint32_t* status = nullptr;
   // fixed order of the residual projections' additions (bit-identical passes); see TurnOrder
@@ -642,6 +650,82 @@ bool make_expanded_map(CUtensorMap* tm, const cs_model* m, void* pool, int n_pag
   return make_kv_group_map(tm, pool, 2ull * std::max(1, n_pages) * m->d.n_kv_heads * kPageSize, m->d.head_dim, kPageSize / 8);
 }
 
+// The projections of a model after cs_model_quantize_i8: T rows that are normed or quantised into the model's one buffer of codes,
+// then multiplied. What a residual projection computes is left in fp16 (`delta`) and added by the next norm.
+struct I8Pass {
+  cs_model* m;
+  int T;
+  cudaStream_t s;
+  // Maps of the code buffer for products of this pass: they differ by the length of a row and by the product's form.
+  struct Map { int rows = 0, k = 0, box = 0; CUtensorMap tm; } maps[8];
+  int n_maps = 0;
+
+  cudaError_t norm(float* x, const uint16_t* delta, const float* gain, int rows) {
+    QuantRows q = rows_of(x, kF32, m->d.d_model, rows);
+    q.delta = delta;
+    q.delta_type = kF16;
+    q.delta_stride = m->d.d_model;
+    q.x_out = delta ? x : nullptr;
+    q.x_out_stride = m->d.d_model;
+    q.gain = gain;
+    q.eps = m->d.rms_eps;
+    return launch_quantize_i8(q, s);
+  }
+  cudaError_t quantize(const uint16_t* rows16, int d, int rows) { return launch_quantize_i8(rows_of(rows16, kF16, d, rows), s); }
+  // out [rows, N] = the codes times w (gated: w2 as well), in fp16, or added to fp32 x.
+  cudaError_t product(const LayerDev::I8& w, const LayerDev::I8* w2, uint16_t* out, float* x, int rows, int N, int K) {
+    const CUtensorMap* ta = map_of(rows, K, gemm_i8_box(rows, N, K, w2 != nullptr));
+    if (!ta) return cudaErrorInvalidValue;
+    GemmI8 g = {};
+    g.a = static_cast<const int8_t*>(m->codes.p);
+    g.a_stride = K;
+    g.a_scales = static_cast<const float*>(m->row_scales.p);
+    g.w = w.codes;
+    g.w_scales = w.scales;
+    if (w2) {
+      g.w2 = w2->codes;
+      g.w2_scales = w2->scales;
+    }
+    g.add = x;
+    g.out = x ? static_cast<void*>(x) : out;
+    g.add_stride = g.out_stride = N;
+    g.M = rows;
+    g.N = N;
+    g.K = K;
+    g.type = x ? kF32 : kF16;
+    g.weights_settled = 1;
+    g.status = m->status;
+    return gemm_i8(*ta, w.tm, w2 ? w2->tm : w.tm, g, s);
+  }
+
+ private:
+  QuantRows rows_of(const void* x, int type, int d, int rows) const {
+    QuantRows q = {};
+    q.x = x;
+    q.x_stride = d;
+    q.type = type;
+    q.codes = static_cast<int8_t*>(m->codes.p);
+    q.scales = static_cast<float*>(m->row_scales.p);
+    q.rows = rows;
+    q.d = d;
+    return q;
+  }
+  const CUtensorMap* map_of(int rows, int k, int box) {
+    for (int i = 0; i < n_maps; ++i)
+      if (maps[i].rows == rows && maps[i].k == k && maps[i].box == box) return &maps[i].tm;
+    if (n_maps == 8) n_maps = 0;
+    Map& e = maps[n_maps++];
+    e.rows = rows;
+    e.k = k;
+    e.box = box;
+    if (box && !make_i8_map(&e.tm, static_cast<const int8_t*>(m->codes.p), rows, k, k, box)) {
+      --n_maps;
+      return nullptr;
+    }
+    return &e.tm;
+  }
+};
+
 // The forward over all layers for a staged batch. When `append_kv` is given the new K/V of every layer are
 // also written to that cache's pages.
 int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout& L, const int32_t* dev_meta,
@@ -696,6 +780,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
   ap.n_rows = T;
   const int plane_groups = kv->num_pages * d.n_kv_heads * kPageSize / 8;
 
+  I8Pass i8{m, T, s};
   TurnOrder turn_order{m->turn_flags, &m->turn_epoch};
   const TurnOrder* turn = m->deterministic ? &turn_order : nullptr;
   RopeEpilogue rope_epi{rope, d.head_dim / 2, (d.n_q_heads + d.n_kv_heads) * d.head_dim};
@@ -704,9 +789,15 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
   for (int l = 0; l < d.n_layers; ++l) {
     const LayerDev& lw = m->layers[l];
     rope_epi.qk_gain = lw.qk_gain;
-    CS_STEP(kProfNorm, launch_rmsnorm(x, lw.norm1, a, T, d.d_model, d.rms_eps, s));
-    // q and k heads leave the projection already rotated (the turn is applied to the fp32 accumulators)
-    CS_STEP(kProfQkv, gemm_f16_rope(tm_a, lw.tm_wqkv, qkv, T, m->n_qkv, d.d_model, rope_epi, m->status, s));
+    if (m->i8) {
+      CS_STEP(kProfNorm, i8.norm(x, l ? a : nullptr, lw.norm1, T));
+      CS_STEP(kProfQkv, i8.product(lw.qkv8, nullptr, qkv, nullptr, T, m->n_qkv, d.d_model));
+      CS_STEP(kProfRope, launch_rope_rows(qkv, m->n_qkv, T, rope_epi, s));
+    } else {
+      CS_STEP(kProfNorm, launch_rmsnorm(x, lw.norm1, a, T, d.d_model, d.rms_eps, s));
+      // q and k heads leave the projection already rotated (the turn is applied to the fp32 accumulators)
+      CS_STEP(kProfQkv, gemm_f16_rope(tm_a, lw.tm_wqkv, qkv, T, m->n_qkv, d.d_model, rope_epi, m->status, s));
+    }
     ap.k_group_base = (2 * l) * plane_groups;
     ap.v_group_base = (2 * l + 1) * plane_groups;
     const auto append = [&]() -> cudaError_t {
@@ -784,6 +875,26 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
       CS_STEP(kProfAttn, launch_attention(ap, kv->tm_pool, tm_qkv_attn, tm_q3d, d_items, L.n_items, s));
     }
     if (append_kv) CS_STEP(kProfOther, append());
+    if (m->i8) {
+      const bool last = l == d.n_layers - 1;           // of a verification: as below, the MLP of the steps' last rows alone
+      CS_STEP(kProfOther, i8.quantize(attn_o, m->q_dim, T));
+      CS_STEP(kProfO, i8.product(lw.o8, nullptr, a, last ? x : nullptr, T, d.d_model, m->q_dim));
+      if (last) {
+        float* xl = static_cast<float*>(m->x_last.p);
+        CS_STEP(kProfOther, launch_gather_last_rows(x, dev_meta + L.off_cu, xl, L.B, d.d_model, s));
+        CS_STEP(kProfOther, i8.norm(xl, nullptr, lw.norm2, L.B));
+        CS_STEP(kProfOther, i8.product(lw.g8, &lw.u8, hmlp, nullptr, L.B, d.d_ffn, d.d_model));
+        CS_STEP(kProfOther, i8.quantize(hmlp, d.d_ffn, L.B));
+        CS_STEP(kProfOther, i8.product(lw.d8, nullptr, nullptr, xl, L.B, d.d_model, d.d_ffn));
+        m->last_rows_compact = true;
+        break;
+      }
+      CS_STEP(kProfNorm, i8.norm(x, a, lw.norm2, T));
+      CS_STEP(kProfGateUp, i8.product(lw.g8, &lw.u8, hmlp, nullptr, T, d.d_ffn, d.d_model));
+      CS_STEP(kProfOther, i8.quantize(hmlp, d.d_ffn, T));
+      CS_STEP(kProfDown, i8.product(lw.d8, nullptr, a, nullptr, T, d.d_model, d.d_ffn));
+      continue;
+    }
     CS_STEP(kProfO, gemm_f16(tm_o, lw.tm_wo, nullptr, x, T, d.d_model, m->q_dim, kEpiResidAdd, m->status, s, turn));
     if (l == d.n_layers - 1 && !append_kv) {
       // Only each step's last position feeds the LM head, and after the last attention no row depends on another:
@@ -829,6 +940,10 @@ int ensure_workspace(cs_model* m, int B, int T) {
   if ((rc = m->vlogits.ensure(bp * 8 * 4))) return rc;
   if ((rc = m->lse.ensure(bp * 4))) return rc;
   if (m->keep_logits && (rc = m->logits.ensure(static_cast<size_t>(B) * d.vocab * 4))) return rc;
+  if (m->i8) {
+    if ((rc = m->codes.ensure(t * std::max(d.d_model, std::max(m->q_dim, d.d_ffn))))) return rc;
+    if ((rc = m->row_scales.ensure(t * sizeof(float)))) return rc;
+  }
   return CS_OK;
 }
 
@@ -1103,7 +1218,7 @@ int cs_model_free(cs_model* m) {
   for (void* p : m->owned) cudaFree(p);
   DevBuf* bufs[] = {&m->x, &m->x_last, &m->a, &m->qkv, &m->attn_o, &m->hmlp, &m->rope, &m->h_last, &m->lm_part, &m->vlogits,
                     &m->logits, &m->lse, &m->attn_part_o, &m->attn_part_ml, &m->attn_counters, &m->stg.dev,
-                    &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded};
+                    &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded, &m->codes, &m->row_scales};
   for (DevBuf* b : bufs) b->release();
   if (m->casc_host) cudaFreeHost(m->casc_host);
   for (cudaEvent_t e : m->prof.pool) cudaEventDestroy(e);
@@ -1130,6 +1245,79 @@ int cs_model_set_lm_head_rows(cs_model* m, const int32_t* row_ids, int n_rows, c
   }
   CS_CUDA(cudaStreamSynchronize(s));            // the host rows may be released on return
   return CS_OK;
+}
+
+// The rows of a matrix as codes, in memory of their own.
+static int to_codes(const uint16_t* w, int rows, int d, LayerDev::I8* out, std::vector<void*>* held, cudaStream_t s) {
+  void *codes = nullptr, *scales = nullptr;
+  CS_CUDA(cudaMalloc(&codes, static_cast<size_t>(rows) * d));
+  held->push_back(codes);
+  CS_CUDA(cudaMalloc(&scales, static_cast<size_t>(rows) * sizeof(float)));
+  held->push_back(scales);
+  out->codes = static_cast<int8_t*>(codes);
+  out->scales = static_cast<float*>(scales);
+  QuantRows q = {};
+  q.x = w;
+  q.x_stride = d;
+  q.type = kF16;
+  q.codes = out->codes;
+  q.scales = out->scales;
+  q.rows = rows;
+  q.d = d;
+  CS_CUDA(launch_quantize_i8(q, s));
+  if (!make_i8_map(&out->tm, out->codes, rows, d, d, 128)) {
+    g_cuda_error = "cuTensorMapEncodeTiled failed for a weight matrix's codes";
+    return CS_ECUDA;
+  }
+  return CS_OK;
+}
+
+static int quantize_layer(cs_model* m, LayerDev* lw, std::vector<void*>* held, cudaStream_t s) {
+  const cs_model_desc& d = m->d;
+  int rc;
+  if ((rc = to_codes(lw->wqkv, m->n_qkv, d.d_model, &lw->qkv8, held, s))) return rc;
+  if ((rc = to_codes(lw->wo, d.d_model, m->q_dim, &lw->o8, held, s))) return rc;
+  if ((rc = to_codes(lw->wg, d.d_ffn, d.d_model, &lw->g8, held, s))) return rc;
+  if ((rc = to_codes(lw->wu, d.d_ffn, d.d_model, &lw->u8, held, s))) return rc;
+  return to_codes(lw->wd, d.d_model, d.d_ffn, &lw->d8, held, s);
+}
+
+int cs_model_quantize_i8(cs_model* m, void* stream) {
+  if (!m || m->d.d_model % 16 || m->d.d_ffn % 16 || std::max(m->q_dim, std::max(m->d.d_model, m->d.d_ffn)) > kMaxI8K) return CS_EINVAL;
+  if (m->i8) return CS_ESTATE;
+  return guarded([&]() -> int {
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    std::vector<LayerDev> layers = m->layers;
+    std::vector<void*> held, kept;
+    std::vector<const void*> gone;
+    held.reserve(10 * layers.size());
+    gone.reserve(5 * layers.size());
+    kept.reserve(m->owned.size() + 10 * layers.size());
+    int rc = CS_OK;
+    for (LayerDev& lw : layers)
+      if ((rc = quantize_layer(m, &lw, &held, s))) break;
+    // everything that still reads the matrices has ended, and their codes are written, before anything is freed
+    const cudaError_t e = cudaDeviceSynchronize();
+    if (!rc && e != cudaSuccess) rc = cuda_fail(e, "quantising the projections");
+    if (rc) {
+      for (void* p : held) cudaFree(p);
+      return rc;
+    }
+    for (LayerDev& lw : layers) {
+      gone.insert(gone.end(), {lw.wqkv, lw.wo, lw.wg, lw.wu, lw.wd});
+      lw.wqkv = lw.wo = lw.wg = lw.wu = lw.wd = nullptr;
+    }
+    std::sort(gone.begin(), gone.end());
+    for (void* p : m->owned) {
+      if (std::binary_search(gone.begin(), gone.end(), static_cast<const void*>(p))) cudaFree(p);
+      else kept.push_back(p);
+    }
+    kept.insert(kept.end(), held.begin(), held.end());
+    m->owned.swap(kept);
+    m->layers.swap(layers);
+    m->i8 = true;
+    return CS_OK;
+  });
 }
 
 int cs_reserve(cs_model* m, int max_steps, int max_tokens) {
@@ -2022,7 +2210,7 @@ int cs_check_workspace(cs_model* m, void* stream) {
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const DevBuf* bufs[] = {&m->x, &m->x_last, &m->a, &m->qkv, &m->attn_o, &m->hmlp, &m->rope, &m->h_last, &m->lm_part,
                           &m->vlogits, &m->logits, &m->lse, &m->attn_part_o, &m->attn_part_ml, &m->attn_counters,
-                          &m->stg.dev, &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded};
+                          &m->stg.dev, &m->casc_idx, &m->casc_conf, &m->casc_verdict, &m->casc_accept, &m->expanded, &m->codes, &m->row_scales};
   for (const DevBuf* b : bufs) {
     const int st = b->canary_state(s);
     if (st < 0) return cuda_fail(cudaGetLastError(), "workspace canary read-back");

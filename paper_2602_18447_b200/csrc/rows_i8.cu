@@ -1,4 +1,5 @@
-// Rows to 8-bit codes with one scale each, the RMS norm in front of them, and codes back to values.
+// Rows to 8-bit codes with one scale each, the RMS norm in front of them, codes back to values, and the rotary turn of rows that a
+// product of codes has left.
 //
 // A row y has A = max |y|, the scale A / 127 and the codes rint(127 y / A), ties to even, of the quotient as a real number. The
 // norm's row is y = x g / rms(x): its factor 1 / rms is common to y and A, so that it drops out of the codes; they are taken from
@@ -10,6 +11,7 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "gemm.h"
 #include "kernels.h"
 
 namespace cs {
@@ -273,6 +275,45 @@ __global__ void __launch_bounds__(256) dequantize_i8_kernel(const int8_t* codes,
   }
 }
 
+// Rotary turn of projected rows in place, behind the 8-bit projection: a warp per (token, head), HALF / 32 pairs a lane. Memory
+// from L2, where the projection has left it.
+template <int HALF>
+__global__ void __launch_bounds__(256) rope_rows_kernel(__half* rows, int row_elems, int T, const RopeEpilogue rope) {
+  pdl_launch_dependents();
+  pdl_wait();
+  constexpr int kPairs = HALF / 32;
+  const int heads = rope.n_rot_cols / (2 * HALF), lane = threadIdx.x & 31;
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const int t = static_cast<int>(i / heads), c = static_cast<int>(i - static_cast<int64_t>(t) * heads) * 2 * HALF;
+  if (t >= T) return;
+  __half* at = rows + static_cast<int64_t>(t) * row_elems + c + lane * kPairs;
+  const float2* table = rope.table + static_cast<int64_t>(t) * HALF + lane * kPairs;
+  float a[kPairs], b[kPairs];
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) {
+    a[j] = __half2float(at[j]);
+    b[j] = __half2float(at[HALF + j]);
+  }
+  if (rope.qk_gain) {
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
+    const float r = rsqrtf(warp_sum(ss) / (2.0f * HALF) + rope.eps);
+    const float* gain = rope.qk_gain + (c < rope.q_cols ? 0 : 2 * HALF) + lane * kPairs;
+#pragma unroll
+    for (int j = 0; j < kPairs; ++j) {
+      a[j] *= r * gain[j];
+      b[j] *= r * gain[HALF + j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kPairs; ++j) {
+    const float2 cs = table[j];
+    at[j] = __float2half_rn(a[j] * cs.x - b[j] * cs.y);
+    at[HALF + j] = __float2half_rn(b[j] * cs.x + a[j] * cs.y);
+  }
+}
+
 template <int TYPE, int DELTA, bool NORM>
 cudaError_t launch_rows(const QuantRows& p, cudaStream_t s) {
   // Pieces a thread. What a thread does once for a row costs as much as ten values, so many rows take four pieces where that leaves
@@ -323,6 +364,16 @@ cudaError_t launch_dequantize_i8(const int8_t* codes, const float* scales, void*
   const auto kernel = type == kF16 ? dequantize_i8_kernel<kF16> : type == kBF16 ? dequantize_i8_kernel<kBF16> : dequantize_i8_kernel<kF32>;
   const cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>(blocks), std::min(64, (units + across - 1) / across)), dim3(across, down), 0,
                                    s, codes, scales, out, out_stride, rows, d);
+  count_launch();
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+cudaError_t launch_rope_rows(uint16_t* rows, int row_elems, int T, const RopeEpilogue& rope, cudaStream_t s) {
+  if (T <= 0) return cudaSuccess;
+  if (!rope.table || (rope.half != 32 && rope.half != 64)) return cudaErrorInvalidValue;
+  const int64_t warps = static_cast<int64_t>(T) * (rope.n_rot_cols / (2 * rope.half));
+  const cudaError_t e = launch_pdl(rope.half == 64 ? rope_rows_kernel<64> : rope_rows_kernel<32>, dim3(static_cast<unsigned>((warps + 7) / 8)),
+                                   dim3(256), 0, s, reinterpret_cast<__half*>(rows), row_elems, T, rope);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

@@ -81,3 +81,49 @@ def codes_of(g, rows, d, limit=127):
     """Random codes and scales as quantised rows have them."""
     c = g.integers(-limit, limit + 1, size=(rows, d)).astype(np.int8)
     return c, np.exp(g.normal(size=rows) * 0.5 - 6.0).astype(np.float32)
+
+
+# ----------------------------------------------------------------------------------- the pass over 8-bit projections
+def as_held(y):
+    """Rows in 64 bits as their codes and scales stand for them."""
+    codes, most = quantise(y)
+    return codes * (most / 127.0)[:, None]
+
+
+def layer_weights(O):
+    """O.LayerWeights with its matrices as the library holds them after cs_model_quantize_i8: fp16 values, then codes."""
+    class Weights(O.LayerWeights):
+        def __init__(self, layer):
+            super().__init__(layer)
+            for name in ("wq", "wk", "wv", "wo", "wg", "wu", "wd"):
+                setattr(self, name, as_held(getattr(self, name).astype(np.float16).astype(np.float64)))
+    return Weights
+
+
+def decoder_layer(O, noise=None):
+    """O.decoder_layer_extend with rows quantised in front of each projection. noise: a generator, with which every value that the
+    library rounds to fp16 is off by up to half a step (2^-11 relative), at random."""
+    def off(y):
+        return y if noise is None else y * (1.0 + 2.0 ** -11 * noise.uniform(-1, 1, size=y.shape))
+
+    def layer(x, lw, shape, ctx_len, k_ctx, v_ctx):
+        n = x.shape[0]
+        hq, hkv, hd = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
+        if n == 0:
+            return x, np.zeros((0, hkv, hd)), np.zeros((0, hkv, hd))
+        pos = ctx_len + np.arange(n)
+
+        def normed(rows, gain):
+            return as_held(rows * gain) / np.sqrt((rows * rows).mean(-1, keepdims=True) + shape.rms_eps)
+
+        a = normed(x, lw.norm1)
+        q, k, v = (off(a @ w.T).reshape(n, h, hd) for w, h in ((lw.wq, hq), (lw.wk, hkv), (lw.wv, hkv)))
+        if lw.q_norm is not None:
+            q, k = O.rmsnorm(q, lw.q_norm, shape.rms_eps), O.rmsnorm(k, lw.k_norm, shape.rms_eps)
+        q, k = off(O.rope(q, pos, shape.rope_theta)), off(O.rope(k, pos, shape.rope_theta))
+        o = off(O.attention_extend(q, k_ctx, v_ctx, k, v).reshape(n, hq * hd))
+        x = x + off(as_held(o) @ lw.wo.T)
+        b = normed(x, lw.norm2)
+        h = off(O.silu(b @ lw.wg.T) * (b @ lw.wu.T))
+        return x + off(as_held(h) @ lw.wd.T), k, v
+    return layer

@@ -97,7 +97,8 @@ def calls(monkeypatch):
             return call
 
     monkeypatch.setattr(B, "load_library", lambda path=None: Library())
-    monkeypatch.setattr(B, "_stream_ptr", lambda stream: 0)
+    monkeypatch.setattr(B, "_stream_on", lambda dev, stream: 0)
+    monkeypatch.setattr(B, "_lib", None)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     return B, seen
 
@@ -143,7 +144,7 @@ def test_shapes_types_and_places(calls):
         lambda: B.cs_gemm_i8(a, _f32(8), w, sw, o), lambda: B.cs_gemm_i8(a, sa, _i8(8, 80), sw, o), lambda: B.cs_gemm_i8(a, sa, w, sa, o),
         lambda: B.cs_gemm_i8(a, sa, w, sw, Rows(3, 9)), lambda: B.cs_gemm_i8(a, sa, w, sw, _i8(3, 8)),
         lambda: B.cs_gemm_i8(a, sa, _i8(8, 64, strides=(128, 1)), sw, o), lambda: B.cs_gemm_i8(a, sa, w, sw, o, w2=_i8(9, 64), w2_scales=sw),
-        lambda: B.cs_gemm_i8(a, sa, w, sw, o, w2_scales=sw), lambda: B.cs_gemm_i8(a, sa, w, sw, _f32(3, 8), w2=w, w2_scales=sw),
+        lambda: B.cs_gemm_i8(a, sa, w, sw, o, w2_scales=sw), lambda: B.cs_gemm_i8(a, sa, w, sw, o, w2=w), lambda: B.cs_gemm_i8(a, sa, w, sw, _f32(3, 8), w2=w, w2_scales=sw),
         lambda: B.cs_gemm_i8(a, sa, w, sw, o, add=_f32(3, 8)), lambda: B.cs_gemm_i8(a, sa, w, sw, _f32(3, 8), add=o),
         lambda: B.cs_gemm_i8(a, sa, w, sw, _f32(3, 8), add=_f32(3, 8), w2=w, w2_scales=sw), lambda: B.cs_gemm_i8(a, sa, w, sw, Rows(3, 8, device=1)),
     ]
