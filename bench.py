@@ -279,7 +279,7 @@ def run_ours(args, cfg):
 
     weights = model_weights(cfg.model, cfg.seed)
     batch = make_batch(cfg, seed=replica_seed(cfg, rank))
-    ses = VerifySession(cfg, weights, batch, device=f"cuda:{local}")
+    ses = VerifySession(cfg, weights, batch, device=f"cuda:{local}", i8=args.projections == "i8")
     total, pages = page_assignment(cfg, batch.ctx_lens)
     if cfg.ctx_kv == "prefill":
         ses.alloc_cache(pages, total, batch.ctx_lens, room_for_prefill=True)
@@ -407,7 +407,8 @@ def run_ours(args, cfg):
     l_ms = per_launch_ms("lm_head")
     kernels["lm_head"] = {"ms_per_launch": l_ms, "gbs": counts["lm_head_bytes"] / (l_ms * 1e-3) / 1e9,
                           "frac_hbm": counts["lm_head_bytes"] / (l_ms * 1e-3) / 1e9 / hbm_peak}
-    back_to_back = projections_back_to_back(cfg, counts["T"], tensor_peak, tensor_peak_sus) if world == 1 else None
+    i8 = args.projections == "i8"
+    back_to_back = projections_back_to_back(cfg, counts["T"], tensor_peak, tensor_peak_sus) if world == 1 and not i8 else None
     prof_total = sum(v[0] for v in prof.values())
     shares = {k: (v[0] / prof_total if prof_total else 0.0) for k, v in prof.items()}
     all_gemm_flops = sum(counts[k] for k in ("gemm_qkv_flops", "gemm_o_flops", "gemm_gateup_flops", "gemm_down_flops"))
@@ -467,6 +468,11 @@ def run_ours(args, cfg):
                         "kernels_back_to_back: 40 launches of the same kernel and shape under one event pair",
         "time_shares": shares,
     }
+    if i8:       # another arithmetic: named as such, and the fp16 kernel's roofline entry does not apply
+        out["dtype"] = "i8 projections, f16 elsewhere"
+        out["config"]["projections"] = "i8"
+        out["roofline"].update(kernel="gemm_i8_wide_kernel<gated> (gate/up projection)", traffic=None,
+                               peak_kind=f"{peak_kind} bf16 burst; 8-bit integers have twice the nominal peak")
     if rank == 0 and world == 1 and not args.no_cpu_baseline:
         sample = list(range(min(6, batch.n_steps)))         # ~15 s of CPU work at the 1.5B shape
         t = oracle_sample_run(cfg, weights, batch, sample)
@@ -599,6 +605,8 @@ def main():
     ap.add_argument("--layers", type=int, default=None,
                     help="run a reduced-depth copy of the workload (for profiler captures of single kernels); "
                          "not a benchmark configuration")
+    ap.add_argument("--projections", default="f16", choices=["f16", "i8"],
+                    help="i8: the model's projections in 8-bit integers (cs_model_quantize_i8); results differ by their rounding")
     ap.add_argument("--cascade", default=None,
                     help="time the two-tier pass of this cascade workload instead (one GPU; with --layers the target "
                          "model runs at that depth)")

@@ -19,12 +19,6 @@ enum GemmEpilogue {
 // box = [box_rows, box_cols].
 bool make_tensor_map_16b(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows,
                          uint32_t box_cols, bool swizzle128, bool is_bf16);
-// The same over bytes, rows `stride` bytes apart (a multiple of 16), 128-byte swizzle.
-bool make_tensor_map_8b(CUtensorMap* tm, const void* base, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows,
-                        uint32_t box_cols);
-// 2D map for stores of row boxes of 2- or 4-byte values, rows `stride` values apart: box rows of 64 or 128 bytes, swizzled alike.
-bool make_tensor_map_rows(CUtensorMap* tm, void* base, uint64_t rows, uint64_t cols, uint64_t stride, int bytes, uint32_t box_rows,
-                          uint32_t box_cols);
 // 3D fp16 tensor map over a row-major [tokens, heads, head_dim] view (token stride = row_elems elements):
 // box = [box_tokens, box_heads, 64], 128-byte swizzle. Used to fetch a query tile whose rows are
 // (token, head-in-group) pairs.

@@ -14,7 +14,6 @@
 #include <algorithm>
 
 #include "common.cuh"
-#include "gemm.h"
 #include "kernels.h"
 
 namespace cs {
@@ -24,6 +23,27 @@ namespace {
 constexpr int kBK = 128;                    // codes (= bytes) of a k block: one 128-byte swizzled row
 constexpr int kTileBytes = 128 * kBK;       // 128 rows of it
 constexpr int kMaxSplit = 8;
+
+// 2D map over rows of `bytes`-byte values, `stride` values apart: boxes whose rows are 64 or 128 bytes, swizzled alike.
+bool make_map(CUtensorMap* tm, void* base, CUtensorMapDataType type, int bytes, int64_t rows, int64_t cols, int64_t stride, int box_rows,
+              int box_cols) {
+  using Encode = decltype(&cuTensorMapEncodeTiled);
+  static const Encode encode = []() -> Encode {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+                   q == cudaDriverEntryPointSuccess
+               ? reinterpret_cast<Encode>(p)
+               : nullptr;
+  }();
+  if (!encode) return false;
+  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
+  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride * bytes)};
+  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
+  return encode(tm, type, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                box_cols * bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 // Time-outs of launches that are given no status word.
 static __device__ uint32_t g_status;
@@ -810,7 +830,9 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
                       (!p.add || (reinterpret_cast<uintptr_t>(p.add) % 16 == 0 && p.add_stride % 4 == 0));
   const int out_way = !pieces ? kOutValues : p.add ? kOutPieces : kOutBoxes;
   CUtensorMap tm_out = ta;
-  if (out_way == kOutBoxes && !make_tensor_map_rows(&tm_out, p.out, p.M, p.N, p.out_stride, bytes, 32, 32)) return cudaErrorInvalidValue;
+  if (out_way == kOutBoxes && !make_map(&tm_out, p.out, bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
+                                        bytes, p.M, p.N, p.out_stride, 32, 32))
+    return cudaErrorInvalidValue;
   const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide::kTotal, s,
                                            2 * split, ta, tw, tw2, tm_out, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
                                            out_way);
@@ -840,8 +862,7 @@ int gemm_i8_box(int M, int N, int K, bool gated) {
 }
 
 bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows) {
-  return make_tensor_map_8b(tm, base, static_cast<uint64_t>(rows), static_cast<uint64_t>(k), static_cast<uint64_t>(stride),
-                            static_cast<uint32_t>(box_rows), kBK);
+  return make_map(tm, const_cast<int8_t*>(base), CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, stride, box_rows, kBK);
 }
 
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {

@@ -18,13 +18,15 @@ from . import binding as B
 class VerifySession:
     """One model, one paged context cache and one batch of steps resident on the GPU."""
 
-    def __init__(self, cfg, weights: dict, batch, device: str = "cuda:0"):
+    def __init__(self, cfg, weights: dict, batch, device: str = "cuda:0", i8: bool = False):
         self.cfg, self.batch = cfg, batch
         self.shape = cfg.model
         self.device = torch.device(device)
         torch.cuda.set_device(self.device)
         B.load_library()
         self.model = B.cs_model_load(self.shape, weights)
+        if i8:
+            B.cs_model_quantize_i8(self.model)
         self.kv = None
         self.n_steps = batch.n_steps
         self.seq_ids = np.arange(self.n_steps, dtype=np.int32)

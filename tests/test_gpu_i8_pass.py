@@ -7,7 +7,7 @@ import pytest
 
 import i8_common as I
 import parity_common as P
-from workloads import get_config, make_batch, model_weights, scaled_config
+from workloads import context_kv, get_config, make_batch, model_weights, page_assignment, scaled_config
 
 pytestmark = pytest.mark.gpu
 
@@ -25,19 +25,17 @@ def _f16(a):
 
 
 def _session(B, cfg, weights, batch):
-    """As P.build_session, quantised before anything has run on the model."""
-    from paper_2602_18447_b200 import runner
-    load = B.cs_model_load
-
-    def quantised(*args):
-        m = load(*args)
-        B.cs_model_quantize_i8(m)
-        return m
-    runner.B.cs_model_load = quantised
-    try:
-        return P.build_session(cfg, weights, batch)
-    finally:
-        runner.B.cs_model_load = load
+    """As P.build_session, over 8-bit projections from the first prefill on."""
+    from paper_2602_18447_b200 import VerifySession
+    ses = VerifySession(cfg, weights, batch, i8=True)
+    B.cs_set_keep_logits(ses.model, True)
+    total, pages = page_assignment(cfg, batch.ctx_lens)
+    ses.alloc_cache(pages, total, batch.ctx_lens, room_for_prefill=cfg.ctx_kv == "prefill")
+    if cfg.ctx_kv == "prefill":
+        ses.prefill_context(batch.ctx_tokens)
+    else:
+        ses.fill_synthetic_context(lambda i, l: context_kv(cfg, i, l, int(batch.ctx_lens[i])))
+    return ses
 
 
 @pytest.mark.parametrize("name,batch", [("cfg1_tiny", 1), ("cfg1_tiny", 7), ("cfg1_tiny", 40), ("cfg8_tiny_qknorm", 11), ("cfg2", 5), ("cfg2", 150)])
