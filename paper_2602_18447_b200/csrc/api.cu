@@ -54,7 +54,7 @@ struct LayerDev {
   struct I8 {
     int8_t* codes = nullptr;
     float* scales = nullptr;
-    CUtensorMap tm;
+    CUtensorMap tm, tm_deep;       // boxes of one and, where the rows allow it, of two pieces of a row (I8Box)
   } qkv8, o8, g8, u8, d8;
 };
 
@@ -657,7 +657,7 @@ struct I8Pass {
   int T;
   cudaStream_t s;
   // Maps of the code buffer for products of this pass: they differ by the length of a row and by the product's form.
-  struct Map { int rows = 0, k = 0, box = 0; CUtensorMap tm; } maps[8];
+  struct Map { int rows = 0, k = 0; I8Box box = {0, false}; CUtensorMap tm; } maps[8];
   int n_maps = 0;
 
   cudaError_t norm(float* x, const uint16_t* delta, const float* gain, int rows) {
@@ -674,7 +674,8 @@ struct I8Pass {
   cudaError_t quantize(const uint16_t* rows16, int d, int rows) { return launch_quantize_i8(rows_of(rows16, kF16, d, rows), s); }
   // out [rows, N] = the codes times w (gated: w2 as well), in fp16, or added to fp32 x.
   cudaError_t product(const LayerDev::I8& w, const LayerDev::I8* w2, uint16_t* out, float* x, int rows, int N, int K) {
-    const CUtensorMap* ta = map_of(rows, K, gemm_i8_box(rows, N, K, w2 != nullptr));
+    const I8Box box = gemm_i8_box(rows, N, K, w2 != nullptr);
+    const CUtensorMap* ta = map_of(rows, K, box);
     if (!ta) return cudaErrorInvalidValue;
     GemmI8 g = {};
     g.a = static_cast<const int8_t*>(m->codes.p);
@@ -695,7 +696,8 @@ struct I8Pass {
     g.type = x ? kF32 : kF16;
     g.weights_settled = 1;
     g.status = m->status;
-    return gemm_i8(*ta, w.tm, w2 ? w2->tm : w.tm, g, s);
+    const LayerDev::I8& second = w2 ? *w2 : w;
+    return box.deep ? gemm_i8(*ta, w.tm_deep, second.tm_deep, g, s) : gemm_i8(*ta, w.tm, second.tm, g, s);
   }
 
  private:
@@ -710,15 +712,15 @@ struct I8Pass {
     q.d = d;
     return q;
   }
-  const CUtensorMap* map_of(int rows, int k, int box) {
+  const CUtensorMap* map_of(int rows, int k, I8Box box) {
     for (int i = 0; i < n_maps; ++i)
-      if (maps[i].rows == rows && maps[i].k == k && maps[i].box == box) return &maps[i].tm;
+      if (maps[i].rows == rows && maps[i].k == k && maps[i].box.rows == box.rows && maps[i].box.deep == box.deep) return &maps[i].tm;
     if (n_maps == 8) n_maps = 0;
     Map& e = maps[n_maps++];
     e.rows = rows;
     e.k = k;
     e.box = box;
-    if (box && !make_i8_map(&e.tm, static_cast<const int8_t*>(m->codes.p), rows, k, k, box)) {
+    if (box.rows && !make_i8_map(&e.tm, static_cast<const int8_t*>(m->codes.p), rows, k, k, box)) {
       --n_maps;
       return nullptr;
     }
@@ -1265,7 +1267,8 @@ static int to_codes(const uint16_t* w, int rows, int d, LayerDev::I8* out, std::
   q.rows = rows;
   q.d = d;
   CS_CUDA(launch_quantize_i8(q, s));
-  if (!make_i8_map(&out->tm, out->codes, rows, d, d, 128)) {
+  if (!make_i8_map(&out->tm, out->codes, rows, d, d, {128, false}) ||
+      (d % 128 == 0 && !make_i8_map(&out->tm_deep, out->codes, rows, d, d, {128, true}))) {
     g_cuda_error = "cuTensorMapEncodeTiled failed for a weight matrix's codes";
     return CS_ECUDA;
   }
@@ -2419,9 +2422,9 @@ int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const i
   if (!aligned(out, type_bytes(dtype)) || out_stride < N) return CS_EINVAL;
   if (add && (!aligned(add, 4) || add_stride < N || (add == out && add_stride != out_stride && M > 1))) return CS_EINVAL;
   CUtensorMap ta, tw, tw2;
-  const int box = gemm_i8_box(M, N, K, w2 != nullptr);
-  if (box && (!make_i8_map(&ta, a, M, K, a_stride, box) || !make_i8_map(&tw, w, N, K, K, 128) ||
-              (w2 && !make_i8_map(&tw2, w2, N, K, K, 128)))) {
+  const I8Box box = gemm_i8_box(M, N, K, w2 != nullptr), of_w = {128, box.deep};
+  if (box.rows && (!make_i8_map(&ta, a, M, K, a_stride, box) || !make_i8_map(&tw, w, N, K, K, of_w) ||
+                   (w2 && !make_i8_map(&tw2, w2, N, K, K, of_w)))) {
     g_cuda_error = "cuTensorMapEncodeTiled failed";
     return CS_ECUDA;
   }

@@ -24,9 +24,10 @@ constexpr int kBK = 128;                    // codes (= bytes) of a k block: one
 constexpr int kTileBytes = 128 * kBK;       // 128 rows of it
 constexpr int kMaxSplit = 8;
 
-// 2D map over rows of `bytes`-byte values, `stride` values apart: boxes whose rows are 64 or 128 bytes, swizzled alike.
+// Map over rows of `bytes`-byte values, `stride` values apart: boxes whose rows are 64 or 128 bytes, swizzled alike. deep > 1: boxes of
+// so many such pieces of every row, one after the other; `cols` is then a multiple of box_cols.
 bool make_map(CUtensorMap* tm, void* base, CUtensorMapDataType type, int bytes, int64_t rows, int64_t cols, int64_t stride, int box_rows,
-              int box_cols) {
+              int box_cols, int deep = 1) {
   using Encode = decltype(&cuTensorMapEncodeTiled);
   static const Encode encode = []() -> Encode {
     void* p = nullptr;
@@ -37,10 +38,13 @@ bool make_map(CUtensorMap* tm, void* base, CUtensorMapDataType type, int bytes, 
                : nullptr;
   }();
   if (!encode) return false;
-  const cuuint64_t dims[2] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows)};
-  const cuuint64_t strides[1] = {static_cast<cuuint64_t>(stride * bytes)};
-  const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows)}, ones[2] = {1, 1};
-  return encode(tm, type, 2, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const int rank = deep > 1 ? 3 : 2;
+  const auto u64 = [](int64_t v) { return static_cast<cuuint64_t>(v); };
+  const cuuint64_t dims[3] = {u64(rank == 3 ? box_cols : cols), u64(rows), u64(cols / box_cols)};
+  const cuuint64_t strides[2] = {u64(stride * bytes), u64(box_cols * bytes)};
+  const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), static_cast<cuuint32_t>(deep)};
+  const cuuint32_t ones[3] = {1, 1, 1};
+  return encode(tm, type, rank, base, dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 box_cols * bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
@@ -427,7 +431,7 @@ cudaError_t launch_narrow(const CUtensorMap& ta, const CUtensorMap& tw, const CU
 
 template <bool GATED>
 cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
-  switch (gemm_i8_box(p.M, p.N, p.K, GATED)) {
+  switch (gemm_i8_box(p.M, p.N, p.K, GATED).rows) {
     case 16: return launch_narrow<16, GATED>(ta, tw, tw2, p, s);
     case 32: return launch_narrow<32, GATED>(ta, tw, tw2, p, s);
     case 64: return launch_narrow<64, GATED>(ta, tw, tw2, p, s);
@@ -442,8 +446,11 @@ cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const
 // what two separate 128 x 256 tiles would fetch.
 constexpr int kWideThreads = 320;                      // warp 0: copies, warp 1: products, warps 2-9: results
 struct Wide {
-  static constexpr int kStageBytes = 2 * kTileBytes;
-  static constexpr int kStages = 6;
+  // Two k blocks of both operands. A box costs the copy engine about 60 cycles besides its bytes, so that boxes of two blocks (32 KB)
+  // leave 90 % of the time that boxes of one do.
+  static constexpr int kOperandBytes = 2 * kTileBytes;
+  static constexpr int kStageBytes = 2 * kOperandBytes;
+  static constexpr int kStages = 3;
   static constexpr int kBoxOff = kStages * kStageBytes;               // [8 warps] 32 rows of 32 results on their way out
   static constexpr int kBoxBytes = 4096;
   static constexpr int kScaleOff = kBoxOff + 8 * kBoxBytes;           // [256] scales of the tile's weights
@@ -452,22 +459,19 @@ struct Wide {
   static_assert(kTotal <= 227 * 1024, "shared memory");
 };
 
-// The same as umma_i8_block over the pair, and an arrival at `commit_bar` of both CTAs once the products are done.
-__device__ __forceinline__ void umma_i8_pair_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate,
-                                                   uint64_t* commit_bar, uint32_t ctas) {
+// The same as umma_i8_block over the pair.
+__device__ __forceinline__ void umma_i8_pair_block(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred Q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t.reg .b16 m;\n\t"
+      "{\n\t.reg .pred Q;\n\t.reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
       "setp.ne.b32 Q, %4, 0;\n\t"
       "add.u64 a1, %1, 2;\n\tadd.u64 b1, %2, 2;\n\t"
       "add.u64 a2, %1, 4;\n\tadd.u64 b2, %2, 4;\n\t"
       "add.u64 a3, %1, 6;\n\tadd.u64 b3, %2, 6;\n\t"
-      "cvt.u16.u32 m, %6;\n\t"
       "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, Q;\n\t"
       "tcgen05.mma.cta_group::2.kind::i8 [%0], a1, b1, %3, 1;\n\t"
       "tcgen05.mma.cta_group::2.kind::i8 [%0], a2, b2, %3, 1;\n\t"
-      "tcgen05.mma.cta_group::2.kind::i8 [%0], a3, b3, %3, 1;\n\t"
-      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%5], m;\n\t}"
-      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(smem_u32(commit_bar)), "r"(ctas)
+      "tcgen05.mma.cta_group::2.kind::i8 [%0], a3, b3, %3, 1;\n\t}"
+      ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // Whether the phase is complete, without waiting.
@@ -493,6 +497,12 @@ __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m
   asm volatile(
       "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
       ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leader_bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(void* dst, const CUtensorMap* m, uint32_t leader_bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leader_bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
@@ -603,7 +613,7 @@ template <bool GATED>
 __global__ void __launch_bounds__(kWideThreads, 1)
 gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
                     const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_out, const GemmI8 p, int t_tiles,
-                    int tiles, int split, int out_way) {
+                    int tiles, int split, int out_way, int deep) {
   using L = Wide;
   constexpr uint32_t kIdesc = idesc_i8(256, 256);
   constexpr int kOut = GATED ? 128 : 256;              // output columns of a tile
@@ -625,9 +635,10 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   const uint32_t half = rank & 1, leader = rank & ~1u, pair_mask = 3u << leader;
   const int piece = rank >> 1;
-  const int kblocks = (p.K + kBK - 1) / kBK;
-  const int kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * piece / split);
-  const int kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (piece + 1) / split);
+  // k ranges are counted in pairs of blocks
+  const int kblocks = (p.K + kBK - 1) / kBK, kpairs = (kblocks + 1) / 2;
+  const int kp0 = static_cast<int>(static_cast<int64_t>(kpairs) * piece / split);
+  const int kp1 = static_cast<int>(static_cast<int64_t>(kpairs) * (piece + 1) / split);
   const int first = blockIdx.x / (2 * split), step = gridDim.x / (2 * split);
 
   if (threadIdx.x == 0) {
@@ -655,16 +666,24 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   // Token tiles run fastest: tiles that are in work together share their weights, and every weight is read from DRAM about once.
   const auto token0 = [&](int tile) { return (tile % t_tiles) * 256 + static_cast<int>(half) * 128; };
   const auto column0 = [&](int tile) { return tile / t_tiles * kOut; };
-  const auto load_w = [&](int stage, uint32_t bar, int kb, int tile) {
-    uint8_t* dst = smem + stage * L::kStageBytes + kTileBytes;
-    if (GATED) tma_load_2d_pair(dst, half ? &tm_w2 : &tm_w, bar, kb * kBK, column0(tile));
-    else tma_load_2d_pair(dst, &tm_w, bar, kb * kBK, column0(tile) + static_cast<int>(half) * 128);
+  const auto load = [&](uint8_t* dst, const CUtensorMap* m, uint32_t bar, int kp, int row) {
+    if (deep) {
+      tma_load_3d_pair(dst, m, bar, 0, row, 2 * kp);
+    } else {
+      tma_load_2d_pair(dst, m, bar, 2 * kp * kBK, row);
+      tma_load_2d_pair(dst + kTileBytes, m, bar, (2 * kp + 1) * kBK, row);      // zeros behind the last block
+    }
+  };
+  const auto load_w = [&](int stage, uint32_t bar, int kp, int tile) {
+    uint8_t* dst = smem + stage * L::kStageBytes + L::kOperandBytes;
+    if (GATED) load(dst, half ? &tm_w2 : &tm_w, bar, kp, column0(tile));
+    else load(dst, &tm_w, bar, kp, column0(tile) + static_cast<int>(half) * 128);
   };
   int ahead = 0;
   if (threadIdx.x == 0 && p.weights_settled && first < tiles) {
-    for (; ahead < L::kStages && kb0 + ahead < kb1; ++ahead) {
+    for (; ahead < L::kStages && kp0 + ahead < kp1; ++ahead) {
       if (!half) mbar_arrive_expect_tx(&full_bar[ahead], 2 * L::kStageBytes);
-      load_w(ahead, peer_addr(smem_u32(&full_bar[ahead]), leader), kb0 + ahead, first);
+      load_w(ahead, peer_addr(smem_u32(&full_bar[ahead]), leader), kp0 + ahead, first);
     }
   }
   pdl_wait();
@@ -675,14 +694,14 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       int stage = 0, issued = 0;
       uint32_t phase = 0;
       for (int tile = first; tile < tiles && ok; tile += step) {
-        for (int kb = kb0; kb < kb1; ++kb, ++issued) {
+        for (int kp = kp0; kp < kp1; ++kp, ++issued) {
           const uint32_t bar = peer_addr(smem_u32(&full_bar[stage]), leader);
           if (issued >= ahead) {
             if (!mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, status)) { ok = false; break; }
             if (!half) mbar_arrive_expect_tx(&full_bar[stage], 2 * L::kStageBytes);
-            load_w(stage, bar, kb, tile);
+            load_w(stage, bar, kp, tile);
           }
-          tma_load_2d_pair(smem + stage * L::kStageBytes, &tm_a, bar, kb * kBK, token0(tile));
+          load(smem + stage * L::kStageBytes, &tm_a, bar, kp, token0(tile));
           if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -696,18 +715,23 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ready = false;
-      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem)), bdesc0 = umma_desc_k128(smem_u32(smem) + kTileBytes);
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem)), bdesc0 = umma_desc_k128(smem_u32(smem) + L::kOperandBytes);
       for (int tile = first; tile < tiles && ok; tile += step) {
         if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, status)) { ok = false; break; }
         tc_fence_after();
-        for (int kb = kb0; kb < kb1; ++kb) {
+        for (int kp = kp0; kp < kp1; ++kp) {
           if (!ready && !mbar_wait(&full_bar[stage], phase, abort_flag, status)) { ok = false; break; }
           tc_fence_after();
           const int next = stage + 1 == L::kStages ? 0 : stage + 1;
           const uint32_t next_phase = next == 0 ? phase ^ 1u : phase;
           const uint64_t off = static_cast<uint64_t>(stage * (L::kStageBytes >> 4));
           ready = mbar_test(&full_bar[next], next_phase);
-          if (elect_one()) umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kb != kb0, &empty_bar[stage], pair_mask);
+          if (elect_one()) {
+            umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kp != kp0);
+            if (2 * kp + 1 < kblocks)
+              umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off + (kTileBytes >> 4), bdesc0 + off + (kTileBytes >> 4), kIdesc, 1);
+            umma_commit_pair(&empty_bar[stage], pair_mask);
+          }
           __syncwarp();
           stage = next;
           phase = next_phase;
@@ -835,7 +859,7 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
     return cudaErrorInvalidValue;
   const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide::kTotal, s,
                                            2 * split, ta, tw, tw2, tm_out, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
-                                           out_way);
+                                           out_way, p.K % kBK == 0 ? 1 : 0);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -856,13 +880,15 @@ Form form_of(int M, int N, int K, bool gated) {
 }
 }  // namespace
 
-int gemm_i8_box(int M, int N, int K, bool gated) {
+I8Box gemm_i8_box(int M, int N, int K, bool gated) {
   const Form f = form_of(M, N, K, gated);
-  return f == Form::kVector ? 0 : f == Form::kWide ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128;
+  if (f == Form::kVector) return {0, false};
+  if (f == Form::kWide) return {128, K % kBK == 0};
+  return {M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, false};
 }
 
-bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows) {
-  return make_map(tm, const_cast<int8_t*>(base), CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, stride, box_rows, kBK);
+bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, I8Box box) {
+  return make_map(tm, const_cast<int8_t*>(base), CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, stride, box.rows, kBK, box.deep ? 2 : 1);
 }
 
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {

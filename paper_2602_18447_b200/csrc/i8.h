@@ -40,12 +40,17 @@ struct GemmI8 {
   int32_t weights_settled;      // nothing that may still run before this launch writes the weights
   uint32_t* status;             // null: the word that i8_status reads
 };
-// 2D map over [rows, k] codes, rows `stride` bytes apart: boxes of box_rows x 128 bytes, 128-byte swizzle.
-bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows);
-// Rows of a box of the activations' map for such a product; 0: it takes no maps.
-int gemm_i8_box(int M, int N, int K, bool gated);
-// out = the codes' product times both scales (+ add), or silu(first) * second. K a multiple of 16, at most kMaxI8K. Maps: of a with
-// boxes of gemm_i8_box rows, of the weights with boxes of 128; tw2 is read for gated products only.
+// How a product reads its operands: boxes of so many rows (0: no maps), of one 128-byte piece of every row or of two (deep).
+struct I8Box {
+  int rows;
+  bool deep;
+};
+// The box of the activations' map for such a product; the weights' boxes have 128 rows and are as deep.
+I8Box gemm_i8_box(int M, int N, int K, bool gated);
+// Map over [rows, k] codes, rows `stride` bytes apart, 128-byte swizzle. k a multiple of 128 for deep boxes.
+bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, I8Box box);
+// out = the codes' product times both scales (+ add), or silu(first) * second. K a multiple of 16, at most kMaxI8K. Maps as gemm_i8_box
+// says; tw2 is read for gated products only.
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s);
 // The time-out bits that launches without a status word of their own have left on this device, and clears them. Synchronises s.
 cudaError_t i8_status(uint32_t* bits, cudaStream_t s);
