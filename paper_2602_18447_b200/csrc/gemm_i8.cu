@@ -101,8 +101,22 @@ __device__ __forceinline__ void st_peer_v4(uint32_t addr, uint32_t a, uint32_t b
 __device__ __forceinline__ float scaled(uint32_t acc, float as, float ws) {
   return __fmul_rn(__fmul_rn(static_cast<float>(static_cast<int>(acc)), as), ws);
 }
-// silu(y) y2, silu(y) = y / (1 + e^-y); the fast division leaves 0 for a divisor beyond 2^126, which is what the quotient tends to.
-__device__ __forceinline__ float gate(float y, float y2) { return __fmul_rn(__fdividef(y, __fadd_rn(1.0f, __expf(-y))), y2); }
+// The same without the conversion unit, which the exponential and the reciprocal of a gated tile keep busy: the upper half of the sum
+// (its sign turned) and the lower half are put under the exponent of 2^23; the upper one times 2^16 less both offsets is exact, and
+// adding the lower one rounds once.
+__device__ __forceinline__ float scaled_by_parts(uint32_t acc, float as, float ws) {
+  const float hi = __uint_as_float(__byte_perm(acc ^ 0x80000000u, 0x4b000000u, 0x7632));
+  const float lo = __uint_as_float(__byte_perm(acc, 0x4b000000u, 0x7610));
+  const float sum = __fadd_rn(fmaf(hi, 65536.0f, -(8388608.0f + 32768.0f) * 65536.0f - 8388608.0f), lo);
+  return __fmul_rn(__fmul_rn(sum, as), ws);
+}
+// silu(y) y2, silu(y) = y / (1 + e^-y). The divisor is at least 1; beyond 2^126 its reciprocal is 0, which is what it tends to.
+__device__ __forceinline__ float gate(float y, float y2) {
+  const float d = __fadd_rn(1.0f, fast_exp2(__fmul_rn(y, -1.44269504f)));
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+  return __fmul_rn(__fmul_rn(y, r), y2);
+}
 
 __device__ __forceinline__ void store_one(void* out, int64_t at, float v, int type) {
   if (type == kF16) static_cast<__half*>(out)[at] = __float2half_rn(v);
@@ -505,8 +519,10 @@ __device__ __forceinline__ void tma_load_3d_pair(void* dst, const CUtensorMap* m
       ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(leader_bar), "r"(x), "r"(y), "r"(z)
       : "memory");
 }
+// An arrival at another CTA's barrier that orders tensor-memory reads only (between the tcgen05 fences on either side): a release at
+// cluster scope would wait for this thread's stores to global memory, 2500 cycles in which the products wait for the accumulator.
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols) {
   asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;\n\t"
@@ -529,7 +545,7 @@ __device__ __forceinline__ void results_of(const uint32_t (&r)[32], const uint32
       const float4 w2 = reinterpret_cast<const float4*>(ws2)[j];
       const float w2j[4] = {w2.x, w2.y, w2.z, w2.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[4 * j + e] = gate(v[4 * j + e], scaled(r2[4 * j + e], as, w2j[e]));
+      for (int e = 0; e < 4; ++e) v[4 * j + e] = gate(v[4 * j + e], scaled_by_parts(r2[4 * j + e], as, w2j[e]));
     }
   }
 }
