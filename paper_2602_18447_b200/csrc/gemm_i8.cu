@@ -863,7 +863,9 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
   const int kblocks = (p.K + kBK - 1) / kBK;
   int split = 1;
-  while (split < (GATED ? 2 : 4) && tiles <= kClusters[0][2 * split] && kblocks >= 8 * split) split *= 2;
+  // Handing sums over takes about as long as the products of 8 k blocks (300 x 1536 x 1536, 12 blocks: 8.0 us whole and cut in two;
+  // 421 x 2048 x 2048: 9.6 and 9.1; 300 x 1536 x 3584: 12.9, 10.8 and, in four, 10.4; 735 x 1536 x 8960: 24.6 and 17.7).
+  while (split < (GATED ? 2 : 4) && tiles <= kClusters[0][2 * split] && kblocks >= 14 * split) split *= 2;
   const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
   const int bytes = p.type == kF32 ? 4 : 2;
   const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
