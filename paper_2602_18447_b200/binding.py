@@ -563,47 +563,48 @@ def cs_rmsnorm(x, gain, out, rows: int, d: int, eps: float, stream=None) -> None
 CS_F32 = 2
 
 _i8_types: dict = {}
-_ROWS, _F32, _I8 = (CS_F16, CS_BF16, CS_F32), (CS_F32,), (-1,)
+_ROWS, _F32 = (CS_F16, CS_BF16, CS_F32), (CS_F32,)
 
 
 def _i8_ready():
-    """The current device; the types' codes are looked up at the first call."""
+    """The current device; the types are looked up at the first call."""
     torch = _torch or _t()
     if not _i8_types:
-        _i8_types.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16, torch.float32: CS_F32, torch.int8: -1})
+        _i8_types.update({torch.float16: CS_F16, torch.bfloat16: CS_BF16, torch.float32: CS_F32, "codes": torch.int8,
+                          "scales": torch.float32})
     return torch.cuda.current_device()
 
 
-def _whole(t, name, kinds, shape, dev):
-    """The address of a contiguous CUDA tensor of one of the types `kinds` and of this shape on the device `dev`."""
-    if _i8_types.get(t.dtype) not in kinds or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous tensor of shape {tuple(shape)} on the current device, "
-                         f"got {tuple(t.shape)} of {t.dtype}")
+def _whole(t, name, kind, shape, dev):
+    """The address of a contiguous CUDA tensor of codes or scales (`kind`) and of this shape on the device `dev`."""
+    if t.dtype is not _i8_types[kind] or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous {kind} of shape {tuple(shape)} on the current device, got {tuple(t.shape)} of "
+                         f"{t.dtype}")
     return t.data_ptr()
 
 
 def _spread(t, name, kinds, shape, dev, step):
-    """(address, elements between rows, type) of such a matrix whose rows are contiguous but may lie apart; what a single row
-    is given as its stride is a row's length, in whole `step`s."""
+    """(address, elements between rows, type) of a matrix of one of the types `kinds` (None: codes) whose rows are contiguous but may
+    lie apart; what a single row is given as its stride is a row's length, in whole `step`s."""
     code = _i8_types.get(t.dtype)
-    if code not in kinds or t.shape != shape or t.get_device() != dev:
+    if (t.dtype is not _i8_types["codes"] if kinds is None else code not in kinds) or t.shape != shape or t.get_device() != dev:
         raise ValueError(f"{name}: expected a matrix of shape {tuple(shape)} on the current device, got {tuple(t.shape)} of {t.dtype}")
     rows, cols = shape
-    if rows <= 1:
-        if rows and cols > 1 and t.stride()[1] != 1:
-            raise ValueError(f"{name}: the values of a row have to be contiguous")
-        return (t.data_ptr() if rows else None), (cols + step - 1) // step * step, code
     apart, along = t.stride()
-    if apart < cols or (cols > 1 and along != 1):
-        raise ValueError(f"{name}: the values of a row have to be contiguous, and rows must not overlap")
-    return t.data_ptr(), apart, code
+    if rows > 1:
+        if apart < cols or (along != 1 and cols > 1):
+            raise ValueError(f"{name}: the values of a row have to be contiguous, and rows must not overlap")
+        return t.data_ptr(), apart, code
+    if rows and along != 1 and cols > 1:
+        raise ValueError(f"{name}: the values of a row have to be contiguous")
+    return (t.data_ptr() if rows else None), (cols + step - 1) // step * step, code
 
 
 def _rows_2d(t, name):
-    shape = tuple(t.shape)
+    shape = t.shape
     if len(shape) != 2:
         raise ValueError(f"{name} is a matrix of rows")
-    return shape
+    return tuple(shape)
 
 
 def _stream_on(dev, stream):
@@ -614,26 +615,30 @@ def _stream_on(dev, stream):
 def cs_quantize_i8(x, codes, scales, stream=None) -> None:
     """x: CUDA rows [M, d] (float16, bfloat16 or float32; the rows may lie apart); codes: contiguous int8 [M, d]; scales:
     float32 [M]."""
-    dev, shape = _i8_ready(), _rows_2d(x, "x")
+    dev = _i8_ready()
+    m, d = shape = _rows_2d(x, "x")
     xp, xs, kind = _spread(x, "x", _ROWS, shape, dev, 8)
-    _check((_lib or load_library()).cs_quantize_i8(xp, xs, kind, _whole(codes, "codes", _I8, shape, dev),
-                                         _whole(scales, "scales", _F32, shape[:1], dev), shape[0], shape[1], _stream_on(dev, stream)),
+    _check((_lib or load_library()).cs_quantize_i8(xp, xs, kind, _whole(codes, "codes", "codes", shape, dev),
+                                                   _whole(scales, "scales", "scales", (m,), dev), m, d, _stream_on(dev, stream)),
            "cs_quantize_i8")
 
 
 def cs_dequantize_i8(codes, scales, out, stream=None) -> None:
     """codes: contiguous CUDA int8 [M, d]; scales: float32 [M]; out: rows [M, d] (float16, bfloat16 or float32)."""
-    dev, shape = _i8_ready(), _rows_2d(codes, "codes")
+    dev = _i8_ready()
+    m, d = shape = _rows_2d(codes, "codes")
     op, os_, kind = _spread(out, "out", _ROWS, shape, dev, 8)
-    _check((_lib or load_library()).cs_dequantize_i8(_whole(codes, "codes", _I8, shape, dev), _whole(scales, "scales", _F32, shape[:1], dev),
-                                           shape[0], shape[1], op, os_, kind, _stream_on(dev, stream)), "cs_dequantize_i8")
+    _check((_lib or load_library()).cs_dequantize_i8(_whole(codes, "codes", "codes", shape, dev),
+                                                     _whole(scales, "scales", "scales", (m,), dev), m, d, op, os_, kind,
+                                                     _stream_on(dev, stream)), "cs_dequantize_i8")
 
 
 def cs_rmsnorm_i8(x, gain, codes, scales, eps: float, delta=None, x_out=None, stream=None) -> None:
     """x: CUDA rows [M, d] (float16, bfloat16 or float32); gain: float32 [d]; codes: contiguous int8 [M, d]; scales: float32 [M].
     delta: rows added to x first (of the type of x, or of any of the three for float32 x), x_out: rows of the type of x that
     receive the sum (x itself where it is not given)."""
-    dev, shape = _i8_ready(), _rows_2d(x, "x")
+    dev = _i8_ready()
+    m, d = shape = _rows_2d(x, "x")
     xp, xs, kind = _spread(x, "x", _ROWS, shape, dev, 8)
     dp, ds, dkind, op, os_ = None, 0, kind, None, 0
     if delta is not None:
@@ -641,17 +646,20 @@ def cs_rmsnorm_i8(x, gain, codes, scales, eps: float, delta=None, x_out=None, st
         op, os_ = (xp, xs) if x_out is None else _spread(x_out, "x_out", (kind,), shape, dev, 8)[:2]
     elif x_out is not None:
         raise ValueError("x_out comes with delta")
-    _check((_lib or load_library()).cs_rmsnorm_i8(xp, xs, kind, dp, ds, dkind, op, os_, _whole(gain, "gain", _F32, shape[1:], dev),
-                                        _whole(codes, "codes", _I8, shape, dev), _whole(scales, "scales", _F32, shape[:1], dev),
-                                        shape[0], shape[1], float(eps), _stream_on(dev, stream)), "cs_rmsnorm_i8")
+    _check((_lib or load_library()).cs_rmsnorm_i8(xp, xs, kind, dp, ds, dkind, op, os_, _whole(gain, "gain", "scales", (d,), dev),
+                                                  _whole(codes, "codes", "codes", shape, dev),
+                                                  _whole(scales, "scales", "scales", (m,), dev), m, d, eps, _stream_on(dev, stream)),
+           "cs_rmsnorm_i8")
 
 
 def cs_gemm_i8(a, a_scales, w, w_scales, out, w2=None, w2_scales=None, add=None, stream=None) -> None:
     """a: CUDA int8 codes [M, K] (rows may lie apart by a multiple of 16); w, w2: contiguous int8 codes [N, K]; scales: float32 [M],
     [N], [N]; out: rows [M, N]. out = y (any of the three row types), add + y (add, out: float32 rows; out may be add) or
     silu(y) * y2 (float16 or bfloat16)."""
-    dev, (m, k), n = _i8_ready(), _rows_2d(a, "a"), _rows_2d(w, "w")[0]
-    ap, as_, _ = _spread(a, "a", _I8, (m, k), dev, 16)
+    dev = _i8_ready()
+    m, k = shape = _rows_2d(a, "a")
+    n = _rows_2d(w, "w")[0]
+    ap, as_, _ = _spread(a, "a", None, shape, dev, 16)
     w2p = w2sp = dp = None
     ds, kinds = 0, _ROWS
     if w2 is not None:
@@ -660,16 +668,16 @@ def cs_gemm_i8(a, a_scales, w, w_scales, out, w2=None, w2_scales=None, add=None,
         if w2_scales is None:
             raise ValueError("w2 comes with w2_scales")
         kinds = _ROWS[:2]
-        w2p, w2sp = _whole(w2, "w2", _I8, (n, k), dev), _whole(w2_scales, "w2_scales", _F32, (n,), dev)
+        w2p, w2sp = _whole(w2, "w2", "codes", (n, k), dev), _whole(w2_scales, "w2_scales", "scales", (n,), dev)
     elif w2_scales is not None:
         raise ValueError("w2_scales come with w2")
     if add is not None:
         kinds = _F32
         dp, ds, _ = _spread(add, "add", _F32, (m, n), dev, 1)
     op, os_, kind = _spread(out, "out", kinds, (m, n), dev, 1)
-    _check((_lib or load_library()).cs_gemm_i8(ap, as_, _whole(a_scales, "a_scales", _F32, (m,), dev), _whole(w, "w", _I8, (n, k), dev),
-                                     _whole(w_scales, "w_scales", _F32, (n,), dev), w2p, w2sp, dp, ds, op, os_, m, n, k, kind,
-                                     _stream_on(dev, stream)), "cs_gemm_i8")
+    _check((_lib or load_library()).cs_gemm_i8(ap, as_, _whole(a_scales, "a_scales", "scales", (m,), dev),
+                                               _whole(w, "w", "codes", (n, k), dev), _whole(w_scales, "w_scales", "scales", (n,), dev),
+                                               w2p, w2sp, dp, ds, op, os_, m, n, k, kind, _stream_on(dev, stream)), "cs_gemm_i8")
 
 
 def cs_i8_status(stream=None) -> None:

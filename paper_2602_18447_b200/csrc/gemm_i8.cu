@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kBK = 128;                    // codes (= bytes) of a k block: one 128-byte swizzled row
 constexpr int kTileBytes = 128 * kBK;       // 128 rows of it
-constexpr int kMaxSplit = 8;
+constexpr int kMaxSplit = 8;                // CTAs along k of the narrow form: the largest cluster
 
 // Map over rows of `bytes`-byte values, `stride` values apart: boxes whose rows are 64 or 128 bytes, swizzled alike. deep > 1: boxes of
 // so many such pieces of every row, one after the other; `cols` is then a multiple of box_cols.
@@ -80,6 +80,12 @@ __device__ __forceinline__ void tmem_ld_16(uint32_t taddr, uint32_t (&r)[16]) {
       : "r"(taddr)
       : "memory");
 }
+__device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, uint64_t* bar, int x, int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 __device__ __forceinline__ void cluster_arrive_wait() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -124,9 +130,9 @@ __device__ __forceinline__ void store_one(void* out, int64_t at, float v, int ty
   else static_cast<float*>(out)[at] = v;
 }
 
-// Clusters of 2 c CTAs that run at once, [one or two such CTAs to an SM][c]: what cudaOccupancyMaxActiveClusters says on a B200, whose
-// 148 SMs are not evenly spread over the groups that a cluster has to fit in.
-constexpr int kClusters[2][5] = {{0, 74, 33, 0, 15}, {0, 148, 71, 0, 33}};
+// Clusters of c CTAs, one to an SM, that run at once: what cudaOccupancyMaxActiveClusters says on a B200, whose 148 SMs are not evenly
+// spread over the groups that a cluster has to fit in.
+constexpr int kClusters[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
 
 // -------------------------------------------------------------------------------------------------------- vector form
 constexpr int kVectorTokens = 8;            // at most
@@ -223,44 +229,47 @@ constexpr int kNarrowThreads = 320;         // warp 0: copies, warp 1: products,
 template <int BN, bool GATED>
 struct Narrow {
   static constexpr int kWTiles = GATED ? 2 : 1;
-  static constexpr int kStageBytes = kWTiles * kTileBytes + BN * kBK;
-  // Two CTAs to an SM where the columns are few, else one that takes it all.
-  static constexpr int kStages = (BN * kWTiles <= 64 ? 112 * 1024 : 216 * 1024) / kStageBytes;
+  // A stage is two k blocks (see the wide form): of the weights' 128 rows, of the second weights', and of the tokens.
+  static constexpr int kTokenBlock = BN * kBK;
+  static constexpr int kTokenOff = kWTiles * 2 * kTileBytes;
+  static constexpr int kStageBytes = kTokenOff + 2 * kTokenBlock;
   static constexpr uint32_t kCols = kWTiles * BN < 32 ? 32 : kWTiles * BN;
-  static constexpr int kScaleOff = kStages * kStageBytes;   // [BN] scales of the tokens
-  static constexpr int kBarOff = kScaleOff + BN * 4;
-  static constexpr int kTotal = kBarOff + 256 + 1024;       // + slack for the tiles' alignment
-  // CTAs that share an SM must find their columns whenever they fit its shared memory: one that waited for columns while the rest of
-  // its cluster waited for it could wait for a CTA that waits likewise.
-  static_assert(kTotal * 512ll >= kCols * 227ll * 1024, "tensor memory before shared memory");
-  static_assert(kStages >= 3 && kTotal <= 227 * 1024 && std::max(BN, 4 * kMaxSplit) * kWTiles * 512 <= kStages * kStageBytes, "stages");
+  static constexpr int kBarOff = BN * 4;                    // behind the tokens' scales
+  static constexpr int kHead = 1024;                        // scales and barriers, then the stages
+  static constexpr int kMostStages = std::min(8, (224 * 1024 - kHead) / kStageBytes);
+  // Shared memory of a CTA with so many stages, with slack for the tiles' alignment. CTAs that share an SM must find their columns
+  // whenever they fit its shared memory: one that waited for columns while the rest of its cluster waited for it could wait for a CTA
+  // that waits likewise.
+  static constexpr int bytes(int stages) { return std::max(kHead + stages * kStageBytes + 1024, static_cast<int>(kCols) * 227 * 2 + 512); }
+  static_assert(kMostStages >= 2 && bytes(kMostStages) <= 227 * 1024 && kBarOff + (2 * kMostStages + 2) * 8 <= kHead, "stages");
 };
 
 template <int BN, bool GATED>
 __global__ void __launch_bounds__(kNarrowThreads)
 gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
-                      const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int split, int log_own) {
+                      const __grid_constant__ CUtensorMap tm_w2, const GemmI8 p, int split, int log_own,
+                      int stages, int deep) {
   using L = Narrow<BN, GATED>;
   constexpr uint32_t kIdesc = idesc_i8(128, BN);
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  float* a_scales = reinterpret_cast<float*>(smem + L::kScaleOff);
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
-  uint64_t* full_bar = bars;
-  uint64_t* empty_bar = bars + L::kStages;
-  uint64_t* acc_bar = bars + 2 * L::kStages;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * L::kStages + 1);
+  float* a_scales = reinterpret_cast<float*>(smem);
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem + L::kBarOff);
+  uint64_t* empty_bar = full_bar + L::kMostStages;
+  uint64_t* acc_bar = full_bar + 2 * L::kMostStages;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_bar + 1);
+  smem += L::kHead;
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* status = p.status ? p.status : &g_status;
 
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const int piece = blockIdx.x % split, n0 = blockIdx.x / split * 128;
-  const int kblocks = (p.K + kBK - 1) / kBK;
-  const int kb0 = static_cast<int>(static_cast<int64_t>(kblocks) * piece / split);
-  const int kb1 = static_cast<int>(static_cast<int64_t>(kblocks) * (piece + 1) / split);
+  const int kblocks = (p.K + kBK - 1) / kBK, kpairs = (kblocks + 1) / 2;
+  const int kp0 = static_cast<int>(static_cast<int64_t>(kpairs) * piece / split);
+  const int kp1 = static_cast<int>(static_cast<int64_t>(kpairs) * (piece + 1) / split);
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < L::kStages; ++s) {
+    for (int s = 0; s < stages; ++s) {
       mbar_init(&full_bar[s], 1);
       mbar_init(&empty_bar[s], 1);
     }
@@ -280,16 +289,24 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   pdl_launch_dependents();
+  const auto load = [&](uint8_t* dst, const CUtensorMap* m, uint64_t* bar, int kp, int row, int block) {
+    if (deep) {
+      tma_load_3d(dst, m, bar, 0, row, 2 * kp);
+    } else {
+      tma_load_2d(dst, m, bar, 2 * kp * kBK, row);
+      tma_load_2d(dst + block, m, bar, (2 * kp + 1) * kBK, row);      // zeros behind the last block
+    }
+  };
+  const auto load_w = [&](int stage, int kp) {
+    uint8_t* dst = smem + stage * L::kStageBytes;
+    mbar_arrive_expect_tx(&full_bar[stage], L::kStageBytes);
+    load(dst, &tm_w, &full_bar[stage], kp, n0, kTileBytes);
+    if (GATED) load(dst + 2 * kTileBytes, &tm_w2, &full_bar[stage], kp, n0, kTileBytes);
+  };
   // Weights that nothing in front of this launch writes are sent for at once, the tokens' rows after the wait.
   int ahead = 0;
-  if (threadIdx.x == 0 && p.weights_settled) {
-    for (; ahead < L::kStages && kb0 + ahead < kb1; ++ahead) {
-      uint8_t* sw = smem + ahead * L::kStageBytes;
-      mbar_arrive_expect_tx(&full_bar[ahead], L::kStageBytes);
-      tma_load_2d(sw, &tm_w, &full_bar[ahead], (kb0 + ahead) * kBK, n0);
-      if (GATED) tma_load_2d(sw + kTileBytes, &tm_w2, &full_bar[ahead], (kb0 + ahead) * kBK, n0);
-    }
-  }
+  if (threadIdx.x == 0 && p.weights_settled)
+    for (; ahead < stages && kp0 + ahead < kp1; ++ahead) load_w(ahead, kp0 + ahead);
   pdl_wait();
 
   bool ok = true;
@@ -297,16 +314,13 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
-      for (int kb = kb0; kb < kb1; ++kb) {
-        uint8_t* sw = smem + stage * L::kStageBytes;
-        if (kb - kb0 >= ahead) {
+      for (int kp = kp0; kp < kp1; ++kp) {
+        if (kp - kp0 >= ahead) {
           if (!mbar_wait(&empty_bar[stage], phase ^ 1u, abort_flag, status)) { ok = false; break; }
-          mbar_arrive_expect_tx(&full_bar[stage], L::kStageBytes);
-          tma_load_2d(sw, &tm_w, &full_bar[stage], kb * kBK, n0);
-          if (GATED) tma_load_2d(sw + kTileBytes, &tm_w2, &full_bar[stage], kb * kBK, n0);
+          load_w(stage, kp);
         }
-        tma_load_2d(sw + L::kWTiles * kTileBytes, &tm_a, &full_bar[stage], kb * kBK, 0);
-        if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+        load(smem + stage * L::kStageBytes + L::kTokenOff, &tm_a, &full_bar[stage], kp, 0, L::kTokenBlock);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
       // after a time-out: let the copies in flight land before the CTA goes away
       if (!ok)
@@ -317,15 +331,17 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
       int stage = 0;
       uint32_t phase = 0;
       const uint64_t wdesc0 = umma_desc_k128(smem_u32(smem));
-      for (int kb = kb0; kb < kb1; ++kb) {
+      for (int kp = kp0; kp < kp1; ++kp) {
         if (!mbar_wait(&full_bar[stage], phase, abort_flag, status)) { ok = false; break; }
         tc_fence_after();
         const uint64_t wd = wdesc0 + static_cast<uint64_t>(stage * (L::kStageBytes >> 4));
-        const uint64_t ad = wd + (L::kWTiles * kTileBytes >> 4);
-        umma_i8_block(tmem_base, wd, ad, kIdesc, kb != kb0);
-        if (GATED) umma_i8_block(tmem_base + BN, wd + (kTileBytes >> 4), ad, kIdesc, kb != kb0);
+        for (int b = 0; b < 2 && 2 * kp + b < kblocks; ++b) {
+          const uint64_t wb = wd + b * (kTileBytes >> 4), ab = wd + (L::kTokenOff + b * L::kTokenBlock >> 4);
+          umma_i8_block(tmem_base, wb, ab, kIdesc, kp != kp0 || b);
+          if (GATED) umma_i8_block(tmem_base + BN, wb + (2 * kTileBytes >> 4), ab, kIdesc, kp != kp0 || b);
+        }
         umma_commit(&empty_bar[stage]);
-        if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
       }
       if (ok) umma_commit(acc_bar);
     }
@@ -380,6 +396,14 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
 #pragma unroll 1
     for (int c = (own0 & ~15) + side * 16; c < own1; c += 32) {
       uint32_t r[16], r2[16];
+      float x[16];
+      if (!GATED && p.add) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int64_t t = c + j;
+          x[j] = t >= own0 && t < own1 && n < p.N ? p.add[t * p.add_stride + n] : 0.f;
+        }
+      }
       tmem_ld_16(t_row + c, r);
       if (GATED) tmem_ld_16(t_row + BN + c, r2);
       tmem_ld_wait();
@@ -406,7 +430,7 @@ gemm_i8_narrow_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_con
           if (t >= own1 || n >= p.N) continue;
           float v = scaled(s[e], as[e], ws);
           if (GATED) v = gate(v, scaled(s2[e], as[e], ws2));
-          if (p.add) v = __fadd_rn(p.add[t * p.add_stride + n], v);
+          else if (p.add) v = __fadd_rn(x[j + e], v);
           store_one(p.out, t * p.out_stride + n, v, p.type);
         }
       }
@@ -425,20 +449,25 @@ template <int BN, bool GATED>
 cudaError_t launch_narrow(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
   using L = Narrow<BN, GATED>;
   static std::atomic<uint64_t> opted{0};
-  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_narrow_kernel<BN, GATED>, L::kTotal, opted); e != cudaSuccess) return e;
-  const int tiles = (p.N + 127) / 128, kblocks = (p.K + kBK - 1) / kBK;
-  int split = 1, log_own = BN == 16 ? 4 : BN == 32 ? 5 : BN == 64 ? 6 : 7;
-  // every piece has a k block, and all clusters run at once; fewer than four tokens are not shared out
-  constexpr int kTogether = L::kTotal > 113 * 1024 ? 1 : 2;
-  while (split < kMaxSplit && tiles <= kClusters[kTogether - 1][split] && kblocks >= 2 * split) {
-    split *= 2;
-    log_own = std::max(2, log_own - 1);
-  }
+  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_narrow_kernel<BN, GATED>, L::bytes(L::kMostStages), opted); e != cudaSuccess) return e;
+  // As many pieces as there are SMs for, each with a pair of k blocks; fewer than four tokens are not shared out.
+  const int tiles = (p.N + 127) / 128, kpairs = ((p.K + kBK - 1) / kBK + 1) / 2;
+  int split = std::max(1, std::min(std::min(kMaxSplit, kpairs), kNumSMs / tiles));
+  int log_own = 2;
+  const auto fits = [&] {      // the clusters on the GPU, and what a CTA is handed over in two stages
+    for (log_own = 2; (split << log_own) < BN;) ++log_own;
+    return tiles <= kClusters[split] && (split << log_own) * L::kWTiles * 512 <= 2 * L::kStageBytes;
+  };
+  while (!fits() && split > 1) --split;
+  // One CTA to an SM has it all; where there are more CTAs than SMs, two share it if their columns are few.
+  const int two = (112 * 1024 - L::kHead) / L::kStageBytes;
+  const int stages = tiles * split > kNumSMs && two >= 2 ? two : L::kMostStages;
   const dim3 grid(static_cast<unsigned>(tiles * split));
-  const cudaError_t e = split > 1 ? launch_pdl_cluster(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::kTotal, s, split,
-                                                       ta, tw, tw2, p, split, log_own)
-                                  : launch_pdl(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::kTotal, s, ta, tw, tw2, p,
-                                               split, log_own);
+  const int deep = p.K % kBK == 0;
+  const cudaError_t e = split > 1 ? launch_pdl_cluster(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::bytes(stages), s,
+                                                       split, ta, tw, tw2, p, split, log_own, stages, deep)
+                                  : launch_pdl(gemm_i8_narrow_kernel<BN, GATED>, grid, dim3(kNarrowThreads), L::bytes(stages), s, ta, tw,
+                                               tw2, p, split, log_own, stages, deep);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -562,65 +591,90 @@ __device__ __forceinline__ void tma_store_wait() {
 constexpr int kOutBoxes = 0, kOutPieces = 1, kOutValues = 2;
 // A warp's 32 rows x 32 columns through its box in shared memory, so that rows are written in whole 64- or 128-byte pieces (from the
 // lanes' registers every store would touch 32 rows). Stores are boxes of a tensor map, or, where the residual is added, 16-byte pieces,
-// or single values where rows of the output are not made of 16-byte pieces. Boxes of 16-bit results alternate between two places.
-__device__ __forceinline__ void write_box(const GemmI8& p, const CUtensorMap* tm_out, uint8_t* box, int& turn, const float (&v)[32], int t0,
-                                          int n0, int lane, int out_way) {
-  if (p.type != kF32) {
-    box += turn * 2048;
-    if (out_way == kOutBoxes) {
-      if (lane == 0) tma_store_wait<1>();
-      turn ^= 1;
-    }
-    __syncwarp();
+// or, where rows of the output are not made of 16-byte pieces, words and single values. Boxes of 16-bit results alternate between two
+// places.
+__device__ __forceinline__ void fill_box(uint8_t* box, const float (&v)[32], int lane, int type) {
+  if (type != kF32) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint32_t w[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float lo = v[8 * j + 2 * e], hi = v[8 * j + 2 * e + 1];
-        w[e] = p.type == kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
+        w[e] = type == kF16 ? pack_f16x2(lo, hi) : pack_bf16x2(lo, hi);
       }
       *reinterpret_cast<uint4*>(box + lane * 64 + ((j ^ (lane >> 1 & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
     }
   } else {
-    if (out_way == kOutBoxes && lane == 0) tma_store_wait<0>();
-    __syncwarp();
 #pragma unroll
     for (int j = 0; j < 8; ++j)
       *reinterpret_cast<float4*>(box + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
   }
-  if (out_way == kOutBoxes) {
-    fence_proxy_async();
-    __syncwarp();
-    if (lane == 0 && t0 < p.M) tma_store_2d(tm_out, box, n0, t0);
+}
+// The residual's pieces that add_pieces adds: sent for ahead of the products' results.
+__device__ __forceinline__ void load_pieces(const GemmI8& p, int t0, int n0, int lane, float4 (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t t = t0 + 4 * i + (lane >> 3);
+    x[i] = t < p.M && n0 + 32 <= p.N ? *reinterpret_cast<const float4*>(p.add + t * p.add_stride + n0 + 4 * (lane & 7))
+                                     : make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+}
+__device__ __forceinline__ void add_pieces(const GemmI8& p, const uint8_t* box, int t0, int n0, int lane, const float4 (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int row = 4 * i + (lane >> 3);
+    const int64_t t = t0 + row;
+    const float4 y = *reinterpret_cast<const float4*>(box + row * 128 + (((lane & 7) ^ (row & 7)) << 4));
+    if (t < p.M)
+      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + t * p.out_stride + n0 + 4 * (lane & 7)) =
+          make_float4(__fadd_rn(x[i].x, y.x), __fadd_rn(x[i].y, y.y), __fadd_rn(x[i].z, y.z), __fadd_rn(x[i].w, y.w));
+  }
+}
+// `width`: 32, or 64 for two boxes of 16-bit results side by side: the fewer pieces a row is written in, the fewer of them share a
+// sector of memory with their neighbours.
+__device__ __forceinline__ void write_values(const GemmI8& p, const uint8_t* box, int t0, int n0, int lane, int width) {
+  const int rows = min(32, p.M - t0), cols = min(width, p.N - n0);
+  if (p.type == kF32) {
+    // a value a lane, eight rows at a time
+    for (int r = 0; r < rows; r += 8) {
+      float x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        x[j] = p.add && r + j < rows && lane < cols ? p.add[(t0 + r + j) * p.add_stride + n0 + lane] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = r + j;
+        const float y = *reinterpret_cast<const float*>(box + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4);
+        if (row < rows && lane < cols) static_cast<float*>(p.out)[(t0 + row) * p.out_stride + n0 + lane] = p.add ? __fadd_rn(x[j], y) : y;
+      }
+    }
     return;
   }
-  __syncwarp();
-  if (out_way == kOutPieces && n0 + 32 <= p.N) {           // fp32, with or without the residual
-    const int c = lane & 7;
+  // A row at a time, a word a lane: of values 2 l, 2 l + 1 where the row begins on a word, else of 2 l + 1, 2 l + 2, and the last lane
+  // has the first and the last value.
+  const auto value = [&](int row, int c) {
+    return *reinterpret_cast<const uint16_t*>(box + (c >> 5) * 2048 + row * 64 + (((c >> 3 & 3) ^ (row >> 1 & 3)) << 4) + (c & 7) * 2);
+  };
+  // eight rows at a time, so that their way through shared memory and out overlaps
+  uint16_t* o = static_cast<uint16_t*>(p.out) + static_cast<int64_t>(t0) * p.out_stride + n0;
+  const int first = static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1), turns = static_cast<int>(p.out_stride & 1);
+#pragma unroll 1
+  for (int r = 0; r < rows; r += 8, o += 8 * p.out_stride) {
+    uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = 4 * i + (lane >> 3);
-      const int64_t t = t0 + row;
-      if (t >= p.M) break;
-      float4 y = *reinterpret_cast<const float4*>(box + row * 128 + ((c ^ (row & 7)) << 4));
-      if (p.add) {
-        const float4 x = *reinterpret_cast<const float4*>(p.add + t * p.add_stride + n0 + 4 * c);
-        y = make_float4(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y), __fadd_rn(x.z, y.z), __fadd_rn(x.w, y.w));
-      }
-      *reinterpret_cast<float4*>(static_cast<float*>(p.out) + t * p.out_stride + n0 + 4 * c) = y;
+    for (int j = 0; j < 8; ++j) {
+      const int c = 2 * lane + (first ^ (turns & j));
+      w[j] = value(r + j, c) | static_cast<uint32_t>(value(r + j, c + 1 & 63)) << 16;
     }
-  } else if (n0 + lane < p.N) {
-    for (int row = 0; row < 32 && t0 + row < p.M; ++row) {
-      const int64_t t = t0 + row;
-      if (p.type == kF32) {
-        float y = *reinterpret_cast<const float*>(box + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4);
-        if (p.add) y = __fadd_rn(p.add[t * p.add_stride + n0 + lane], y);
-        static_cast<float*>(p.out)[t * p.out_stride + n0 + lane] = y;
-      } else {
-        static_cast<uint16_t*>(p.out)[t * p.out_stride + n0 + lane] =
-            *reinterpret_cast<const uint16_t*>(box + row * 64 + (((lane >> 3) ^ (row >> 1 & 3)) << 4) + (lane & 7) * 2);
-      }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int odd = first ^ (turns & j), c = 2 * lane + odd;
+      uint16_t* at = o + j * p.out_stride + c;
+      const bool row_ok = r + j < rows;
+      if (row_ok && c + 1 < cols) *reinterpret_cast<uint32_t*>(at) = w[j];
+      if (row_ok && c + 1 == cols) *at = static_cast<uint16_t>(w[j]);
+      if (row_ok && odd && lane == 31) at[-63] = static_cast<uint16_t>(w[j] >> 16);
     }
   }
 }
@@ -767,6 +821,8 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
     const bool results = warp >= 2;
     const int quad = warp & 3, side = (warp - 2) >> 2;
     const int row = quad * 32 + lane;
+    const int own = kUnits / split;                    // 32-column units that this pair writes: own * piece ..
+    const int u0 = own * piece + side * (own / 2), u1 = u0 + own / 2;      // this warp's
     uint8_t* box = smem + L::kBoxOff + (results ? warp - 2 : 0) * L::kBoxBytes;
     int acc = 0, turn = 0;
     uint32_t acc_phase = 0;
@@ -785,7 +841,6 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
         tc_fence_after();
       }
       const uint32_t t_row = tmem_base + acc * 256 + (static_cast<uint32_t>(quad * 32) << 16);
-      const int own = kUnits / split;                  // 32-column units that this pair writes: own * piece ..
       if (split > 1) {
         // Everybody's products are done with the stages: they become [piece][own unit][matrix][4-column group][128 tokens][4].
         cluster_meet();
@@ -811,10 +866,12 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
         cluster_arrive_wait();
       }
       if (results) {
-        const int u0 = own * piece + side * (own / 2);
-        for (int u = u0; u < u0 + own / 2; ++u) {
-          if (!ok || n0 + u * 32 >= p.N) break;
+        for (int u = u0; u < u1; ++u) {
+          const int t0 = token0(tile) + quad * 32, n = n0 + u * 32;
+          if (!ok || n >= p.N) break;
           uint32_t r[32], r2[32];
+          float4 x[8];
+          if (!GATED && out_way == kOutPieces) load_pieces(p, t0, n, lane, x);
           tmem_ld_32x32(t_row + u * 32, r);
           if (GATED) tmem_ld_32x32(t_row + 128 + u * 32, r2);
           tmem_ld_wait();
@@ -833,7 +890,28 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
           }
           float v[32];
           results_of<GATED>(r, r2, as, scales + u * 32, scales + 128 + u * 32, v);
-          write_box(p, &tm_out, box, turn, v, token0(tile) + quad * 32, n0 + u * 32, lane, out_way);
+          uint8_t* to = box + (p.type == kF32 ? 0 : turn * 2048);
+          if (out_way == kOutBoxes && lane == 0) {      // the box that was here has left
+            if (p.type == kF32) tma_store_wait<0>();
+            else tma_store_wait<1>();
+          }
+          __syncwarp();
+          fill_box(to, v, lane, p.type);
+          if (out_way == kOutBoxes) fence_proxy_async();
+          __syncwarp();
+          if (out_way == kOutBoxes) {
+            if (lane == 0 && t0 < p.M) tma_store_2d(&tm_out, to, n, t0);
+            turn ^= 1;
+          } else if (!GATED && out_way == kOutPieces && n + 32 <= p.N) {
+            add_pieces(p, to, t0, n, lane, x);
+          } else if (p.type == kF32) {
+            write_values(p, to, t0, n, lane, 32);
+          } else if (turn || u + 1 == u1 || n + 32 >= p.N) {
+            write_values(p, box, t0, n - 32 * turn, lane, 32 * (turn + 1));
+            turn = 0;
+          } else {
+            turn = 1;                                    // together with the next one
+          }
         }
         tc_fence_before();
         __syncwarp();
@@ -865,7 +943,9 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   int split = 1;
   // Handing sums over takes about as long as the products of 8 k blocks (300 x 1536 x 1536, 12 blocks: 8.0 us whole and cut in two;
   // 421 x 2048 x 2048: 9.6 and 9.1; 300 x 1536 x 3584: 12.9, 10.8 and, in four, 10.4; 735 x 1536 x 8960: 24.6 and 17.7).
-  while (split < (GATED ? 2 : 4) && tiles <= kClusters[0][2 * split] && kblocks >= 14 * split) split *= 2;
+  // fp32 results, whose rows are long to write, gain from more CTAs earlier (1163 x 1536 x 1536 onto the residual: 15.4 and 12.6).
+  const int worth = p.type == kF32 ? 8 : 14;
+  while (split < (GATED ? 2 : 4) && tiles <= kClusters[4 * split] && kblocks >= worth * split) split *= 2;
   const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
   const int bytes = p.type == kF32 ? 4 : 2;
   const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
@@ -901,8 +981,7 @@ Form form_of(int M, int N, int K, bool gated) {
 I8Box gemm_i8_box(int M, int N, int K, bool gated) {
   const Form f = form_of(M, N, K, gated);
   if (f == Form::kVector) return {0, false};
-  if (f == Form::kWide) return {128, K % kBK == 0};
-  return {M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, false};
+  return {f == Form::kWide ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, K % kBK == 0};
 }
 
 bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, I8Box box) {
