@@ -541,8 +541,8 @@ int cs_rmsnorm(const float* x, const float* gain, uint16_t* out, int rows, int d
  *   The codes are those of fp32(x' g), exactly (the root is common to the row); the scale carries the root. Sums in fp32.
  *   x, x_out           device rows of dtype; x_out may be x. delta, x_out: both NULL to norm x as it is.
  *   delta              device rows of delta_dtype: any type for x in CS_F32, else the type of x.
- *   gain               device float [d]; eps >= 0. A row with a NaN or infinity in x' or x' g, or whose squares overflow fp32, is
- *                      left as cs_quantize_i8 leaves one.
+ *   gain               device float [d]; eps >= 0. A row with a NaN or infinity in x' or x' g, or whose squares overflow fp32 or,
+ *                      with eps = 0, vanish in it, is left as cs_quantize_i8 leaves one.
  * For these three, d is a multiple of 16, rows and gains are 16-byte aligned and strides whole 16-byte pieces; rows may be 0.
  *
  * cs_gemm_i8 - with acc[t, n] = sum_k a[t, k] w[n, k] in 32-bit integers (exact) and y = a_scales[t] w_scales[n] acc:
@@ -553,8 +553,9 @@ int cs_rmsnorm(const float* x, const float* gain, uint16_t* out, int rows, int d
  *   a                  device codes, M rows of K, a_stride bytes apart (a multiple of 16).
  *   w, w2              device codes [N, K], contiguous. All codes 16-byte aligned, K a multiple of 16 and at most 131056.
  *   out, add           strides in elements, any that hold a row; aligned to their type.
- *   Any M from 0 and N from 1. Deterministic. No workspace: calls on several streams, and graphs that hold them, may overlap.
- * All are asynchronous on `stream` and may be captured. Pointers belong to the current device.
+ *   M from 0 and N from 1, to 2^30. Deterministic, and a token's results are the same bits in every batch. No workspace: calls on several streams, and graphs that hold them, may overlap.
+ * All are asynchronous on `stream` and may be captured. Pointers belong to the current device. Outputs may not overlap inputs other
+ * than as said.
  * cs_i8_status       synchronises `stream`: CS_ETIMEOUT if a cs_gemm_i8 of the current device has given up on a bounded wait since
  *                    the last query (its output is not to be used), else CS_OK.
  */

@@ -54,7 +54,7 @@ struct LayerDev {
   struct I8 {
     int8_t* codes = nullptr;
     float* scales = nullptr;
-    CUtensorMap tm, tm_deep;       // boxes of one and, where the rows allow it, of two pieces of a row (I8Box)
+    CUtensorMap tm, tm_deep, tm_half;       // boxes of 128 rows, of one piece or (K a multiple of 128) two of a row, and of 64 rows and two
   } qkv8, o8, g8, u8, d8;
 };
 
@@ -657,7 +657,7 @@ struct I8Pass {
   int T;
   cudaStream_t s;
   // Maps of the code buffer for products of this pass: they differ by the length of a row and by the product's form.
-  struct Map { int rows = 0, k = 0; I8Box box = {0, false}; CUtensorMap tm; } maps[8];
+  struct Map { int rows = 0, k = 0; int box = 0; bool deep = false; CUtensorMap tm; } maps[8];
   int n_maps = 0;
 
   cudaError_t norm(float* x, const uint16_t* delta, const float* gain, int rows) {
@@ -697,7 +697,8 @@ struct I8Pass {
     g.weights_settled = 1;
     g.status = m->status;
     const LayerDev::I8& second = w2 ? *w2 : w;
-    return box.deep ? gemm_i8(*ta, w.tm_deep, second.tm_deep, g, s) : gemm_i8(*ta, w.tm, second.tm, g, s);
+    const auto map = [&](const LayerDev::I8& of) { return !box.deep ? of.tm : box.w_rows == 128 ? of.tm_deep : of.tm_half; };
+    return gemm_i8(*ta, map(w), map(second), g, s);
   }
 
  private:
@@ -714,13 +715,14 @@ struct I8Pass {
   }
   const CUtensorMap* map_of(int rows, int k, I8Box box) {
     for (int i = 0; i < n_maps; ++i)
-      if (maps[i].rows == rows && maps[i].k == k && maps[i].box.rows == box.rows && maps[i].box.deep == box.deep) return &maps[i].tm;
+      if (maps[i].rows == rows && maps[i].k == k && maps[i].box == box.rows && maps[i].deep == box.deep) return &maps[i].tm;
     if (n_maps == 8) n_maps = 0;
     Map& e = maps[n_maps++];
     e.rows = rows;
     e.k = k;
-    e.box = box;
-    if (box.rows && !make_i8_map(&e.tm, static_cast<const int8_t*>(m->codes.p), rows, k, k, box)) {
+    e.box = box.rows;
+    e.deep = box.deep;
+    if (box.rows && !make_i8_map(&e.tm, static_cast<const int8_t*>(m->codes.p), rows, k, k, box.rows, box.deep)) {
       --n_maps;
       return nullptr;
     }
@@ -1267,8 +1269,9 @@ static int to_codes(const uint16_t* w, int rows, int d, LayerDev::I8* out, std::
   q.rows = rows;
   q.d = d;
   CS_CUDA(launch_quantize_i8(q, s));
-  if (!make_i8_map(&out->tm, out->codes, rows, d, d, {128, false}) ||
-      (d % 128 == 0 && !make_i8_map(&out->tm_deep, out->codes, rows, d, d, {128, true}))) {
+  if (!make_i8_map(&out->tm, out->codes, rows, d, d, 128, false) ||
+      (d % 128 == 0 && (!make_i8_map(&out->tm_deep, out->codes, rows, d, d, 128, true) ||
+                        !make_i8_map(&out->tm_half, out->codes, rows, d, d, 64, true)))) {
     g_cuda_error = "cuTensorMapEncodeTiled failed for a weight matrix's codes";
     return CS_ECUDA;
   }
@@ -2293,6 +2296,7 @@ int cs_gemm_f16(const uint16_t* a, const uint16_t* w, const uint16_t* w2, void* 
     CS_CUDA(cudaMemset(g_test_turn_flags, 0, sizeof(uint32_t) * kTurnWords));
   }
   TurnOrder turn{g_test_turn_flags, &g_test_turn_epoch};
+  const OrdinaryLaunches ordinary;      // w may be what the kernel in front of this one writes (cs_dequantize_i8, say)
   CS_CUDA(gemm_f16(ta, tb, w2 ? &tb2 : nullptr, out, M, N, K, epilogue == 3 ? kEpiResidAdd : epilogue, g_test_status,
                     static_cast<cudaStream_t>(stream), epilogue == 1 ? &turn : nullptr));
   return CS_OK;
@@ -2413,7 +2417,7 @@ int cs_rmsnorm_i8(const void* x, int64_t x_stride, int dtype, const void* delta,
 int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const int8_t* w, const float* w_scales, const int8_t* w2,
                const float* w2_scales, const float* add, int64_t add_stride, void* out, int64_t out_stride, int M, int N, int K,
                int dtype, void* stream) {
-  if (M < 0 || N < 1 || K < 16 || K % 16 || K > kMaxI8K || !type_bytes(dtype)) return CS_EINVAL;
+  if (M < 0 || M > kMaxI8Rows || N < 1 || N > kMaxI8Rows || K < 16 || K % 16 || K > kMaxI8K || !type_bytes(dtype)) return CS_EINVAL;
   if ((w2 == nullptr) != (w2_scales == nullptr) || (w2 && (add || dtype == CS_F32)) || (add && dtype != CS_F32)) return CS_EINVAL;
   if (M == 0) return CS_OK;
   const auto aligned = [](const void* p, uintptr_t to) { return p && reinterpret_cast<uintptr_t>(p) % to == 0; };
@@ -2422,9 +2426,9 @@ int cs_gemm_i8(const int8_t* a, int64_t a_stride, const float* a_scales, const i
   if (!aligned(out, type_bytes(dtype)) || out_stride < N) return CS_EINVAL;
   if (add && (!aligned(add, 4) || add_stride < N || (add == out && add_stride != out_stride && M > 1))) return CS_EINVAL;
   CUtensorMap ta, tw, tw2;
-  const I8Box box = gemm_i8_box(M, N, K, w2 != nullptr), of_w = {128, box.deep};
-  if (box.rows && (!make_i8_map(&ta, a, M, K, a_stride, box) || !make_i8_map(&tw, w, N, K, K, of_w) ||
-                   (w2 && !make_i8_map(&tw2, w2, N, K, K, of_w)))) {
+  const I8Box box = gemm_i8_box(M, N, K, w2 != nullptr);
+  if (box.rows && (!make_i8_map(&ta, a, M, K, a_stride, box.rows, box.deep) || !make_i8_map(&tw, w, N, K, K, box.w_rows, box.deep) ||
+                   (w2 && !make_i8_map(&tw2, w2, N, K, K, box.w_rows, box.deep)))) {
     g_cuda_error = "cuTensorMapEncodeTiled failed";
     return CS_ECUDA;
   }

@@ -6,6 +6,8 @@
 
 namespace cs {
 
+thread_local int g_ordinary_launches = 0;
+
 namespace {
 
 thread_local int64_t g_launches = 0;

@@ -2,12 +2,12 @@
 // (tcgen05, kind::i8) and exact, whatever its order.
 //
 // Three forms by the number of tokens; a token has the same bits in all of them.
-//   up to 8     vector: integer dot products of the ordinary cores, weights straight from global memory into registers
+//   a few       vector: integer dot products of the ordinary cores, weights straight from global memory into registers
 //   up to 128   narrow: the weights are the 128-row side of the product and the tokens its columns, so that a few tokens cost a few
 //               columns; a CTA owns 128 output channels, all tokens and a piece of the k range, and the pieces of a tile are the
 //               CTAs of a cluster, each of which collects the others' sums for its share of the tokens through distributed shared
 //               memory
-//   more        wide: pairs of CTAs over 256 tokens x 256 rows of weights (below)
+//   more        wide: pairs of CTAs over 256 tokens x 256 (or 128) rows of weights (below)
 // Nothing is kept between calls and no global memory is used in between.
 #include "i8.h"
 
@@ -488,12 +488,15 @@ cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const
 // tokens in its tensor memory, in one of two accumulators. Per SM and k block 32 KB are fetched for 512 cycles of products, half of
 // what two separate 128 x 256 tiles would fetch.
 constexpr int kWideThreads = 320;                      // warp 0: copies, warp 1: products, warps 2-9: results
+// BN: rows of weights in a tile, each CTA holding half of them.
+template <int BN>
 struct Wide {
-  // Two k blocks of both operands. A box costs the copy engine about 60 cycles besides its bytes, so that boxes of two blocks (32 KB)
-  // leave 90 % of the time that boxes of one do.
-  static constexpr int kOperandBytes = 2 * kTileBytes;
-  static constexpr int kStageBytes = 2 * kOperandBytes;
-  static constexpr int kStages = 3;
+  // Two k blocks of both operands. A box costs the copy engine about 190 cycles besides its bytes, at 92 a cycle, so that two blocks a
+  // box (32 KB) take 535 cycles a block, which the products take as well, and boxes of one take 735 (8192^3 363 us against 415).
+  static constexpr int kWBlock = BN / 2 * kBK;
+  static constexpr int kTokenBytes = 2 * kTileBytes;
+  static constexpr int kStageBytes = kTokenBytes + 2 * kWBlock;
+  static constexpr int kStages = BN == 256 ? 3 : 4;
   static constexpr int kBoxOff = kStages * kStageBytes;               // [8 warps] 32 rows of 32 results on their way out
   static constexpr int kBoxBytes = 4096;
   static constexpr int kScaleOff = kBoxOff + 8 * kBoxBytes;           // [256] scales of the tile's weights
@@ -679,14 +682,15 @@ __device__ __forceinline__ void write_values(const GemmI8& p, const uint8_t* box
   }
 }
 
-template <bool GATED>
+template <bool GATED, int BN>
 __global__ void __launch_bounds__(kWideThreads, 1)
 gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_w,
                     const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_out, const GemmI8 p, int t_tiles,
                     int tiles, int split, int out_way, int deep) {
-  using L = Wide;
-  constexpr uint32_t kIdesc = idesc_i8(256, 256);
-  constexpr int kOut = GATED ? 128 : 256;              // output columns of a tile
+  using L = Wide<BN>;
+  constexpr uint32_t kIdesc = idesc_i8(256, BN);
+  constexpr int kOut = GATED ? BN / 2 : BN;            // output columns of a tile
+  static_assert(!GATED || BN == 256, "the second matrix's sums begin at column 128");
   constexpr int kUnits = kOut / 32;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -736,18 +740,18 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   // Token tiles run fastest: tiles that are in work together share their weights, and every weight is read from DRAM about once.
   const auto token0 = [&](int tile) { return (tile % t_tiles) * 256 + static_cast<int>(half) * 128; };
   const auto column0 = [&](int tile) { return tile / t_tiles * kOut; };
-  const auto load = [&](uint8_t* dst, const CUtensorMap* m, uint32_t bar, int kp, int row) {
+  const auto load = [&](uint8_t* dst, const CUtensorMap* m, uint32_t bar, int kp, int row, int block) {
     if (deep) {
       tma_load_3d_pair(dst, m, bar, 0, row, 2 * kp);
     } else {
       tma_load_2d_pair(dst, m, bar, 2 * kp * kBK, row);
-      tma_load_2d_pair(dst + kTileBytes, m, bar, (2 * kp + 1) * kBK, row);      // zeros behind the last block
+      tma_load_2d_pair(dst + block, m, bar, (2 * kp + 1) * kBK, row);      // zeros behind the last block
     }
   };
   const auto load_w = [&](int stage, uint32_t bar, int kp, int tile) {
-    uint8_t* dst = smem + stage * L::kStageBytes + L::kOperandBytes;
-    if (GATED) load(dst, half ? &tm_w2 : &tm_w, bar, kp, column0(tile));
-    else load(dst, &tm_w, bar, kp, column0(tile) + static_cast<int>(half) * 128);
+    uint8_t* dst = smem + stage * L::kStageBytes + L::kTokenBytes;
+    if (GATED) load(dst, half ? &tm_w2 : &tm_w, bar, kp, column0(tile), L::kWBlock);
+    else load(dst, &tm_w, bar, kp, column0(tile) + static_cast<int>(half) * (BN / 2), L::kWBlock);
   };
   int ahead = 0;
   if (threadIdx.x == 0 && p.weights_settled && first < tiles) {
@@ -771,7 +775,7 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
             if (!half) mbar_arrive_expect_tx(&full_bar[stage], 2 * L::kStageBytes);
             load_w(stage, bar, kp, tile);
           }
-          load(smem + stage * L::kStageBytes, &tm_a, bar, kp, token0(tile));
+          load(smem + stage * L::kStageBytes, &tm_a, bar, kp, token0(tile), kTileBytes);
           if (++stage == L::kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -785,7 +789,7 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
       bool ready = false;
-      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem)), bdesc0 = umma_desc_k128(smem_u32(smem) + L::kOperandBytes);
+      const uint64_t adesc0 = umma_desc_k128(smem_u32(smem)), bdesc0 = umma_desc_k128(smem_u32(smem) + L::kTokenBytes);
       for (int tile = first; tile < tiles && ok; tile += step) {
         if (!mbar_wait(&acc_empty[acc], acc_phase ^ 1u, abort_flag, status)) { ok = false; break; }
         tc_fence_after();
@@ -799,7 +803,7 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
           if (elect_one()) {
             umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off, bdesc0 + off, kIdesc, kp != kp0);
             if (2 * kp + 1 < kblocks)
-              umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off + (kTileBytes >> 4), bdesc0 + off + (kTileBytes >> 4), kIdesc, 1);
+              umma_i8_pair_block(tmem_base + acc * 256, adesc0 + off + (kTileBytes >> 4), bdesc0 + off + (L::kWBlock >> 4), kIdesc, 1);
             umma_commit_pair(&empty_bar[stage], pair_mask);
           }
           __syncwarp();
@@ -932,12 +936,12 @@ gemm_i8_wide_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_const
   }
 }
 
-template <bool GATED>
+template <bool GATED, int BN>
 cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
   static std::atomic<uint64_t> opted{0};
-  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_wide_kernel<GATED>, Wide::kTotal, opted); e != cudaSuccess) return e;
-  constexpr int kPairs = kNumSMs / 2;
-  const int64_t t_tiles = (p.M + 255) / 256, n_tiles = (p.N + (GATED ? 127 : 255)) / (GATED ? 128 : 256), tiles = t_tiles * n_tiles;
+  if (cudaError_t e = opt_in_dynamic_smem(gemm_i8_wide_kernel<GATED, BN>, Wide<BN>::kTotal, opted); e != cudaSuccess) return e;
+  constexpr int kPairs = kNumSMs / 2, kOut = GATED ? BN / 2 : BN;
+  const int64_t t_tiles = (static_cast<int64_t>(p.M) + 255) / 256, n_tiles = (p.N + kOut - 1) / kOut, tiles = t_tiles * n_tiles;
   if (tiles > 0x3fffffff) return cudaErrorInvalidValue;
   const int kblocks = (p.K + kBK - 1) / kBK;
   int split = 1;
@@ -945,7 +949,7 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   // 421 x 2048 x 2048: 9.6 and 9.1; 300 x 1536 x 3584: 12.9, 10.8 and, in four, 10.4; 735 x 1536 x 8960: 24.6 and 17.7).
   // fp32 results, whose rows are long to write, gain from more CTAs earlier (1163 x 1536 x 1536 onto the residual: 15.4 and 12.6).
   const int worth = p.type == kF32 ? 8 : 14;
-  while (split < (GATED ? 2 : 4) && tiles <= kClusters[4 * split] && kblocks >= worth * split) split *= 2;
+  while (BN == 256 && split < (GATED ? 2 : 4) && tiles <= kClusters[4 * split] && kblocks >= worth * split) split *= 2;
   const int clusters = split > 1 ? static_cast<int>(tiles) : static_cast<int>(std::min<int64_t>(tiles, kPairs));
   const int bytes = p.type == kF32 ? 4 : 2;
   const bool pieces = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && p.out_stride * bytes % 16 == 0 &&
@@ -955,7 +959,7 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
   if (out_way == kOutBoxes && !make_map(&tm_out, p.out, bytes == 4 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16,
                                         bytes, p.M, p.N, p.out_stride, 32, 32))
     return cudaErrorInvalidValue;
-  const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide::kTotal, s,
+  const cudaError_t e = launch_pdl_cluster(gemm_i8_wide_kernel<GATED, BN>, dim3(clusters * 2 * split), dim3(kWideThreads), Wide<BN>::kTotal, s,
                                            2 * split, ta, tw, tw2, tm_out, p, static_cast<int>(t_tiles), static_cast<int>(tiles), split,
                                            out_way, p.K % kBK == 0 ? 1 : 0);
   count_launch();
@@ -965,27 +969,35 @@ cudaError_t launch_wide(const CUtensorMap& ta, const CUtensorMap& tw, const CUte
 }  // namespace
 
 namespace {
-enum class Form { kVector, kNarrow, kWide };
-// Which form. The vector form is bound by its dot products from about 2^26 products on (4 tokens x 1536 x 8960 6.4 us against 8.3
-// narrow, 8 tokens 8.2 and 8.4; gated 4 x 8960 x 1536 9.0 and 8.7, 8 x 18944 x 3584 40.7 and 26.0), except that one and two tokens
-// never are. Between 64 and 128 tokens the wide form wins where its tiles occupy half of the pairs (gated 128 x 8960 x 1536 12.6 us
-// against 14.4; 128 x 2048 x 1536 8.8 and 7.3).
+enum class Form { kVector, kNarrow, kWide, kWideHalf };
+// Which form, as measured (us; weights not in L2).
+// Vector: its dot products bind it from about 2^26 on (4 tokens x 1536 x 8960 5.4 against 6.8 narrow, 8 tokens 8.2 and 6.9; gated
+// 4 x 8960 x 1536 9.0 and 8.8, 8 x 18944 x 3584 40 and 25), except that one and two tokens never do.
+// Wide with tiles of 128 rows of weights (half): where all of them still run at once and the sum is not long. Their copies take 460
+// cycles a block for half of the products, but a tile's end takes half as long and no sums are handed over (1163 x 1536 x 1536 6.9
+// against 8.4 of whole tiles, 421 x 2048 x 2048 7.4 and 9.1, 421 x 2048 x 6144 14.3 and 13.8 cut in two, 1163 x 1792 x 4608, whose whole
+// tiles are too many to be cut, 12.4 and 15.4).
+// Between 64 and 128 tokens: narrow, unless whole tiles occupy half of the pairs (gated 128 x 8960 x 1536 10.9 against 14.0 narrow) or
+// halves have a short sum (128 x 2048 x 1536 6.2 and 8.6; 128 x 3584 x 3584 10.1 and 9.6).
 Form form_of(int M, int N, int K, bool gated) {
   const int64_t weights = static_cast<int64_t>(N) * K * (gated ? 2 : 1);
   if (M <= 2 || (M <= kVectorTokens && weights * (M <= 4 ? 4 : 8) <= 1 << 26)) return Form::kVector;
-  const int wide_tiles = N / (gated ? 128 : 256);
-  return M <= (wide_tiles > kNumSMs / 4 ? 64 : kNarrowTokens) ? Form::kNarrow : Form::kWide;
+  if (M <= 64) return Form::kNarrow;
+  const auto tiles = [&](int columns) { return (static_cast<int64_t>(M) + 255) / 256 * ((static_cast<int64_t>(N) + columns - 1) / columns); };
+  const bool halves = !gated && K % kBK == 0 && tiles(128) <= kNumSMs / 2;
+  if (M <= kNarrowTokens && tiles(gated ? 128 : 256) <= kNumSMs / 4 && !(halves && K <= 20 * kBK)) return Form::kNarrow;
+  return halves && (K < 44 * kBK || tiles(256) > kClusters[4]) ? Form::kWideHalf : Form::kWide;
 }
 }  // namespace
 
 I8Box gemm_i8_box(int M, int N, int K, bool gated) {
   const Form f = form_of(M, N, K, gated);
-  if (f == Form::kVector) return {0, false};
-  return {f == Form::kWide ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, K % kBK == 0};
+  if (f == Form::kVector) return {0, 0, false};
+  return {f != Form::kNarrow ? 128 : M <= 16 ? 16 : M <= 32 ? 32 : M <= 64 ? 64 : 128, f == Form::kWideHalf ? 64 : 128, K % kBK == 0};
 }
 
-bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, I8Box box) {
-  return make_map(tm, const_cast<int8_t*>(base), CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, stride, box.rows, kBK, box.deep ? 2 : 1);
+bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows, bool deep) {
+  return make_map(tm, const_cast<int8_t*>(base), CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, rows, k, stride, box_rows, kBK, deep ? 2 : 1);
 }
 
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s) {
@@ -994,7 +1006,8 @@ cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensor
   switch (form_of(p.M, p.N, p.K, gated)) {
     case Form::kVector: return gated ? launch_vector<true>(p, s) : launch_vector<false>(p, s);
     case Form::kNarrow: return gated ? launch_by_tokens<true>(ta, tw, tw2, p, s) : launch_by_tokens<false>(ta, tw, tw, p, s);
-    default: return gated ? launch_wide<true>(ta, tw, tw2, p, s) : launch_wide<false>(ta, tw, tw, p, s);
+    case Form::kWideHalf: return launch_wide<false, 128>(ta, tw, tw, p, s);
+    default: return gated ? launch_wide<true, 256>(ta, tw, tw2, p, s) : launch_wide<false, 256>(ta, tw, tw, p, s);
   }
 }
 

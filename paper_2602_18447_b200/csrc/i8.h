@@ -11,6 +11,8 @@ namespace cs {
 constexpr int kF16 = 0, kBF16 = 1, kF32 = 2;
 // The largest K whose sum of products of any two 8-bit codes fits 32 bits: 2^14 K < 2^31.
 constexpr int kMaxI8K = 131056;
+// Tokens and output channels of a product at most.
+constexpr int kMaxI8Rows = 1 << 30;
 
 struct QuantRows {
   const void* x;            // [rows, >= d] of `type`, rows x_stride elements apart
@@ -40,15 +42,15 @@ struct GemmI8 {
   int32_t weights_settled;      // nothing that may still run before this launch writes the weights
   uint32_t* status;             // null: the word that i8_status reads
 };
-// How a product reads its operands: boxes of so many rows (0: no maps), of one 128-byte piece of every row or of two (deep).
+// How a product reads its operands: boxes of so many rows of the activations (0: no maps) and of the weights, of one 128-byte piece
+// of every row or of two (deep).
 struct I8Box {
-  int rows;
+  int rows, w_rows;
   bool deep;
 };
-// The box of the activations' map for such a product; the weights' boxes have 128 rows and are as deep.
 I8Box gemm_i8_box(int M, int N, int K, bool gated);
 // Map over [rows, k] codes, rows `stride` bytes apart, 128-byte swizzle. k a multiple of 128 for deep boxes.
-bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, I8Box box);
+bool make_i8_map(CUtensorMap* tm, const int8_t* base, int rows, int k, int64_t stride, int box_rows, bool deep);
 // out = the codes' product times both scales (+ add), or silu(first) * second. K a multiple of 16, at most kMaxI8K. Maps as gemm_i8_box
 // says; tw2 is read for gated products only.
 cudaError_t gemm_i8(const CUtensorMap& ta, const CUtensorMap& tw, const CUtensorMap& tw2, const GemmI8& p, cudaStream_t s);

@@ -225,6 +225,14 @@ cudaError_t launch_range_check_selftest(uint32_t* status, cudaStream_t s);
 // Failure-detection self-test: a bounded wait that is made to run out (see cs_selftest_wait_timeout).
 cudaError_t launch_wait_timeout_selftest(uint32_t* status, uint32_t limit, int32_t* gave_up, cudaStream_t s);
 
+// While one lives on this host thread, launches are ordinary ones: for a kernel that reads some of its inputs before it waits for its
+// predecessor, at an entry where nobody knows that the predecessor does not write them.
+extern thread_local int g_ordinary_launches;
+struct OrdinaryLaunches {
+  OrdinaryLaunches() { ++g_ordinary_launches; }
+  ~OrdinaryLaunches() { --g_ordinary_launches; }
+};
+
 // Launch with programmatic stream serialisation (see pdl_wait in common.cuh).
 template <typename... KArgs, typename... Args>
 cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, Args&&... args) {
@@ -237,7 +245,7 @@ cudaError_t launch_pdl(void (*kernel)(KArgs...), dim3 grid, dim3 block, size_t s
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = g_ordinary_launches ? 0 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, KArgs(args)...);
 }
 

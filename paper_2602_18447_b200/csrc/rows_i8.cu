@@ -218,11 +218,11 @@ __global__ void __launch_bounds__(NV == 4 ? 640 : 1024, NV == 4 && TYPE != kF32 
 
   const float most = s.most;
   bool good = most < __uint_as_float(0x7f800000u);
-  const float mean = NORM ? s.squares / static_cast<float>(p.d) + p.eps : 1.f;
-  if (NORM) good = good && mean < __uint_as_float(0x7f800000u) && (mean > 0.f || most == 0.f);
+  // the squares' mean has to be a normal number, or eps to stand in for it
+  if (NORM) good = good && s.squares < __uint_as_float(0x7f800000u) && (s.squares >= p.d * 0x1p-126f || p.eps > 0.f || most == 0.f);
   if (threadIdx.x == 0) {
     float scale = most / 127.0f;
-    if (NORM && most > 0.f) scale = most / sqrtf(mean) / 127.0f;
+    if (NORM && most > 0.f) scale = most / sqrtf(s.squares / static_cast<float>(p.d) + p.eps) / 127.0f;
     p.scales[row] = good ? scale : __uint_as_float(0x7fffffffu);
   }
   // Rows far from 1 are brought nearer, by a power of two, so that neither inv nor a product leaves the normal range; values that this
@@ -329,7 +329,7 @@ cudaError_t launch_rows(const QuantRows& p, cudaStream_t s) {
   const auto kernel = nv == 4   ? quantize_i8_kernel<TYPE, DELTA, NORM, 4>
                       : nv == 2 ? quantize_i8_kernel<TYPE, DELTA, NORM, 2>
                                 : quantize_i8_kernel<TYPE, DELTA, NORM, NORM ? 1 : 2>;
-  const cudaError_t e = launch_pdl(kernel, dim3((p.rows + together - 1) / together), dim3(threads, together), 0, s, p);
+  const cudaError_t e = launch_pdl(kernel, dim3(static_cast<unsigned>((static_cast<int64_t>(p.rows) + together - 1) / together)), dim3(threads, together), 0, s, p);
   count_launch();
   return e != cudaSuccess ? e : cudaGetLastError();
 }

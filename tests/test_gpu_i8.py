@@ -174,6 +174,12 @@ def test_norm_of_extreme_rows(B):
     assert np.array_equal(_np(codes)[good], want[good])
     I.check(_np(scales)[good], scale[good], bound[good])
     assert np.isnan(_np(scales)[[1, 2, 3]]).all() and not _np(codes)[[1, 2, 3]].any()      # 1e18 * 1e30 is none either
+    B.cs_rmsnorm_i8(_dev(x), _dev(gain), codes, scales, 0.0)                               # the squares of 1e-30 vanish
+    want, scale, bound = I.norm(x, gain, 0.0, 64)
+    good = [4, 5]
+    assert np.array_equal(_np(codes)[good], want[good])
+    I.check(_np(scales)[good], scale[good], bound[good])
+    assert np.isnan(_np(scales)[:4]).all() and not _np(codes)[:4].any()
 
 
 # ----------------------------------------------------------------------------------------------------------- products
@@ -373,3 +379,54 @@ def test_a_block_as_it_is_used_and_replayed(B, M):
         torch.cuda.synchronize()
         hold()
     B.cs_i8_status()
+
+
+def test_first_calls_inside_a_capture():
+    """Nothing has to be prepared outside: a process whose first call of every form is captured."""
+    import subprocess
+    import sys
+    import os
+    code = """
+import torch
+from paper_2602_18447_b200 import binding as B
+B.load_library()
+w, sw = torch.ones(300, 256, dtype=torch.int8, device="cuda"), torch.ones(300, device="cuda")
+x = torch.ones(700, 256, device="cuda")
+c, s, y = torch.zeros(700, 256, dtype=torch.int8, device="cuda"), torch.zeros(700, device="cuda"), torch.zeros(700, 256, device="cuda")
+outs = [torch.zeros(m, 300, device="cuda") for m in (1, 20, 700)]
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    B.cs_rmsnorm_i8(x, x[0].contiguous(), c, s, 0.0)
+    B.cs_quantize_i8(x, c, s)
+    for o in outs:
+        B.cs_gemm_i8(c[:len(o)], s[:len(o)], w, sw, o)
+    B.cs_dequantize_i8(c, s, y)
+g.replay()
+torch.cuda.synchronize()
+assert all((o - 256).abs().max() < 1e-3 for o in outs) and (y - 1).abs().max() < 1e-6, [o[0, 0] for o in outs]
+B.cs_i8_status()
+print("fine")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, cwd=root)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stderr[-2000:]
+
+
+def test_values_read_back_are_a_product_s_weights(B):
+    """The fp16 product asks for its weights before anything else: they have to be there when the call in front of it writes them."""
+    import torch
+    g = np.random.default_rng(3)
+    c, s = I.codes_of(g, 4096, 512)
+    dc, ds = _dev(c), _dev(s)
+    a = _dev(g.standard_normal((64, 512)), "f16")
+    w = [torch.zeros(4096, 512, dtype=torch.float16, device="cuda") for _ in range(2)]
+    ref, out = (torch.empty(64, 4096, dtype=torch.float16, device="cuda") for _ in range(2))
+    B.cs_dequantize_i8(dc, ds, w[0])
+    torch.cuda.synchronize()
+    B.cs_gemm_f16(a, w[0], None, ref, 64, 4096, 512, 0)
+    for _ in range(20):
+        w[1].zero_()
+        B.cs_dequantize_i8(dc, ds, w[1])
+        B.cs_gemm_f16(a, w[1], None, out, 64, 4096, 512, 0)
+        assert torch.equal(out, ref)
