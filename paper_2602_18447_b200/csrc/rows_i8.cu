@@ -6,6 +6,8 @@
 // fp32(x g), and only the scale carries the factor. A row that holds a NaN or an infinity gets codes of 0 and the scale NaN.
 //
 // Bound by memory: a row is read once, held in registers while its maximum (and the sum of its squares) is formed, and written.
+// 5377 x 8960 bf16: 28.7 us, 5.0 TB/s of reads and writes, and 26.5 us, 5.5 TB/s, back again; norm and residual of 8191 x 3584 bf16:
+// 36.1 us, 5.7 TB/s; of one row of 1536: 1.9 us, a round trip to memory and the two exchanges over the block.
 #include "i8.h"
 
 #include <algorithm>
@@ -76,6 +78,12 @@ __device__ __forceinline__ Inverse inverse_of(float most) {
   const uint32_t near = __float_as_uint(__fdividef(127.0f, most));      // off by two steps at most
   return {__uint_as_float(near + 3), __uint_as_float(near - 3), most};
 }
+__device__ __forceinline__ uint2 low_bytes(const uint32_t (&b)[8]) {
+  uint2 r;
+  r.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+  r.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+  return r;
+}
 // Eight codes. 1.5 * 2^23 added in the same rounding as the product leaves the nearest integer in the low bits of the sum. Where the
 // two inverses give one integer, it is the quotient's. Else the half between the two is compared with the quotient exactly: the sign
 // of 127 y - half * most, both products as a rounded part and its error. (One value in twenty thousand; in 16-bit rows half of the
@@ -106,10 +114,19 @@ __device__ __forceinline__ uint2 codes8(const float (&y)[8], const Inverse& by) 
       for (int j = 0; j < 8; ++j) b[j] = at == j ? __float_as_uint(c + kMagic) : b[j];
     }
   }
-  uint2 r;
-  r.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-  r.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
-  return r;
+  return low_bytes(b);
+}
+// Eight codes of a row that came in 16 bits. Let y have the significand m < 2^11. 127 y / A is a tie, or it is off the next one by
+// 1 / (254 m) > 2^-19 of itself at least, as 254 y - (2 k + 1) A is a whole number of units of y's last place; `up` is off by five
+// steps at most, 5 * 2^-23. So one product decides all but the ties. Of those, A / 2 goes to 64, as its product with `up` does; others
+// need a significand of A that 127, a prime, divides (`ties`; one row in 128). Without the second product and without A / 2, which two
+// warps' pieces in five hold, among the doubtful 5377 x 8960 bf16 takes 33.6 -> 28.9 us.
+__device__ __forceinline__ uint2 codes8_of_16_bits(const float (&y)[8], const Inverse& by, bool ties) {
+  if (ties) return codes8(y, by);
+  uint32_t b[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) b[j] = __float_as_uint(fmaf(y[j], by.up, 12582912.0f));
+  return low_bytes(b);
 }
 // The larger of m and |v|; NaN if either is.
 __device__ __forceinline__ float larger(float m, float v) {
@@ -230,6 +247,7 @@ __global__ void __launch_bounds__(NV == 4 ? 640 : 1024, NV == 4 && TYPE != kF32 
   const float by = most < 0x1p-60f ? 0x1p90f : most > 0x1p100f ? 0x1p-60f : 1.0f;
   const Inverse inverse = inverse_of(most * by);
   const bool any = good && most > 0.f;
+  const bool ties = ((__float_as_uint(inverse.most) & 0x7fffffu) | 0x800000u) % 127u == 0;
   uint2* codes = reinterpret_cast<uint2*>(p.codes + row * p.d);
   const auto put = [&](int unit, const Piece<TYPE>& a) {
     float v[8];
@@ -239,7 +257,9 @@ __global__ void __launch_bounds__(NV == 4 ? 640 : 1024, NV == 4 && TYPE != kF32 
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] *= by;
     }
-    codes[unit] = any ? codes8(v, inverse) : make_uint2(0u, 0u);
+    uint2 c = make_uint2(0u, 0u);
+    if (any) c = !NORM && TYPE != kF32 ? codes8_of_16_bits(v, inverse, ties) : codes8(v, inverse);
+    codes[unit] = c;
   };
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -317,9 +337,10 @@ __global__ void __launch_bounds__(256) rope_rows_kernel(__half* rows, int row_el
 template <int TYPE, int DELTA, bool NORM>
 cudaError_t launch_rows(const QuantRows& p, cudaStream_t s) {
   // Pieces a thread. What a thread does once for a row costs as much as ten values, so many rows take four pieces where that leaves
-  // four warps to a row (8191 x 3584 bf16: 36.0 us, two pieces 39.1; 1163 x 1536 fp16: 3.7 and 3.2), fp32 rows two, whose registers
-  // are twice as many (2048 x 3584: 8.1 either way; norm of 5377 x 1536: 18.4 and 17.5). Few rows are bound by latency: two pieces,
-  // the norm, whose loads are three, one (16 x 1536: 2.0 us against 2.3 with two and 2.8 with four).
+  // four warps to a row (8191 x 3584 bf16 with its norm: 36.1 us, two pieces 39.5; 5377 x 8960 bf16: 28.7, two 38.8, eight, which
+  // leave an SM too few rows, 37.9; 1163 x 1536 fp16: two 3.1, four 3.7), fp32 rows two, whose registers are twice as many (2048 x
+  // 3584: 8.1 either way; norm of 5377 x 1536: 17.5, four 18.4). Few rows are bound by latency: two pieces, the norm, whose loads are
+  // three, one (16 x 1536: 2.0 us against 2.3 with two and 2.8 with four).
   const int units = p.d >> 3;
   const bool few = p.rows <= kNumSMs;
   int nv = units > (TYPE == kF32 ? 2048 : 256) && !few ? 4 : 2;

@@ -83,6 +83,26 @@ def test_every_border_of_a_code(B):
     I.check(_np(scales), *I.scale_of(most))
 
 
+@pytest.mark.parametrize("kind, exponents", [("f16", (0, 1, 15, 30)), ("bf16", (0, 1, 60, 127, 230, 254))])
+def test_every_code_of_16_bits(B, kind, exponents):
+    """Every number of the type, of both signs, in rows of every largest magnitude that an exponent has. The quotient of numbers of 11
+    bits and less is rounded to 53 bits without reaching or leaving a half."""
+    import torch
+    t, bits = I.torch_type(kind), 10 if kind == "f16" else 7
+    every = torch.arange(65536, dtype=torch.int32, device="cuda").to(torch.int16)
+    every = torch.where(torch.isfinite(every.view(t)), every, 0)
+    for e in exponents:
+        tops = (torch.arange(1 << bits, dtype=torch.int32, device="cuda") + (e << bits)).to(torch.int16)
+        tops = tops[tops > 0]
+        for i in range(0, len(tops), 128):
+            top = tops[i:i + 128, None]
+            x = torch.where((every & 0x7fff) <= top, every, 0).view(t)
+            codes = torch.empty(x.shape, dtype=torch.int8, device="cuda")
+            scales = torch.empty(len(top), device="cuda")
+            B.cs_quantize_i8(x, codes, scales)
+            assert torch.equal(codes.double(), torch.round(127.0 * x.double() / top.view(t).double()))
+
+
 @pytest.mark.parametrize("kind", ["f16", "bf16", "f32"])
 def test_rows_of_zeros_and_of_no_numbers(B, kind):
     import torch
