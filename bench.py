@@ -614,6 +614,8 @@ def main():
     args = ap.parse_args()
     if args.gpus > 1 and "WORLD_SIZE" not in os.environ and args.cascade is None:
         sys.exit(spawn_replicas(args.gpus, sys.argv[1:]))
+    if args.cascade is not None and args.projections != "f16":
+        ap.error("--projections goes with the single-model workloads")
     if args.cascade is not None:
         run_cascade(args)
         return

@@ -553,7 +553,8 @@ int cs_rmsnorm(const float* x, const float* gain, uint16_t* out, int rows, int d
  *   a                  device codes, M rows of K, a_stride bytes apart (a multiple of 16).
  *   w, w2              device codes [N, K], contiguous. All codes 16-byte aligned, K a multiple of 16 and at most 131056.
  *   out, add           strides in elements, any that hold a row; aligned to their type.
- *   M from 0 and N from 1, to 2^30. Deterministic, and a token's results are the same bits in every batch. No workspace: calls on several streams, and graphs that hold them, may overlap.
+ *   M from 0 and N from 1, to 2^30. Deterministic, and a token's results are the same bits in every batch. No workspace: calls on
+ *   several streams, and graphs that hold them, may overlap.
  * All are asynchronous on `stream` and may be captured. Pointers belong to the current device. Outputs may not overlap inputs other
  * than as said.
  * cs_i8_status       synchronises `stream`: CS_ETIMEOUT if a cs_gemm_i8 of the current device has given up on a bounded wait since

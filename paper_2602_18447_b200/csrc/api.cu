@@ -880,7 +880,7 @@ int run_layers(cs_model* m, const cs_kv* kv, cs_kv* append_kv, const BatchLayout
     }
     if (append_kv) CS_STEP(kProfOther, append());
     if (m->i8) {
-      const bool last = l == d.n_layers - 1;           // of a verification: as below, the MLP of the steps' last rows alone
+      const bool last = l == d.n_layers - 1;           // behind its attention only the steps' last rows are read, of a prefill none
       CS_STEP(kProfOther, i8.quantize(attn_o, m->q_dim, T));
       CS_STEP(kProfO, i8.product(lw.o8, nullptr, a, last ? x : nullptr, T, d.d_model, m->q_dim));
       if (last) {
