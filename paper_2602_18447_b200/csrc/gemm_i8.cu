@@ -151,7 +151,8 @@ __device__ __forceinline__ int dot16(uint4 a, uint4 b, int s) {
 }
 
 // A CTA holds eight rows of weights (gated: four of each matrix), its warps and lanes 16 codes of k at a time. Bound by reading the
-// weights.
+// weights: 1 x 1536 x 8960 4.7 us, 2.9 TB/s; smaller ones by latency (1 x 2048 x 1536 2.0 us), which is why all eight rows' loads leave
+// before the first is used and before the tokens are waited for.
 template <int TOKENS, bool GATED, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS)
 gemm_i8_vector_kernel(const int8_t* a, int64_t a_stride, const int8_t* w, const int8_t* w2, const GemmI8 p) {
@@ -223,6 +224,9 @@ cudaError_t launch_vector(const GemmI8& p, cudaStream_t s) {
 }
 
 // -------------------------------------------------------------------------------------------------------- narrow form
+// Bound by reading the weights too: gated 8 x 18944 x 3584 25.0 us, 5.4 TB/s; 16 x 3584 x 18944 onto the residual 15.7 us, 4.4 TB/s (28
+// tiles in clusters of four are 112 CTAs, and clusters of five are too many for the GPU). With 64 tokens and more the products' ends
+// count: 64 x 1536 x 8960 8.5 us.
 constexpr int kNarrowTokens = 128;
 constexpr int kNarrowThreads = 320;         // warp 0: copies, warp 1: products, warps 2-9: results
 
@@ -486,7 +490,9 @@ cudaError_t launch_by_tokens(const CUtensorMap& ta, const CUtensorMap& tw, const
 // Two CTAs (a pair) share a tile of 256 tokens x 256 rows of weights (gated: 128 of each matrix): each holds 128 rows of either
 // operand, the leader issues products that read both CTAs' shared memory (cta_group::2), and each keeps the sums of its own 128
 // tokens in its tensor memory, in one of two accumulators. Per SM and k block 32 KB are fetched for 512 cycles of products, half of
-// what two separate 128 x 256 tiles would fetch.
+// what two separate 128 x 256 tiles would fetch. Bound by the tensor cores where tiles are many: gated 5377 x 8960 x 1536 101 us, 2910
+// Top/s, gated 2038 x 18944 x 3584 168-175 us, 3200 Top/s; by the last turn of tiles at 350 of them (gated 1163 x 8960 x 1536 26.6 us,
+// 2400 Top/s); by the copies, the exchange of sums and the ends where they are few (1163 x 1536 x 8960 17.8 us, 1800 Top/s).
 constexpr int kWideThreads = 320;                      // warp 0: copies, warp 1: products, warps 2-9: results
 // BN: rows of weights in a tile, each CTA holding half of them.
 template <int BN>
