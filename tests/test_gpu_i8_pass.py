@@ -121,6 +121,9 @@ CASES = [
     ("1.5B-shaped, 2 layers", scaled_config("cfg2_1p5b_b16", n_layers=2, batch=5, vocab=4104)),
     ("1.7B-shaped, short steps", scaled_config("cfg7_q3_short", n_layers=1, batch=9, vocab=4104)),
     ("1.7B-shaped, short steps, 8-bit cache", scaled_config("cfg9_q3_short_fp8", n_layers=1, batch=9, vocab=4104)),
+    ("tiny, five heads to turn", replace(get_config("cfg1_tiny"), batch=5, model=replace(get_config("cfg1_tiny").model, n_kv_heads=1))),
+    ("tiny, second family, nine heads to turn",
+     replace(get_config("cfg8_tiny_qknorm"), model=replace(get_config("cfg8_tiny_qknorm").model, n_q_heads=6, n_kv_heads=3))),
 ]
 
 
